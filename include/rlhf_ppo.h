@@ -16,6 +16,13 @@
  *   rlhf_whiten_advantages  optional masked whitening of the advantages between steps 3 and 4
  *   rlhf_ppo_stats          monitors of the policy step: approximate KL to the old policy, clip fraction
  *
+ * and of the objectives that are trained beside PPO over the same logits (the paper has no counterpart to these):
+ *
+ *   rlhf_policy_kl_loss_fwd_bwd    clipped policy loss with the KL to the reference inside the loss (no critic)
+ *   rlhf_preference_loss_fwd_bwd   loss over pairs of a chosen and a rejected response
+ *   rlhf_topk_logprobs             a teacher's K largest log-probs per token
+ *   rlhf_distill_loss_fwd_bwd      distillation of a student from those
+ *
  * The paper gives these quantities in prose only; the formulas are the standard definitions and
  * are written out beside each function.
  *
@@ -104,7 +111,7 @@ int rlhf_pad_share(long long n_valid, long long n_padded, int n_blocks, int bloc
                    long long* start, long long* count);
 
 /* Bytes of scratch that rlhf_gather_logprobs, rlhf_experience and rlhf_ppo_loss_fwd_bwd need for a batch of B x T
- * tokens: O(B*T), never O(B*T*V) -- at most 16*B*T + 65536.  0 if B or T is not positive.
+ * tokens: O(B*T), never O(B*T*V) -- at most 16*B*T + 65536.  The same workspace serves the objectives below.  0 if B or T is not positive.
  * The workspace must be 256-byte aligned and must have been cleared once with rlhf_workspace_init
  * before its first use; it can then be reused by any number of calls on the same stream. */
 size_t rlhf_workspace_bytes(int B, int T);
@@ -289,6 +296,68 @@ int rlhf_ppo_loss_fwd_bwd_ex(const void* logits, int logits_dtype, long long str
  */
 int rlhf_ppo_stats(const float* lp_new, const float* lp_old, const float* adv, const int* lengths, int B, int T,
                    float clip_eps, float* out_stats, void* workspace, size_t workspace_bytes, void* stream);
+
+/* What a loss is a mean over. */
+typedef enum {
+    RLHF_MEAN_TOKENS = 0,       /* every valid token weighs 1/N */
+    RLHF_MEAN_SEQUENCES = 1     /* every non-empty sequence weighs the same: a token of it 1/(B' * lengths[b]), B' their number */
+} rlhf_reduction_t;
+
+/*
+ * Clipped policy loss with a KL term, and its gradient (policy training without a critic: the advantages come from the
+ * scores of a group of responses, and the reference acts in the loss instead of the reward).  For each valid token, with
+ * lp = z_y - lse(z), rho = exp(lp - lp_old), d = lp_ref - lp, and w the token's weight under `reduction`:
+ *     l_pg = max(-A*rho, -A*clamp(rho, 1-clip_low, 1+clip_high))
+ *     l_kl = exp(d) - d - 1                                          (non-negative; 0 where lp = lp_ref)
+ *     g    = grad_scale * w * ([-A*rho >= -A*clamp(...)] * (-A*rho) + kl_coef * (1 - exp(d)))
+ *     out_dlogits[b,t,v] = g * ([v == y] - exp(z_v - lse))           rounded to the logits' type
+ *     *out_loss_pg = sum w l_pg      *out_loss_kl = sum w l_kl       (kl_coef is not applied to the latter)
+ * A token whose id is out of range gives 0 to both sums and a zero row; it keeps its weight.  No valid token: all 0.
+ *   logits, ids, lengths, out_dlogits, out_lp_new   as step 4 (logits_dtype: rlhf_dtype_t of both tensors; in place allowed)
+ *   lp_old, lp_ref   fp32 [B,T]; lp_ref may be NULL (no KL term: l_kl = 0)   read
+ *   adv              fp32, adv[b*adv_stride_b + t*adv_stride_t] (strides in elements, >= 0; adv_stride_t = 0 for one
+ *                    advantage per sequence)                           read
+ *   out_loss_pg, out_loss_kl   fp32 scalars (device)                   written
+ *   clip_low in (0,1), clip_high > 0, kl_coef >= 0, all finite.   workspace as for step 1.
+ */
+int rlhf_policy_kl_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                                const long long* ids, long long ids_stride_b, const int* lengths,
+                                const float* lp_old, const float* lp_ref,
+                                const float* adv, long long adv_stride_b, long long adv_stride_t,
+                                int B, int T, int V, float clip_low, float clip_high, float kl_coef,
+                                int reduction, float grad_scale, float* out_loss_pg, float* out_loss_kl,
+                                void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                                float* out_lp_new, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Loss of one pair as a function of h = beta * (s_chosen - s_rejected) - margin. */
+typedef enum {
+    RLHF_PREF_SIGMOID = 0,      /* -(1-e) log sigma(h) - e log sigma(-h), e = label_smoothing */
+    RLHF_PREF_HINGE = 1,        /* max(0, 1 - h); gradient 0 at h >= 1 */
+    RLHF_PREF_SQUARED = 2       /* ((h - 1/2) / beta)^2 */
+} rlhf_preference_t;
+
+/*
+ * Preference loss over pairs of responses, and its gradient.  Sequence i (i < B/2) is the chosen and sequence i + B/2
+ * the rejected response of pair i.  With lp = z_y - lse(z) for every valid token,
+ *     s_b = c_b * sum_t (lp[b,t] - lp_ref[b,t]),   c_b = 1, or 1/lengths[b] if length_mean = 1 (s_b = 0 if lengths[b] = 0)
+ *     *out_loss = (2/B) sum_i loss(h_i)            loss and h as rlhf_preference_t says
+ *     out_rewards[b] = beta * s_b
+ *     out_dlogits[b,t,v] = grad_scale * (2/B) * (+-)loss'(h) * beta * c_b * ([v == y] - exp(z_v - lse))
+ * (+ for the chosen, - for the rejected).  The sums over tokens and pairs are formed in double precision in a fixed order.
+ * A token whose id is out of range adds 0 to s_b (its lp_ref neither) and gets a zero row; it still counts in lengths[b].
+ *   logits, ids, lengths, out_dlogits, out_lp_new   as step 4 (logits_dtype: rlhf_dtype_t of both tensors; in place allowed)
+ *   lp_ref         fp32 [B,T] or NULL (no reference: 0)                read
+ *   out_loss       fp32 scalar (device)                                written
+ *   out_rewards    fp32 [B]                                            written
+ *   B even (else RLHF_ERR_SHAPE); beta > 0; label_smoothing in [0, 1/2), 0 unless RLHF_PREF_SIGMOID; length_mean 0 or 1.
+ *   workspace as for step 1.
+ */
+int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                                 const long long* ids, long long ids_stride_b, const int* lengths, const float* lp_ref,
+                                 int B, int T, int V, int kind, float beta, float margin, float label_smoothing,
+                                 int length_mean, float grad_scale, float* out_loss, float* out_rewards,
+                                 void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                                 float* out_lp_new, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Step 4 for callers that cannot provide a workspace.  (The paper has no counterpart to this

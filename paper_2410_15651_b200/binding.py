@@ -49,9 +49,17 @@ SIGNATURES = {
     "rlhf_ppo_loss_fwd_bwd_noalloc": (_int, [_vp, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
                                              _int, _int, _int, _f32, _f32, _f32, _vp, _vp,
                                              _vp, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "rlhf_policy_kl_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64,
+                                           _int, _int, _int, _f32, _f32, _f32, _int, _f32, _vp, _vp,
+                                           _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "rlhf_preference_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _int, _int, _int,
+                                            _int, _f32, _f32, _f32, _int, _f32, _vp, _vp,
+                                            _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
 }
 
 NOALLOC_MAX_TOKENS = 65536
+MEAN_TOKENS, MEAN_SEQUENCES = 0, 1                    # rlhf_reduction_t
+PREF_SIGMOID, PREF_HINGE, PREF_SQUARED = 0, 1, 2      # rlhf_preference_t
 
 _lib = None
 
@@ -389,4 +397,117 @@ def ppo_loss_fwd_bwd_noalloc(logits: torch.Tensor, ids: torch.Tensor, lengths: t
         loss.data_ptr(), loss.data_ptr() + 4,
         out.dlogits.data_ptr(), dsb, dst, out.dvalues.data_ptr(), lp_new_ptr,
         st_ptr, _stream(logits)), "rlhf_ppo_loss_fwd_bwd_noalloc")
+    return out
+
+
+# ---------------------------------------------------------------- objectives beside the PPO step
+def _together(logits: torch.Tensor, *named) -> None:
+    """Every tensor of a call lives on the device of the logits, and the call is made with that device current."""
+    for name, t in named:
+        if t is not None and t.device != logits.device:
+            raise ValueError(f"{name} is on {t.device}, the logits on {logits.device}")
+
+
+def _ws(ws: torch.Tensor) -> Tuple[int, int]:
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous CUDA tensor (see workspace())")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _dlogits(t: torch.Tensor, logits: torch.Tensor) -> Tuple[int, int]:
+    """Strides of the gradient tensor, which has the shape and type of the logits."""
+    if t.dtype != logits.dtype:
+        raise TypeError("out.dlogits must have the element type of logits")
+    if tuple(t.shape) != tuple(logits.shape):
+        raise ValueError("out.dlogits must have the shape of logits")
+    return _logits(t, "out.dlogits")[3:]
+
+
+def _vector(t: torch.Tensor, n: int, what: str) -> int:
+    _dev(t, torch.float32, what)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor of {n} floats")
+    return t.data_ptr()
+
+
+class PolicyKlOutputs:
+    """Buffers written by policy_kl_loss_fwd_bwd; reusable from call to call."""
+
+    def __init__(self, logits: torch.Tensor, in_place: bool = False, want_lp_new: bool = True):
+        B, T = logits.shape[0], logits.shape[1]
+        self.loss = torch.empty(2, dtype=torch.float32, device=logits.device)      # [loss_pg, loss_kl]
+        self.dlogits = logits if in_place else torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        self.lp_new = torch.empty((B, T), dtype=torch.float32, device=logits.device) if want_lp_new else None
+
+
+def policy_kl_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor, lp_old: torch.Tensor,
+                           lp_ref: Optional[torch.Tensor], adv: torch.Tensor, clip_low: float, clip_high: float,
+                           kl_coef: float, reduction: int, grad_scale: float, ws: torch.Tensor,
+                           out: Optional[PolicyKlOutputs] = None) -> PolicyKlOutputs:
+    """rlhf_policy_kl_loss_fwd_bwd.  `adv` is [B,T] (any strides) or [B], one advantage per sequence; `reduction` is
+    MEAN_TOKENS or MEAN_SEQUENCES."""
+    B, T, V, sb, st = _logits(logits, "logits")
+    isb = _ids(ids, B, T)
+    _lengths(lengths, B)
+    _bt(lp_old, B, T, "lp_old")
+    ref_ptr = _bt(lp_ref, B, T, "lp_ref").data_ptr() if lp_ref is not None else None
+    _dev(adv, torch.float32, "adv")
+    if tuple(adv.shape) == (B, T):
+        asb, ast = adv.stride()
+    elif tuple(adv.shape) == (B,):
+        asb, ast = adv.stride(0), 0
+    else:
+        raise ValueError(f"adv must be [{B},{T}] or [{B}]")
+    if out is None:
+        out = PolicyKlOutputs(logits)
+    dsb, dst = _dlogits(out.dlogits, logits)
+    loss = _vector(out.loss, 2, "out.loss")
+    lp_new_ptr = _bt(out.lp_new, B, T, "out.lp_new").data_ptr() if out.lp_new is not None else None
+    _together(logits, ("ids", ids), ("lengths", lengths), ("lp_old", lp_old), ("lp_ref", lp_ref), ("adv", adv), ("ws", ws),
+              ("out.loss", out.loss), ("out.dlogits", out.dlogits), ("out.lp_new", out.lp_new))
+    wp, wn = _ws(ws)
+    with torch.cuda.device(logits.device):
+        _check(lib().rlhf_policy_kl_loss_fwd_bwd(
+            logits.data_ptr(), DTYPES[logits.dtype], sb, st, ids.data_ptr(), isb, lengths.data_ptr(),
+            lp_old.data_ptr(), ref_ptr, adv.data_ptr(), asb, ast, B, T, V, clip_low, clip_high, kl_coef,
+            reduction, grad_scale, loss, loss + 4, out.dlogits.data_ptr(), dsb, dst, lp_new_ptr,
+            wp, wn, _stream(logits)), "rlhf_policy_kl_loss_fwd_bwd")
+    return out
+
+
+class PreferenceOutputs:
+    """Buffers written by preference_loss_fwd_bwd; reusable from call to call."""
+
+    def __init__(self, logits: torch.Tensor, in_place: bool = False, want_lp_new: bool = True):
+        B, T = logits.shape[0], logits.shape[1]
+        self.loss = torch.empty(1, dtype=torch.float32, device=logits.device)
+        self.rewards = torch.empty(B, dtype=torch.float32, device=logits.device)    # beta * log ratio of every sequence
+        self.dlogits = logits if in_place else torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        self.lp_new = torch.empty((B, T), dtype=torch.float32, device=logits.device) if want_lp_new else None
+
+
+def preference_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor,
+                            lp_ref: Optional[torch.Tensor], kind: int, beta: float, margin: float,
+                            label_smoothing: float, length_mean: bool, grad_scale: float, ws: torch.Tensor,
+                            out: Optional[PreferenceOutputs] = None) -> PreferenceOutputs:
+    """rlhf_preference_loss_fwd_bwd: sequences 0..B/2-1 are the chosen, B/2..B-1 the rejected responses; `kind` is
+    PREF_SIGMOID, PREF_HINGE or PREF_SQUARED."""
+    B, T, V, sb, st = _logits(logits, "logits")
+    isb = _ids(ids, B, T)
+    _lengths(lengths, B)
+    ref_ptr = _bt(lp_ref, B, T, "lp_ref").data_ptr() if lp_ref is not None else None
+    if out is None:
+        out = PreferenceOutputs(logits)
+    dsb, dst = _dlogits(out.dlogits, logits)
+    loss = _vector(out.loss, 1, "out.loss")
+    rewards = _vector(out.rewards, B, "out.rewards")
+    lp_new_ptr = _bt(out.lp_new, B, T, "out.lp_new").data_ptr() if out.lp_new is not None else None
+    _together(logits, ("ids", ids), ("lengths", lengths), ("lp_ref", lp_ref), ("ws", ws), ("out.loss", out.loss),
+              ("out.rewards", out.rewards), ("out.dlogits", out.dlogits), ("out.lp_new", out.lp_new))
+    wp, wn = _ws(ws)
+    with torch.cuda.device(logits.device):
+        _check(lib().rlhf_preference_loss_fwd_bwd(
+            logits.data_ptr(), DTYPES[logits.dtype], sb, st, ids.data_ptr(), isb, lengths.data_ptr(), ref_ptr,
+            B, T, V, kind, beta, margin, label_smoothing, int(length_mean), grad_scale, loss, rewards,
+            out.dlogits.data_ptr(), dsb, dst, lp_new_ptr, wp, wn, _stream(logits)), "rlhf_preference_loss_fwd_bwd")
     return out

@@ -16,6 +16,7 @@
 #include "kernels_cring.cuh"
 #include "kernels_warp.cuh"
 #include "kernels_small.cuh"
+#include "kernels_objective.cuh"
 
 namespace {
 
@@ -38,7 +39,9 @@ int cuda_fail(cudaError_t e, const char* what)
 // Workspace layout (bytes): [0,4) status flags, [4,8) reduction ticket, [8,16) mean and 1/std of the
 // advantage whitening, [16,20) row counter of the loss kernel that deals its rows dynamically, [256, kRowLossOffset) block
 // partial sums of the two losses (2 doubles per block of the kernel that reduces them),
-// [kRowLossOffset, +4*B*T) per-token policy loss terms (kernels without the fused finalisation).
+// [kRowLossOffset, +4*B*T) per-token policy loss terms (kernels without the fused finalisation), then, for the objectives
+// beside step 4, 8*B*T bytes more: per-token KL terms (policy loss with KL); the factor of each sequence and, from
+// 4*B*T on, the loss of each pair (preference loss).
 constexpr size_t kPartialsOffset = 256;
 constexpr size_t kRowLossOffset = 24576;
 constexpr int kMaxFusedBlocks = (int)((kRowLossOffset - kPartialsOffset) / 16);   // block partials that fit the header
@@ -58,6 +61,9 @@ int check_shape(int B, int T, int V)
 
 // Bytes of the workspace that rlhf_ppo_loss_fwd_bwd touches: header + per-token policy loss terms.
 size_t loss_workspace_bytes(int B, int T) { return kRowLossOffset + 4 * (size_t)B * (size_t)T; }
+
+// Bytes that the other objectives touch.
+size_t objective_workspace_bytes(int B, int T) { return kRowLossOffset + 12 * (size_t)B * (size_t)T; }
 
 int check_workspace(const void* ws, size_t bytes, size_t need)
 {
@@ -429,6 +435,21 @@ int keep_max_carveout(K kernel)
     return RLHF_OK;
 }
 
+// What every call that reads logits and writes their gradient checks of the two tensors and the token ids.
+int check_rows(const void* logits, int logits_dtype, long long stride_b, long long stride_t, long long ids_stride_b,
+               int B, int T, int V, const void* out_dlogits, long long dl_stride_b, long long dl_stride_t)
+{
+    if (logits_dtype != RLHF_BF16 && logits_dtype != RLHF_F16) return RLHF_ERR_SCALAR;
+    if (int e = check_shape(B, T, V)) return e;
+    if (stride_b < 0 || stride_t < 0 || ids_stride_b < 0 || dl_stride_b < 0 || dl_stride_t < 0)
+        return RLHF_ERR_STRIDE;
+    if (T > 1 && (stride_t < V || dl_stride_t < V)) return RLHF_ERR_STRIDE;
+    if (B > 1 && dl_stride_b < (long long)(T - 1) * dl_stride_t + V) return RLHF_ERR_STRIDE;
+    if (out_dlogits == logits && (dl_stride_b != stride_b || dl_stride_t != stride_t)) return RLHF_ERR_STRIDE;
+    if (!aligned(logits, 2) || !aligned(out_dlogits, 2)) return RLHF_ERR_ALIGN;
+    return RLHF_OK;
+}
+
 // Host-side checks of the loss call's arguments, the workspace apart (shared by the two loss entry points).
 int check_loss_args(const void* logits, long long stride_b, long long stride_t, const long long* ids,
                     long long ids_stride_b, const int* lengths, const float* lp_old, const float* adv,
@@ -462,6 +483,35 @@ int launch_check(const char* what)
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, what);
     return RLHF_OK;
+}
+
+// Launches the row kernel for an objective with one generated token per row.  Sets a.fused if that kernel also does
+// the finalisation (the losses; value loss and dvalues in step 4); otherwise it leaves per-token terms in a.row_loss
+// (and a.row_kl).
+int launch_objective_rows(RowArgs& a, bool f16, const DeviceInfo& dev, char* ws, cudaStream_t s)
+{
+    const bool all_16B = rows_16B(a.logits, a.stride_b, a.stride_t, a.V) && rows_16B(a.dlogits, a.dl_stride_b, a.dl_stride_t, a.V);
+    // rows off 16-byte boundaries can still take the fast kernel if every dlogits row is as far off a boundary as
+    // its logits row (in place, or a second tensor of the same layout)
+    const bool same_offsets = ((reinterpret_cast<uintptr_t>(a.dlogits) - reinterpret_cast<uintptr_t>(a.logits)) % 16) == 0 &&
+                              ((a.dl_stride_b - a.stride_b) % 8) == 0 && ((a.dl_stride_t - a.stride_t) % 8) == 0;
+    const CregPlan any_plan = plan_creg_any(a.V, dev);
+    const bool ragged_fast = !all_16B && same_offsets && any_plan.cluster == 1;
+    if (((all_16B && fast_loss_rows_apply(a.V, f16, dev)) || ragged_fast) && dev.sm_count * 7 <= kMaxFusedBlocks) {
+        a.fused = 1;
+        a.ticket = (unsigned*)(ws + 4);
+        a.partials = (double*)(ws + kPartialsOffset);
+        if (ragged_fast) {
+            if (int e = f16 ? launch_creg_any<true>(a, any_plan, dev, s) : launch_creg_any<false>(a, any_plan, dev, s)) return e;
+        } else {
+            if (int e = launch_loss_rows(a, f16, dev, s)) return e;
+        }
+        return launch_check("loss row kernel");
+    }
+    const int grid = (int)std::min<long long>((long long)a.B * a.T, (long long)dev.sm_count * 8);
+    if (f16) RLHF_CUDA(launch_kernel(row_generic_kernel<true, true>, grid, kGenericThreads, 0, s, a));
+    else RLHF_CUDA(launch_kernel(row_generic_kernel<true, false>, grid, kGenericThreads, 0, s, a));
+    return launch_check("row_generic_kernel<loss>");
 }
 
 }  // namespace
@@ -513,7 +563,7 @@ int rlhf_pad_share(long long n_valid, long long n_padded, int n_blocks, int bloc
 size_t rlhf_workspace_bytes(int B, int T)
 {
     if (B <= 0 || T <= 0) return 0;
-    size_t n = loss_workspace_bytes(B, T);
+    size_t n = objective_workspace_bytes(B, T);
     return (n + 255) & ~(size_t)255;
 }
 
@@ -820,39 +870,18 @@ int rlhf_ppo_loss_fwd_bwd_ex(const void* logits, int logits_dtype, long long str
     a.row_loss = (float*)(ws + kRowLossOffset);
     a.out_lp_new = out_lp_new;
 
+    a.values_new = values_new;
+    a.values_old = values_old;
+    a.returns = returns;
+    a.value_clip = value_clip;
+    a.out_dvalues = out_dvalues;
+    a.out_loss_pg = out_loss_pg;
+    a.out_loss_vf = out_loss_vf;
+
     cudaStream_t s = (cudaStream_t)stream;
-    long long rows = (long long)B * T;
-    const bool all_16B = rows_16B(logits, stride_b, stride_t, V) && rows_16B(out_dlogits, dl_stride_b, dl_stride_t, V);
-    // rows off 16-byte boundaries can still take the fast kernel if every dlogits row is as far off a boundary as
-    // its logits row (in place, or a second tensor of the same layout)
-    const bool same_offsets = ((reinterpret_cast<uintptr_t>(out_dlogits) - reinterpret_cast<uintptr_t>(logits)) % 16) == 0 &&
-                              ((dl_stride_b - stride_b) % 8) == 0 && ((dl_stride_t - stride_t) % 8) == 0;
-    const CregPlan any_plan = plan_creg_any(V, dev);
-    const bool ragged_fast = !all_16B && same_offsets && any_plan.cluster == 1;
-    if (((all_16B && fast_loss_rows_apply(V, f16, dev)) || ragged_fast) && dev.sm_count * 7 <= kMaxFusedBlocks) {
-        // fast path: the row kernel also does the finalisation (value loss, dvalues, loss reduction)
-        a.fused = 1;
-        a.values_new = values_new;
-        a.values_old = values_old;
-        a.returns = returns;
-        a.value_clip = value_clip;
-        a.out_dvalues = out_dvalues;
-        a.out_loss_pg = out_loss_pg;
-        a.out_loss_vf = out_loss_vf;
-        a.ticket = (unsigned*)(ws + 4);
-        a.partials = (double*)(ws + kPartialsOffset);
-        if (ragged_fast) {
-            if (int e = f16 ? launch_creg_any<true>(a, any_plan, dev, s) : launch_creg_any<false>(a, any_plan, dev, s)) return e;
-        } else {
-            if (int e = launch_loss_rows(a, f16, dev, s)) return e;
-        }
-        return launch_check("loss row kernel");
-    } else {
-        int grid = (int)std::min<long long>(rows, (long long)dev.sm_count * 8);
-        if (f16) RLHF_CUDA(launch_kernel(row_generic_kernel<true, true>, grid, kGenericThreads, 0, s, a));
-        else RLHF_CUDA(launch_kernel(row_generic_kernel<true, false>, grid, kGenericThreads, 0, s, a));
-        if (int e = launch_check("row_generic_kernel<loss>")) return e;
-    }
+    const long long rows = (long long)B * T;
+    if (int e = launch_objective_rows(a, f16, dev, ws, s)) return e;
+    if (a.fused) return RLHF_OK;
 
     FinalArgs f{};
     f.lengths = lengths;
@@ -890,6 +919,161 @@ int rlhf_ppo_loss_fwd_bwd(const void* logits, long long stride_b, long long stri
                                     values_new, values_old, returns, B, T, V, clip_eps, value_clip, grad_scale,
                                     out_loss_pg, out_loss_vf, out_dlogits, dl_stride_b, dl_stride_t, out_dvalues,
                                     out_lp_new, workspace, workspace_bytes, stream);
+}
+
+int rlhf_policy_kl_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                                const long long* ids, long long ids_stride_b, const int* lengths,
+                                const float* lp_old, const float* lp_ref,
+                                const float* adv, long long adv_stride_b, long long adv_stride_t,
+                                int B, int T, int V, float clip_low, float clip_high, float kl_coef,
+                                int reduction, float grad_scale, float* out_loss_pg, float* out_loss_kl,
+                                void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                                float* out_lp_new, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !ids || !lengths || !lp_old || !adv || !out_loss_pg || !out_loss_kl || !out_dlogits) return RLHF_ERR_NULL;
+    if (int e = check_rows(logits, logits_dtype, stride_b, stride_t, ids_stride_b, B, T, V, out_dlogits, dl_stride_b,
+                           dl_stride_t))
+        return e;
+    if (adv_stride_b < 0 || adv_stride_t < 0) return RLHF_ERR_STRIDE;
+    if (!(clip_low > 0.f && clip_low < 1.f) || !std::isfinite(clip_high) || !(clip_high > 0.f) ||
+        !std::isfinite(kl_coef) || kl_coef < 0.f || !std::isfinite(grad_scale) ||
+        (reduction != RLHF_MEAN_TOKENS && reduction != RLHF_MEAN_SEQUENCES))
+        return RLHF_ERR_SCALAR;
+    if (!aligned(ids, 8) || !aligned(lengths, 4) || !aligned(lp_old, 4) || !aligned(lp_ref, 4) || !aligned(adv, 4) ||
+        !aligned(out_loss_pg, 4) || !aligned(out_loss_kl, 4) || !aligned(out_lp_new, 4))
+        return RLHF_ERR_ALIGN;
+    if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
+    DeviceInfo dev;
+    if (int e = device_info(dev)) return e;
+
+    char* ws = (char*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    RowArgs a{};
+    a.objective = kObjPolicyKl;
+    a.logits = (const uint16_t*)logits;
+    a.stride_b = stride_b;
+    a.stride_t = stride_t;
+    a.ids = ids;
+    a.ids_stride_b = ids_stride_b;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.status = (unsigned*)ws;
+    a.wait_limit_ns = kWaitLimitNs;
+    a.lp_old = lp_old;
+    a.lp_ref = lp_ref;
+    a.adv = adv;
+    a.adv_stride_b = adv_stride_b;
+    a.adv_stride_t = adv_stride_t;
+    a.ratio_lo = 1.f - clip_low;
+    a.ratio_hi = 1.f + clip_high;
+    a.kl_coef = kl_coef;
+    a.seq_mean = reduction == RLHF_MEAN_SEQUENCES;
+    a.grad_scale = grad_scale;
+    a.dlogits = (uint16_t*)out_dlogits;
+    a.dl_stride_b = dl_stride_b;
+    a.dl_stride_t = dl_stride_t;
+    a.row_loss = (float*)(ws + kRowLossOffset);
+    a.row_kl = a.row_loss + (size_t)B * T;
+    a.out_lp_new = out_lp_new;
+    a.out_loss_pg = out_loss_pg;
+    a.out_loss_vf = out_loss_kl;
+    if (int e = launch_objective_rows(a, logits_dtype == RLHF_F16, dev, ws, s)) return e;
+    if (a.fused) return RLHF_OK;
+
+    RowSumArgs f{};
+    f.lengths = lengths;
+    f.B = B; f.T = T;
+    f.seq_mean = a.seq_mean;
+    f.row_loss = a.row_loss;
+    f.row_kl = a.row_kl;
+    f.out_lp_new = out_lp_new;
+    f.out_loss = out_loss_pg;
+    f.out_kl = out_loss_kl;
+    f.ticket = (unsigned*)(ws + 4);
+    f.partials = (double*)(ws + kPartialsOffset);
+    const int fgrid = (int)std::min<long long>(((long long)B * T + 1023) / 1024, kFinalMaxBlocks);
+    if (int e = keep_max_carveout(row_sums_kernel)) return e;
+    RLHF_CUDA(launch_kernel(row_sums_kernel, fgrid, kFinalThreads, 0, s, f));
+    return launch_check("row_sums_kernel");
+}
+
+int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                                 const long long* ids, long long ids_stride_b, const int* lengths, const float* lp_ref,
+                                 int B, int T, int V, int kind, float beta, float margin, float label_smoothing,
+                                 int length_mean, float grad_scale, float* out_loss, float* out_rewards,
+                                 void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                                 float* out_lp_new, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !ids || !lengths || !out_loss || !out_rewards || !out_dlogits) return RLHF_ERR_NULL;
+    if (B % 2 != 0) return RLHF_ERR_SHAPE;
+    if (int e = check_rows(logits, logits_dtype, stride_b, stride_t, ids_stride_b, B, T, V, out_dlogits, dl_stride_b,
+                           dl_stride_t))
+        return e;
+    if ((kind != RLHF_PREF_SIGMOID && kind != RLHF_PREF_HINGE && kind != RLHF_PREF_SQUARED) || !std::isfinite(beta) ||
+        !(beta > 0.f) || !std::isfinite(margin) || !(label_smoothing >= 0.f && label_smoothing < 0.5f) ||
+        (kind != RLHF_PREF_SIGMOID && label_smoothing != 0.f) || (length_mean != 0 && length_mean != 1) ||
+        !std::isfinite(grad_scale))
+        return RLHF_ERR_SCALAR;
+    if (!aligned(ids, 8) || !aligned(lengths, 4) || !aligned(lp_ref, 4) || !aligned(out_loss, 4) ||
+        !aligned(out_rewards, 4) || !aligned(out_lp_new, 4))
+        return RLHF_ERR_ALIGN;
+    if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
+    DeviceInfo dev;
+    if (int e = device_info(dev)) return e;
+
+    char* ws = (char*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    const bool f16 = logits_dtype == RLHF_F16;
+    const size_t tokens = (size_t)B * T;
+    RowArgs a{};
+    a.objective = kObjPreference;
+    a.logits = (const uint16_t*)logits;
+    a.stride_b = stride_b;
+    a.stride_t = stride_t;
+    a.ids = ids;
+    a.ids_stride_b = ids_stride_b;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.status = (unsigned*)ws;
+    a.wait_limit_ns = kWaitLimitNs;
+    a.dlogits = (uint16_t*)out_dlogits;
+    a.dl_stride_b = dl_stride_b;
+    a.dl_stride_t = dl_stride_t;
+    a.seq_factor = (const float*)(ws + kRowLossOffset + 4 * tokens);
+
+    // log-probs of every token, the pairs, then the gradient rows with each sequence's factor known
+    WarpArgs wa{};
+    wa.row = a;
+    wa.row.out_lp = out_lp_new ? out_lp_new : (float*)(ws + kRowLossOffset);
+    if (rows_16B(logits, stride_b, stride_t, V)) {
+        if (int e = launch_warp_logprob<false, false>(wa, f16, dev, s)) return e;
+    } else {
+        if (int e = launch_warp_logprob<false, true>(wa, f16, dev, s)) return e;
+    }
+    if (int e = launch_check("logprob_warp_kernel")) return e;
+
+    PairArgs pa{};
+    pa.lp = wa.row.out_lp;
+    pa.lp_ref = lp_ref;
+    pa.ids = ids;
+    pa.ids_stride_b = ids_stride_b;
+    pa.lengths = lengths;
+    pa.B = B; pa.T = T; pa.V = V;
+    pa.kind = kind;
+    pa.beta = beta;
+    pa.margin = margin;
+    pa.smoothing = label_smoothing;
+    pa.length_mean = length_mean;
+    pa.grad_scale = grad_scale;
+    pa.out_loss = out_loss;
+    pa.out_rewards = out_rewards;
+    pa.seq_factor = (float*)(ws + kRowLossOffset + 4 * tokens);
+    pa.pair_loss = (double*)(ws + kRowLossOffset + 8 * tokens);
+    pa.ticket = (unsigned*)(ws + 4);
+    if (int e = keep_max_carveout(preference_pair_kernel)) return e;
+    RLHF_CUDA(launch_kernel(preference_pair_kernel, std::min(B / 2, 1184), kPairThreads, 0, s, pa));
+    if (int e = launch_check("preference_pair_kernel")) return e;
+    return launch_objective_rows(a, f16, dev, ws, s);
 }
 
 }  // extern "C"

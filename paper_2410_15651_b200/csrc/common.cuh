@@ -262,4 +262,24 @@ __device__ inline long long block_count_valid(const int* __restrict__ lengths, i
     return scratch[32];
 }
 
+// Number of sequences with at least one valid token, by the whole block (same scratch and barriers as above).
+__device__ inline long long block_count_nonempty(const int* __restrict__ lengths, int B, long long* scratch)
+{
+    long long n = 0;
+    for (int b = threadIdx.x; b < B; b += blockDim.x) n += __ldg(lengths + b) > 0 ? 1 : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+    int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = (blockDim.x + 31) >> 5;
+    __syncthreads();                 // scratch[32] of the previous count has been read
+    if (lane == 0) scratch[warp] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        long long tot = 0;
+        for (int w = 0; w < nw; ++w) tot += scratch[w];
+        scratch[32] = tot;
+    }
+    __syncthreads();
+    return scratch[32];
+}
+
 }  // namespace rlhf

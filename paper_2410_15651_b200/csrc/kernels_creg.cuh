@@ -53,8 +53,7 @@ struct RowInfo {
     long long dl_offset;    // element offset of the dlogits row
     int y;                  // generated token (0 if it was out of range)
     int bad_id;
-    float lp_old;
-    float adv;
+    RowScalars sc;
     unsigned mis;           // bytes between the 16-byte boundary below the row's first logit and that logit
     unsigned pad;
 };
@@ -265,6 +264,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
     __shared__ int s_last;
     __shared__ __align__(16) float4 s_xchg[2][kCluster];     // per row parity: (M, s, ey, zy) of every block of the cluster
     __shared__ __align__(8) unsigned long long s_xbar[2];
+    static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     static_assert(kCregMaxBufs * 16 <= 64, "the mbarriers of the buffers take the 64 bytes after the zero buffer");
     __shared__ uint32_t s_tmem_base;
 
@@ -310,6 +310,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
     pdl_release_next_grid();
 
     const long long N = block_count_valid(p.lengths, p.B, p.T, s_cnt, blockIdx.x == 0 ? p.status : nullptr);
+    const long long D = p.seq_mean ? block_count_nonempty(p.lengths, p.B, s_cnt) : N;   // what the loss is a mean over
     const int n_mine = N > cid ? (int)((N - cid + G - 1) / G) : 0;   // rows of this cluster: cid, cid + G, ...
 
     bool aborted = false;
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
             struct Ahead {
                 int b, t;
                 long long y;
-                float lp_old, adv;
+                RowScalars sc;
                 bool ok;
             };
             long long k_ahead = cid;
@@ -397,8 +398,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 if (a.ok) {
                     const long long f = (long long)a.b * p.T + a.t;
                     a.y = __ldg(p.ids + (long long)a.b * p.ids_stride_b + a.t);
-                    a.lp_old = __ldg(p.lp_old + f);
-                    a.adv = __ldg(p.adv + f);
+                    a.sc = load_row_scalars(p, a.b, a.t, f);
                 }
                 return a;
             };
@@ -415,8 +415,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 ri.dl_offset = (long long)a.b * p.dl_stride_b + (long long)a.t * p.dl_stride_t;
                 ri.bad_id = (a.y < 0 || a.y >= p.V) ? 1 : 0;
                 ri.y = ri.bad_id ? 0 : (int)a.y;
-                ri.lp_old = a.lp_old;
-                ri.adv = a.adv;
+                ri.sc = a.sc;
                 ri.mis = kAny ? (unsigned)((uintptr_t)row & 15u) : 0u;
                 ri.pad = 0;
                 if (ri.bad_id && crank == 0) atomicOr(p.status, kErrIdRange);
@@ -453,7 +452,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
     }
 
     // ---------------------------------------------------------------- consumers
-    const float scale_over_N = N > 0 ? p.grad_scale / (float)N : 0.f;
+    const float scale_over_N = N > 0 ? p.grad_scale / (float)D : 0.f;
     const int cnt = (uint32_t)tid < nvec ? (int)((nvec - tid + kCons - 1) / kCons) : 0;   // this thread's vectors
     const int nj = (int)((nvec + kCons - 1) / kCons);              // vectors per thread, the -inf tail included
     const int nt = kTmem && nj > kRegVecs ? nj - kRegVecs : 0;     // of which in tensor memory (<= kTmemVecs)
@@ -622,12 +621,13 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
             tot = Acc{Mx, sx, eyx};
             zy_row = zx;
         }
-        const RowResult r = row_finish_fast(tot, zy_row);
+        RowResult r = row_finish_fast(tot, zy_row);
 
-        float loss = 0.f, g = 0.f;
-        if (!ri.bad_id) ppo_token<true>(r.lp, ri.lp_old, ri.adv, p.clip_eps, scale_over_N, loss, g);
+        float loss = 0.f, kl = 0.f, g = 0.f;
+        if (!ri.bad_id) row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
         if (tid == 0 && crank == 0 && !aborted) {
-            p.row_loss[ri.flat] = loss;
+            if (p.row_loss) p.row_loss[ri.flat] = loss;
+            if (p.row_kl) p.row_kl[ri.flat] = kl;
             if (p.out_lp_new) p.out_lp_new[ri.flat] = ri.bad_id ? 0.f : r.lp;
         }
 
@@ -666,8 +666,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
         if (lane == 0) mbar_arrive(computed(buf));
     }
     // The two losses.  Every block leaves its share of the value loss in the workspace; the block that finishes last
-    // adds the per-token policy terms of the whole batch (all its consumer threads, fixed shares, fixed tree) and the
-    // blocks' value-loss shares in block order.
+    // adds the per-token policy terms (and KL terms, where the objective has them) of the whole batch (all its consumer
+    // threads, fixed shares, fixed tree) and the blocks' value-loss shares in block order.
     if (p.fused) {
         if (tid == 0) {
             p.partials[2 * blockIdx.x] = 0.0;
@@ -679,14 +679,18 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
         if (s_last) {
             __threadfence();
             const long long total = (long long)p.B * p.T;
-            double acc = 0.0;
-            for (long long q = tid; q < total; q += kCons) acc += (double)__ldcg(p.row_loss + q);
+            double acc = 0.0, acc_kl = 0.0;
+            if (p.row_loss)
+                for (long long q = tid; q < total; q += kCons) acc += (double)__ldcg(p.row_loss + q);
+            if (p.row_kl)
+                for (long long q = tid; q < total; q += kCons) acc_kl += (double)__ldcg(p.row_kl + q);
             const double pg = consumer_sum_double<NW>(acc, s_dbl, warp, lane);
+            const double kl = consumer_sum_double<NW>(acc_kl, s_dbl + 16, warp, lane);
             if (tid == 0) {
-                double c = 0.0;
+                double c = kl;
                 for (unsigned k = 0; k < gridDim.x; ++k) c += ((volatile double*)p.partials)[2 * k + 1];
-                *p.out_loss_pg = N > 0 ? (float)(pg / (double)N) : 0.f;
-                *p.out_loss_vf = N > 0 ? (float)(c / (double)N) : 0.f;
+                if (p.out_loss_pg) *p.out_loss_pg = N > 0 ? (float)(pg / (double)D) : 0.f;
+                if (p.out_loss_vf) *p.out_loss_vf = N > 0 ? (float)(c / (double)D) : 0.f;
                 *p.ticket = 0u;
                 if (kCluster == 1) *ca.row_counter = 0u;
             }

@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
     auto full = [&](int s) { return bar_addr + 8u * s; };
     auto done = [&](int s) { return bar_addr + 8u * (kCringMaxSlots + s); };
     const uint32_t xbar_addr = smem_u32(s_xbar);
+    static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     static_assert(2 * kCringMaxSlots * 8 <= 256, "the slots' mbarriers take the 256 bytes after the zero buffer");
 
     if (tid == 0) {
@@ -127,6 +128,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
     pdl_release_next_grid();
 
     const long long N = block_count_valid(p.lengths, p.B, p.T, s_cnt, blockIdx.x == 0 ? p.status : nullptr);
+    const long long D = p.seq_mean ? block_count_nonempty(p.lengths, p.B, s_cnt) : N;   // what the loss is a mean over
     const int n_mine = N > cid ? (int)((N - cid + G - 1) / G) : 0;   // rows of this cluster: cid, cid + G, ...
     const uint32_t last_bytes = slice_bytes - (uint32_t)(C - 1) * kChunk;   // of a slice's last chunk (C = ceil(slice/chunk))
 
@@ -188,7 +190,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
             struct Ahead {
                 int b, t;
                 long long y;
-                float lp_old, adv;
+                RowScalars sc;
                 bool ok;
             };
             long long k_ahead = cid;
@@ -213,8 +215,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 if (a.ok) {
                     const long long f = (long long)a.b * p.T + a.t;
                     a.y = __ldg(p.ids + (long long)a.b * p.ids_stride_b + a.t);
-                    a.lp_old = __ldg(p.lp_old + f);
-                    a.adv = __ldg(p.adv + f);
+                    a.sc = load_row_scalars(p, a.b, a.t, f);
                 }
                 return a;
             };
@@ -235,8 +236,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 ri.dl_offset = (long long)b * p.dl_stride_b + (long long)t * p.dl_stride_t;
                 ri.bad_id = (a.y < 0 || a.y >= p.V) ? 1 : 0;
                 ri.y = ri.bad_id ? 0 : (int)a.y;
-                ri.lp_old = a.lp_old;
-                ri.adv = a.adv;
+                ri.sc = a.sc;
                 ri.mis = 0;
                 ri.pad = 0;
                 if (ri.bad_id && crank == 0) atomicOr(p.status, kErrIdRange);
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
     }
 
     // ---------------------------------------------------------------- consumers
-    const float scale_over_N = N > 0 ? p.grad_scale / (float)N : 0.f;
+    const float scale_over_N = N > 0 ? p.grad_scale / (float)D : 0.f;
     const int nj = 2 * C;                                          // vectors per thread, the ones past the slice's end included
     const int nt = nj - kRegVecs;                                  // of which in tensor memory
     const uint32_t tmem_addr = s_tmem_base + (((uint32_t)(warp & 3) * 32u) << 16) + (uint32_t)(warp >> 2) * (uint32_t)(nt * 8);
@@ -448,12 +448,13 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
             tot = Acc{Mx, sx, eyx};
             zy_row = zx;
         }
-        const RowResult r = row_finish_fast(tot, zy_row);
+        RowResult r = row_finish_fast(tot, zy_row);
 
-        float loss = 0.f, g = 0.f;
-        if (!ri.bad_id) ppo_token<true>(r.lp, ri.lp_old, ri.adv, p.clip_eps, scale_over_N, loss, g);
+        float loss = 0.f, kl = 0.f, g = 0.f;
+        if (!ri.bad_id) row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
         if (tid == 0 && crank == 0 && !aborted) {
-            p.row_loss[ri.flat] = loss;
+            if (p.row_loss) p.row_loss[ri.flat] = loss;
+            if (p.row_kl) p.row_kl[ri.flat] = kl;
             if (p.out_lp_new) p.out_lp_new[ri.flat] = ri.bad_id ? 0.f : r.lp;
         }
 
@@ -514,8 +515,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
         if (s0 >= R) { s0 -= R; ph0 ^= 1u; }
     }
     // The two losses.  Every block leaves its share of the value loss in the workspace; the block that finishes last
-    // adds the per-token policy terms of the whole batch (all its consumer threads, fixed shares, fixed tree) and the
-    // blocks' value-loss shares in block order.
+    // adds the per-token policy terms (and KL terms, where the objective has them) of the whole batch (all its consumer
+    // threads, fixed shares, fixed tree) and the blocks' value-loss shares in block order.
     if (p.fused) {
         if (tid == 0) {
             p.partials[2 * blockIdx.x] = 0.0;
@@ -527,14 +528,18 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
         if (s_last) {
             __threadfence();
             const long long total = (long long)p.B * p.T;
-            double acc = 0.0;
-            for (long long q = tid; q < total; q += kCons) acc += (double)__ldcg(p.row_loss + q);
+            double acc = 0.0, acc_kl = 0.0;
+            if (p.row_loss)
+                for (long long q = tid; q < total; q += kCons) acc += (double)__ldcg(p.row_loss + q);
+            if (p.row_kl)
+                for (long long q = tid; q < total; q += kCons) acc_kl += (double)__ldcg(p.row_kl + q);
             const double pg = consumer_sum_double<NW>(acc, s_dbl, warp, lane);
+            const double kl = consumer_sum_double<NW>(acc_kl, s_dbl + 16, warp, lane);
             if (tid == 0) {
-                double c = 0.0;
+                double c = kl;
                 for (unsigned k = 0; k < gridDim.x; ++k) c += ((volatile double*)p.partials)[2 * k + 1];
-                *p.out_loss_pg = N > 0 ? (float)(pg / (double)N) : 0.f;
-                *p.out_loss_vf = N > 0 ? (float)(c / (double)N) : 0.f;
+                if (p.out_loss_pg) *p.out_loss_pg = N > 0 ? (float)(pg / (double)D) : 0.f;
+                if (p.out_loss_vf) *p.out_loss_vf = N > 0 ? (float)(c / (double)D) : 0.f;
                 *p.ticket = 0u;
                 if (kCluster == 1) *ca.row_counter = 0u;
             }

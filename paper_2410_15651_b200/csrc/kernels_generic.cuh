@@ -38,7 +38,97 @@ struct RowArgs {
     float* out_loss_vf;
     unsigned* ticket;           // workspace word 1, zero between calls
     double* partials;           // workspace: [gridDim.x][2] block partial sums (policy, value)
+    // which objective the row belongs to (kObjPpo: step 4), and what the others take beside lp_old and adv
+    int objective;
+    const float* lp_ref;        // kObjPolicyKl: reference log-probs, or null (no KL term)
+    long long adv_stride_b, adv_stride_t;   // kObjPolicyKl: adv[b*adv_stride_b + t*adv_stride_t]
+    float ratio_lo, ratio_hi;   // kObjPolicyKl: bounds of the clipped ratio
+    float kl_coef;
+    int seq_mean;               // kObjPolicyKl: a token weighs 1 / (non-empty sequences * its sequence's length)
+    float* row_kl;              // kObjPolicyKl: workspace, per-token KL term
+    const float* seq_factor;    // kObjPreference: d(grad_scale * loss) / d(log-prob of any token of sequence b)
 };
+
+// ---------------------------------------------------------------- objectives of a row with one generated token
+constexpr int kObjPpo = 0, kObjPolicyKl = 1, kObjPreference = 2;
+
+// What a row's objective needs beside its log-prob; loaded ahead of the row.
+struct RowScalars {
+    float lp_old, adv;          // kObjPreference: adv is the sequence's factor
+    float lp_ref, w;            // kObjPolicyKl
+};
+
+__device__ __forceinline__ RowScalars load_row_scalars(const RowArgs& p, int b, int t, long long flat)
+{
+    RowScalars s{0.f, 0.f, 0.f, 1.f};
+    if (p.objective == kObjPpo) {
+        s.lp_old = __ldg(p.lp_old + flat);
+        s.adv = __ldg(p.adv + flat);
+    } else if (p.objective == kObjPolicyKl) {
+        s.lp_old = __ldg(p.lp_old + flat);
+        s.adv = __ldg(p.adv + (long long)b * p.adv_stride_b + (long long)t * p.adv_stride_t);
+        if (p.lp_ref) s.lp_ref = __ldg(p.lp_ref + flat);
+        if (p.seq_mean) s.w = 1.f / (float)clamp_len(__ldg(p.lengths + b), p.T);
+    } else {
+        s.adv = __ldg(p.seq_factor + b);
+    }
+    return s;
+}
+
+// exp(d) - 1 - d without cancellation: the Taylor series where it is short (|d| <= 1/2: the first term left out is
+// below 2^-25 of the sum), else the difference.
+__device__ __forceinline__ float exp_excess(float d)
+{
+    if (fabsf(d) > 0.5f) return expm1f(d) - d;
+    float s = 1.f / 3628800.f;
+    s = fmaf(s, d, 1.f / 362880.f);
+    s = fmaf(s, d, 1.f / 40320.f);
+    s = fmaf(s, d, 1.f / 5040.f);
+    s = fmaf(s, d, 1.f / 720.f);
+    s = fmaf(s, d, 1.f / 120.f);
+    s = fmaf(s, d, 1.f / 24.f);
+    s = fmaf(s, d, 1.f / 6.f);
+    s = fmaf(s, d, 0.5f);
+    return s * d * d;
+}
+
+// The row's log-prob from its partition sum, for the objectives beside step 4: the difference x_y - M is rounded once
+// and log2 of the sum is small, so the result is good to a few units in its own last place (row_finish forms lse first,
+// whose last place is that of the largest logit).
+__device__ __forceinline__ float lp_relative(const Acc& a, float zy)
+{
+    return kLn2 * (fmaf(zy, kLog2e, -a.M) - log2f(a.s + a.ey));
+}
+
+// Loss terms of one token and g = d(grad_scale * total loss) / d(log-prob).  `scale` is grad_scale over the number of
+// tokens (or of non-empty sequences).  lp is replaced by the value the objective is formed with.
+template <bool kFast>
+__device__ __forceinline__ void row_objective(const RowArgs& p, const RowScalars& s, const Acc& tot, float zy, float& lp,
+                                              float scale, float& loss, float& kl, float& g)
+{
+    kl = 0.f;
+    if (p.objective == kObjPpo) {
+        ppo_token<kFast>(lp, s.lp_old, s.adv, p.clip_eps, scale, loss, g);
+    } else if (p.objective == kObjPolicyKl) {
+        lp = lp_relative(tot, zy);
+        const float rho = expf(lp - s.lp_old);
+        const float unclipped = -s.adv * rho;
+        const float clipped = -s.adv * fminf(fmaxf(rho, p.ratio_lo), p.ratio_hi);
+        float d_pg = 0.f, d_kl = 0.f;
+        if (unclipped >= clipped) { loss = unclipped; d_pg = unclipped; } else loss = clipped;
+        if (!(unclipped == unclipped)) loss = d_pg = unclipped;           // NaN stays NaN
+        if (p.lp_ref) {
+            const float d = s.lp_ref - lp;
+            kl = s.w * exp_excess(d);
+            d_kl = -p.kl_coef * expm1f(d);
+        }
+        loss *= s.w;
+        g = scale * s.w * (d_pg + d_kl);
+    } else {
+        loss = 0.f;
+        g = s.adv;
+    }
+}
 
 constexpr int kGenericThreads = 256;
 
@@ -64,7 +154,8 @@ __global__ void __launch_bounds__(kGenericThreads) row_generic_kernel(RowArgs p)
     pdl_wait_prior_grid();
     pdl_release_next_grid();
     const long long N = block_count_valid(p.lengths, p.B, p.T, s_cnt, blockIdx.x == 0 ? p.status : nullptr);
-    const float scale_over_N = N > 0 ? p.grad_scale / (float)N : 0.f;
+    const long long D = kLoss && p.seq_mean ? block_count_nonempty(p.lengths, p.B, s_cnt) : N;
+    const float scale_over_N = N > 0 ? p.grad_scale / (float)D : 0.f;
 
     Cursor cur{0, 0};
     for (long long k = blockIdx.x; k < N; k += gridDim.x) {
@@ -88,10 +179,11 @@ __global__ void __launch_bounds__(kGenericThreads) row_generic_kernel(RowArgs p)
             if (threadIdx.x == 0) p.out_lp[flat] = bad_id ? 0.f : r.lp;
             continue;
         }
-        float loss = 0.f, g = 0.f;
-        if (!bad_id) ppo_token(r.lp, p.lp_old[flat], p.adv[flat], p.clip_eps, scale_over_N, loss, g);
+        float loss = 0.f, kl = 0.f, g = 0.f;
+        if (!bad_id) row_objective<false>(p, load_row_scalars(p, b, t, flat), a, zy, r.lp, scale_over_N, loss, kl, g);
         if (threadIdx.x == 0) {
-            p.row_loss[flat] = loss;
+            if (p.row_loss) p.row_loss[flat] = loss;
+            if (p.row_kl) p.row_kl[flat] = kl;
             if (p.out_lp_new) p.out_lp_new[flat] = bad_id ? 0.f : r.lp;
         }
         uint16_t* drow = p.dlogits + (long long)b * p.dl_stride_b + (long long)t * p.dl_stride_t;

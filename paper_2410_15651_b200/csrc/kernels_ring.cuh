@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
     pdl_release_next_grid();
 
     const long long N = block_count_valid(p.lengths, p.B, p.T, s_cnt, blockIdx.x == 0 ? p.status : nullptr);
+    const long long D = p.seq_mean ? block_count_nonempty(p.lengths, p.B, s_cnt) : N;   // what the loss is a mean over
     const long long G = gridDim.x;
 
     bool aborted = false;
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
     }
 
     // ---------------------------------------------------------------- consumers
-    const float scale_over_N = N > 0 ? p.grad_scale / (float)N : 0.f;
+    const float scale_over_N = N > 0 ? p.grad_scale / (float)D : 0.f;
     const uint32_t nvec = ra.row_bytes / 16u;
     const int full_chunks = (int)(nvec / kChunkVecs);          // chunks in which every vector exists
     double sum_pg = 0.0, sum_vf = 0.0;                         // block partial sums (thread 0)
@@ -446,13 +447,12 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
     // scalars of the row about to be processed (loaded one row ahead)
     int nb = 0, nt = 0;
     long long ny = 0;
-    float n_lp_old = 0.f, n_adv = 0.f;
+    RowScalars n_sc{};
     auto fetch_row = [&](long long k) {
         if (k < N && cursor_seek_valid(cur, k, p.lengths, p.B, p.T, nb, nt)) {
             ny = __ldg(p.ids + (long long)nb * p.ids_stride_b + nt);
             const long long f = (long long)nb * p.T + nt;
-            n_lp_old = __ldg(p.lp_old + f);
-            n_adv = __ldg(p.adv + f);
+            n_sc = load_row_scalars(p, nb, nt, f);
         }
     };
     fetch_row(blockIdx.x);
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
     for (long long k = blockIdx.x; k < N; k += G, par ^= 1) {
         const int b = nb, t = nt;
         long long y = ny;
-        const float lp_old = n_lp_old, adv = n_adv;
+        const RowScalars sc = n_sc;
         const long long flat = (long long)b * p.T + t;
         const bool bad_id = (y < 0 || y >= p.V);
         if (bad_id) { y = 0; if (tid == 0) atomicOr(p.status, kErrIdRange); }
@@ -529,15 +529,15 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
         } else {
             tot = consumer_reduce<NW>(a, s_part[par], &s_lab[par], warp, lane);
         }
-        const RowResult r = row_finish(tot, s_lab[par].zy);
+        RowResult r = row_finish(tot, s_lab[par].zy);
 
         // scalars of the next row, in flight while this row is finished
         fetch_row(k + G);
 
-        float loss = 0.f, g = 0.f;
-        if (!bad_id) ppo_token(r.lp, lp_old, adv, p.clip_eps, scale_over_N, loss, g);
+        float loss = 0.f, kl = 0.f, g = 0.f;
+        if (!bad_id) row_objective<false>(p, sc, tot, s_lab[par].zy, r.lp, scale_over_N, loss, kl, g);
         if (tid == 0) {
-            if (p.fused) sum_pg += (double)loss; else p.row_loss[flat] = loss;
+            if (p.fused) { sum_pg += (double)loss; sum_vf += (double)kl; } else p.row_loss[flat] = loss;
             if (p.out_lp_new) p.out_lp_new[flat] = bad_id ? 0.f : r.lp;
         }
 
@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
             if (++slot == S) { slot = 0; phase ^= 1u; }
         }
     }
-    if (p.fused && tid == 0) publish_block_losses(p, N, sum_pg, sum_vf);
+    if (p.fused && tid == 0) publish_block_losses(p, D, sum_pg, sum_vf);
 }
 
 // ---------------------------------------------------------------- host-side plan

@@ -401,6 +401,7 @@ __global__ void __launch_bounds__(kFinalThreads) ppo_finalize_kernel(FinalArgs p
 // The value-loss part: one thread's share of the block's slice; writes dvalues (and zeroes lp_new at
 // padding) and returns the thread's partial sum of loss terms.
 // zero_pad_terms: also writes 0 to the per-token policy loss terms (row_loss) of the padded tokens.
+// The objectives without a value loss only have their per-token terms zeroed at padding.
 __device__ inline double value_loss_slice(const RowArgs& p, long long N, int tid, int nthreads, bool zero_pad_terms = false)
 {
     const float scale_over_N = N > 0 ? p.grad_scale / (float)N : 0.f;
@@ -408,6 +409,17 @@ __device__ inline double value_loss_slice(const RowArgs& p, long long N, int tid
     const long long per_block = (total + gridDim.x - 1) / gridDim.x;
     const long long begin = per_block * blockIdx.x, end = min(total, begin + per_block);
     double sum_vf = 0.0;
+    if (p.objective != kObjPpo) {
+        if (!p.row_loss && !p.out_lp_new) return 0.0;
+        for (long long i = begin + tid; i < end; i += nthreads) {
+            const int b = (int)(i / p.T), t = (int)(i % p.T);
+            if (t < clamp_len(__ldg(p.lengths + b), p.T)) continue;
+            if (p.out_lp_new) p.out_lp_new[i] = 0.f;
+            if (zero_pad_terms && p.row_loss) p.row_loss[i] = 0.f;
+            if (zero_pad_terms && p.row_kl) p.row_kl[i] = 0.f;
+        }
+        return 0.0;
+    }
     for (long long i = begin + tid; i < end; i += nthreads) {
         int b = (int)(i / p.T), t = (int)(i % p.T);
         float dv = 0.f;
@@ -444,6 +456,7 @@ __device__ inline double consumer_sum_double(double v, double* s_dbl, int warp, 
 // Called by consumer thread 0 of every block when the block has finished its rows: publishes the
 // block's two partial sums; the last block to arrive adds all of them in index order and writes the
 // two losses.
+// N: what the losses are means over.
 __device__ inline void publish_block_losses(const RowArgs& p, long long N, double sum_pg, double sum_vf)
 {
     p.partials[2 * blockIdx.x] = sum_pg;
@@ -457,8 +470,8 @@ __device__ inline void publish_block_losses(const RowArgs& p, long long N, doubl
             a += ((volatile double*)p.partials)[2 * k];
             c += ((volatile double*)p.partials)[2 * k + 1];
         }
-        *p.out_loss_pg = N > 0 ? (float)(a / (double)N) : 0.f;
-        *p.out_loss_vf = N > 0 ? (float)(c / (double)N) : 0.f;
+        if (p.out_loss_pg) *p.out_loss_pg = N > 0 ? (float)(a / (double)N) : 0.f;
+        if (p.out_loss_vf) *p.out_loss_vf = N > 0 ? (float)(c / (double)N) : 0.f;
         *p.ticket = 0u;
     }
 }

@@ -1,0 +1,251 @@
+"""The objectives beside the PPO step on the GPU against their float64 definitions (objectives64.py).
+
+Tolerances.  A log-prob lp is formed in fp32 as ln2 * (fma(z_y, log2e, -M) - log2(sum)): with |x_y - M| <= 64 the first
+term is rounded by at most 2^-24 * 64, the terms of the sum carry 2^-24 * 64 * ln2 from their exponent and 2^-22 from the
+exponential, log2 adds 2^-23 of a value below 32: together below 1.3e-5, and 2e-5 is allowed (LP).  A gradient entry is a
+product of such quantities, rounded once to its type: half a step of the value (finfo.eps / 2), plus 2e-5 of the absolute
+parts it is summed from (a KL part may cancel a policy part), plus half of the type's smallest step (fp16) or the fp32
+flush bound (bf16).  Sums and means of fp32 terms are formed in double: a loss is off by at most the terms' own errors,
+their mean absolute size times 2e-5, and one final rounding to fp32."""
+import pytest
+import torch
+
+import objectives64 as ref
+from paper_2410_15651_b200 import binding as lib
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+LP = 2e-5
+BF, HF = torch.bfloat16, torch.float16
+
+
+def tiny(dtype):
+    return 2.0 ** -25 if dtype == HF else 2.0 ** -120
+
+
+def check_gradient(got, want, parts):
+    """|got - want| within half a step of want, 2e-5 of `parts`, and the smallest step."""
+    tol = torch.finfo(got.dtype).eps / 2 * want.abs() + LP * parts + tiny(got.dtype)
+    bad = (got.double() - want).abs() - tol
+    assert not torch.isnan(got).any()
+    assert (bad <= 0).all(), (bad.max().item(), want.abs().max().item())
+
+
+def mixed_lengths(B, T):
+    pattern = [T, 0, 1, max(1, T - 1), T // 2, T]
+    return torch.tensor([pattern[b % len(pattern)] for b in range(B)], dtype=torch.int32, device=DEV)
+
+
+def labels(B, T, V, gen):
+    return torch.randint(0, V, (B, T), generator=gen, device=DEV)
+
+
+# sizes around the kernels' borders: single entries, vectors off and on 16-byte boundaries, the chunk ring, clusters of two
+# to four blocks, rows streamed twice
+SIZES = [(2, 1, 1), (4, 3, 7), (4, 5, 1000), (4, 5, 1001), (2, 3, 8192), (6, 4, 8200), (6, 4, 32000), (4, 3, 50257),
+         (4, 3, 50272), (2, 3, 57344), (4, 3, 128256), (2, 2, 163840), (2, 2, 230000), (2, 2, 300000), (2, 2, 100003)]
+
+
+def policy_inputs(z, ids, lengths, gen, per_sequence):
+    B, T, _ = z.shape
+    _, lp, _ = ref.label_logprobs(z.double(), ids, lengths)
+    # ratios away from the clip's edges, where either branch would be a right answer
+    rho = torch.tensor([0.5, 0.9, 1.0, 1.1, 1.6], device=DEV)[torch.randint(0, 5, (B, T), generator=gen, device=DEV)]
+    lp_old = (lp - rho.double().log()).float()
+    lp_ref = (lp + 0.5 * torch.randn((B, T), generator=gen, device=DEV)).float()
+    adv = torch.randn((B,) if per_sequence else (B, T), generator=gen, device=DEV)
+    return lp_old, lp_ref, adv
+
+
+def check_policy(z, ids, lengths, lp_old, lp_ref, adv, kl_coef, reduction, scale, out=None, z64=None):
+    B, T, V = z.shape
+    z64 = z.double() if z64 is None else z64
+    ws = lib.workspace(B, T, DEV)
+    got = lib.policy_kl_loss_fwd_bwd(z, ids, lengths, lp_old, lp_ref, adv, 0.2, 0.3, kl_coef, reduction, scale, ws, out)
+    pg, kl, d, lp, size = ref.policy_kl(z64, ids, lengths, lp_old, lp_ref, adv, 0.2, 0.3, kl_coef, reduction, scale)
+    if got.lp_new is not None:
+        assert (got.lp_new.double() - lp).abs().max() <= LP
+    part = torch.softmax(z64, dim=2) + torch.nn.functional.one_hot(ids.clamp(0, V - 1), V)
+    check_gradient(got.dlogits, d, size[..., None] * part)
+    n = lengths.clamp(0, T).double()
+    # every term |A| rho <= 4.3 * 1.6 and its error LP of that; KL terms: d exp(d) per unit of lp
+    assert abs(got.loss[0].item() - pg.item()) <= 8 * LP + 2 ** -23 * abs(pg.item())
+    assert abs(got.loss[1].item() - kl.item()) <= 8 * LP + 2 ** -23 * abs(kl.item())
+    if n.sum() == 0:
+        assert (got.loss == 0).all()
+    return got, ws
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("B,T,V", SIZES)
+def test_policy_kl_sizes(B, T, V, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(V + T)
+    z, _ = ref.row_logits(B, T, V, dtype, gen, DEV)
+    ids, lengths = labels(B, T, V, gen), mixed_lengths(B, T)
+    lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, per_sequence=V % 2 == 0)
+    got, ws = check_policy(z, ids, lengths, lp_old, lp_ref, adv, 0.1, V % 3 % 2, 100.0)
+    assert lib.poll_status(ws) == 0
+    pads = ~ref.valid_mask(lengths, T)
+    assert (got.dlogits[pads] == 0).all() and (got.lp_new[pads] == 0).all()
+
+
+@pytest.mark.parametrize("reduction", [lib.MEAN_TOKENS, lib.MEAN_SEQUENCES])
+@pytest.mark.parametrize("layout", ["prompt", "pitch", "offset", "in_place", "other_offset", "strided_adv"])
+def test_policy_kl_layouts(layout, reduction):
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    B, T, V = 5, 6, 8200
+    kw = {"prompt": dict(prompt=3), "pitch": dict(pitch=5), "offset": dict(offset=3), "in_place": dict(prompt=2, offset=1, pitch=3)}
+    z, store = ref.row_logits(B, T, V, BF, gen, DEV, **kw.get(layout, {}))
+    ids_full = labels(B, T + 4, V, gen)
+    ids, lengths = ids_full[:, 2:2 + T], mixed_lengths(B, T)
+    lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
+    out, z64 = None, z.double()
+    if layout == "in_place":
+        before = store.clone()
+        out = lib.PolicyKlOutputs(z, in_place=True)
+    elif layout == "other_offset":                       # gradient rows off the logits' alignment: element-wise kernel
+        out = lib.PolicyKlOutputs(z)
+        out.dlogits = torch.full((B * T * V + 3,), 7.0, dtype=BF, device=DEV)[3:].view(B, T, V)
+    elif layout == "strided_adv":
+        adv = torch.randn((T, B), generator=gen, device=DEV).t()
+    check_policy(z, ids, lengths, lp_old, lp_ref, adv, 0.05, reduction, 30.0, out, z64)
+    if layout == "in_place":                             # nothing but the rows was written
+        keep = torch.ones_like(store, dtype=torch.bool)
+        keep.as_strided(z.shape, z.stride(), z.storage_offset())[...] = False
+        assert torch.equal(store.view(torch.int16)[keep], before.view(torch.int16)[keep])
+
+
+def test_policy_kl_without_reference_and_without_tokens():
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    B, T, V = 3, 4, 32000
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    ids, lengths = labels(B, T, V, gen), mixed_lengths(B, T)
+    lp_old, _, adv = policy_inputs(z, ids, lengths, gen, True)
+    got, _ = check_policy(z, ids, lengths, lp_old, None, adv, 0.3, 0, 1.0)
+    assert got.loss[1].item() == 0
+    for reduction in (0, 1):
+        got, ws = check_policy(z, ids, torch.zeros_like(lengths), lp_old, None, adv, 0.3, reduction, 1.0)
+        assert (got.dlogits == 0).all() and lib.poll_status(ws) == 0
+
+
+@pytest.mark.parametrize("V", [1000, 8200, 50257, 128256])
+def test_policy_kl_bad_ids_lengths_and_deleted_entries(V):
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    B, T = 4, 4
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    z[..., 5:V - 3:7] = float("-inf")
+    ids, lengths = torch.full((B, T), 3, device=DEV), torch.tensor([T + 9, -2, 2, T], dtype=torch.int32, device=DEV)
+    ids[0, 1], ids[3, 2] = V, -1
+    lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
+    got, ws = check_policy(z, ids, lengths, lp_old, lp_ref, adv, 0.1, 1, 10.0)
+    assert lib.poll_status(ws) == 16 | 32
+    assert (got.dlogits[0, 1] == 0).all() and (got.dlogits[3, 2] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("V", [32000, 128256])
+def test_policy_kl_far_logits(V, dtype):
+    """Peaked rows and logits far above the first ones of their row."""
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    B, T = 2, 4
+    z, _ = ref.row_logits(B, T, V, dtype, gen, DEV, sigma=1.0)
+    z[0, 0, V - 1] = 300.0
+    z[0, 1, :8] = -2000.0
+    z[1, 0] = 0.0
+    ids, lengths = labels(B, T, V, gen), torch.full((B,), T, dtype=torch.int32, device=DEV)
+    ids[0, 0] = V - 1
+    z[0, 2, ids[0, 2]] = 30.0
+    z64 = z.double()
+    lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
+    got, _ = check_policy(z, ids, lengths, lp_old, lp_ref, adv, 0.1, 0, 8.0)
+    assert torch.isfinite(got.loss).all()
+
+
+def check_preference(z, ids, lengths, lp_ref, kind, beta, margin, smoothing, length_mean, scale, out=None, z64=None):
+    B, T, V = z.shape
+    z64 = z.double() if z64 is None else z64
+    ws = lib.workspace(B, T, DEV)
+    got = lib.preference_loss_fwd_bwd(z, ids, lengths, lp_ref, kind, beta, margin, smoothing, length_mean, scale, ws, out)
+    loss, rewards, d, lp, f = ref.preference(z64, ids, lengths, lp_ref, kind, beta, margin, smoothing, length_mean, scale)
+    # a sequence's sum is off by at most LP per token (LP in all where it is a mean over the tokens)
+    per_seq = beta * LP * (torch.ones(B, device=DEV) if length_mean else lengths.clamp(0, T).double())
+    if got.lp_new is not None:
+        assert (got.lp_new.double() - lp).abs().max() <= LP
+    assert ((got.rewards.double() - rewards).abs() <= per_seq + 2 ** -23 * rewards.abs()).all()
+    dh = 2 * per_seq.max().item()                        # error of h
+    slope = 1.0 if kind < 2 else 2 * ((rewards[:B // 2] - rewards[B // 2:] - margin - 0.5).abs().max().item() + dh) / beta ** 2
+    assert abs(got.loss.item() - loss.item()) <= slope * dh + 2 ** -23 * abs(loss.item())
+    # the factor changes by at most max|loss''| per unit of h: 1/4, 0 (away from the kink), 2 / beta^2
+    curve = {0: 0.25, 1: 0.0, 2: 2 / beta ** 2}[kind]
+    c = 1 / lengths.clamp(1, T).double() if length_mean else torch.ones(B, device=DEV).double()
+    df = curve * dh * beta * c * scale * 2 / B
+    part = torch.softmax(z64, dim=2) + torch.nn.functional.one_hot(ids.clamp(0, V - 1), V)
+    check_gradient(got.dlogits, d, (f.abs() + df / LP)[:, None, None] * part)
+    return got, ws
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("B,T,V", SIZES)
+def test_preference_sizes(B, T, V, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(V + T)
+    z, _ = ref.row_logits(B, T, V, dtype, gen, DEV)
+    ids, lengths = labels(B, T, V, gen), mixed_lengths(B, T)
+    _, lp, _ = ref.label_logprobs(z.double(), ids, lengths)
+    lp_ref = (lp + 0.5 * torch.randn((B, T), generator=gen, device=DEV)).float()
+    got, ws = check_preference(z, ids, lengths, lp_ref, V % 3, 0.3, 0.1, 0.1 if V % 3 == 0 else 0.0, T % 2 == 0, 100.0)
+    assert lib.poll_status(ws) == 0
+    pads = ~ref.valid_mask(lengths, T)
+    assert (got.dlogits[pads] == 0).all() and (got.lp_new[pads] == 0).all()
+
+
+@pytest.mark.parametrize("kind", [lib.PREF_SIGMOID, lib.PREF_HINGE, lib.PREF_SQUARED])
+@pytest.mark.parametrize("layout", ["prompt", "in_place", "other_offset", "no_reference", "no_lp"])
+def test_preference_layouts(layout, kind):
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    B, T, V = 6, 5, 16001 if layout == "in_place" else 16000
+    kw = {"prompt": dict(prompt=3), "in_place": dict(prompt=1, offset=1)}
+    z, store = ref.row_logits(B, T, V, BF, gen, DEV, **kw.get(layout, {}))
+    ids, lengths = labels(B, T + 2, V, gen)[:, 1:1 + T], mixed_lengths(B, T)
+    _, lp, _ = ref.label_logprobs(z.double(), ids, lengths)
+    lp_ref = None if layout == "no_reference" else (lp + 0.2 * torch.randn((B, T), generator=gen, device=DEV)).float()
+    out, z64 = lib.PreferenceOutputs(z, in_place=layout == "in_place", want_lp_new=layout != "no_lp"), z.double()
+    if layout == "other_offset":
+        out.dlogits = torch.full((B * T * V + 3,), 7.0, dtype=BF, device=DEV)[3:].view(B, T, V)
+    check_preference(z, ids, lengths, lp_ref, kind, 0.2 if layout != "no_reference" else 0.01, -0.3, 0.0, kind == 2, 50.0, out, z64)
+
+
+def test_preference_saturated_pairs_and_bad_ids():
+    """Ratios of hundreds of nats (no overflow), empty responses, ids out of range."""
+    gen = torch.Generator(device=DEV).manual_seed(18)
+    B, T, V = 8, 6, 8200
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    ids = labels(B, T, V, gen)
+    lengths = torch.tensor([T, T, 0, 0, T, 2, 0, T + 1], dtype=torch.int32, device=DEV)
+    _, lp, _ = ref.label_logprobs(z.double(), ids, lengths)
+    lp_ref = lp.float()
+    lp_ref[0] -= 100.0
+    lp_ref[1] += 100.0
+    ids[5, 1], ids[4, 0] = V + 5, -7
+    for kind in (0, 1, 2):
+        got, ws = check_preference(z, ids, lengths, lp_ref, kind, 1.0, 0.0, 0.0, False, 1.0)
+        assert lib.poll_status(ws) == 16 | 32
+        assert torch.isfinite(got.loss).all()
+        assert (got.dlogits[4, 0] == 0).all() and (got.dlogits[5, 1] == 0).all()
+
+
+def test_repeated_calls_give_the_same_bits_and_leave_the_workspace_usable():
+    gen = torch.Generator(device=DEV).manual_seed(19)
+    for V in (1000, 32000, 50257, 128256):
+        B, T = 6, 37
+        z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+        ids, lengths = labels(B, T, V, gen), mixed_lengths(B, T)
+        lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
+        ws = lib.workspace(B, T, DEV)
+        runs = []
+        for _ in range(3):
+            a = lib.policy_kl_loss_fwd_bwd(z, ids, lengths, lp_old, lp_ref, adv, 0.2, 0.3, 0.1, 1, 1.0, ws)
+            b = lib.preference_loss_fwd_bwd(z, ids, lengths, lp_ref, 0, 0.1, 0.0, 0.0, False, 1.0, ws)
+            runs.append([a.loss, a.dlogits, a.lp_new, b.loss, b.dlogits, b.rewards, b.lp_new])
+        for r in runs[1:]:
+            assert all(torch.equal(x, y) for x, y in zip(runs[0], r))
+        assert lib.poll_status(ws) == 0
