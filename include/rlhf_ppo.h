@@ -297,6 +297,22 @@ int rlhf_ppo_loss_fwd_bwd_ex(const void* logits, int logits_dtype, long long str
 int rlhf_ppo_stats(const float* lp_new, const float* lp_old, const float* adv, const int* lengths, int B, int T,
                    float clip_eps, float* out_stats, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * A teacher's K largest log-probs per token, the targets of rlhf_distill_loss_fwd_bwd.  For t < lengths[b], with
+ * x = logits[b,t,:] / temperature: the entries of the K largest logits, in descending order of the logit and, where
+ * logits are equal, ascending order of the entry,
+ *     out_ids[b,t,k] = v_k,   out_logprobs[b,t,k] = x_{v_k} - log sum_v exp(x_v)
+ * Deleted entries (-inf) are never taken; slots that are left over (fewer than K entries) are -1 and -inf.  At padded
+ * positions both outputs are 0.  One streaming read of each valid row.
+ *   logits          bf16 or binary16 (logits_dtype) through (stride_b, stride_t)   read
+ *   out_ids         int32 [B,T,K], out_logprobs fp32 [B,T,K], contiguous           written
+ *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE; K may exceed V); temperature > 0, finite.   workspace as for step 1.
+ */
+#define RLHF_TOPK_MAX 256
+int rlhf_topk_logprobs(const void* logits, int logits_dtype, long long stride_b, long long stride_t, const int* lengths,
+                       int B, int T, int V, int K, float temperature, int* out_ids, float* out_logprobs,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* What a loss is a mean over. */
 typedef enum {
     RLHF_MEAN_TOKENS = 0,       /* every valid token weighs 1/N */

@@ -49,6 +49,7 @@ SIGNATURES = {
     "rlhf_ppo_loss_fwd_bwd_noalloc": (_int, [_vp, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
                                              _int, _int, _int, _f32, _f32, _f32, _vp, _vp,
                                              _vp, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "rlhf_topk_logprobs": (_int, [_vp, _int, _i64, _i64, _vp, _int, _int, _int, _int, _f32, _vp, _vp, _vp, _sz, _vp]),
     "rlhf_policy_kl_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64,
                                            _int, _int, _int, _f32, _f32, _f32, _int, _f32, _vp, _vp,
                                            _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
@@ -428,6 +429,37 @@ def _vector(t: torch.Tensor, n: int, what: str) -> int:
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous tensor of {n} floats")
     return t.data_ptr()
+
+
+TOPK_MAX = 256
+
+
+class TopK:
+    """Buffers written by topk_logprobs: int32 ids and fp32 log-probs, [B,T,K]; reusable from call to call."""
+
+    def __init__(self, B: int, T: int, K: int, device):
+        self.ids = torch.empty((B, T, K), dtype=torch.int32, device=device)
+        self.logprobs = torch.empty((B, T, K), dtype=torch.float32, device=device)
+
+
+def topk_logprobs(logits: torch.Tensor, lengths: torch.Tensor, k: int, temperature: float, ws: torch.Tensor,
+                  out: Optional[TopK] = None) -> TopK:
+    """rlhf_topk_logprobs: the k largest log-probs of every row and their entries (1 <= k <= TOPK_MAX)."""
+    B, T, V, sb, st = _logits(logits, "logits")
+    _lengths(lengths, B)
+    if out is None:
+        out = TopK(B, T, max(k, 0), logits.device)
+    for name, t, dtype in (("out.ids", out.ids, torch.int32), ("out.logprobs", out.logprobs, torch.float32)):
+        _dev(t, dtype, name)
+        if tuple(t.shape) != (B, T, k) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous [{B},{T},{k}] tensor")
+    _together(logits, ("lengths", lengths), ("ws", ws), ("out.ids", out.ids), ("out.logprobs", out.logprobs))
+    wp, wn = _ws(ws)
+    with torch.cuda.device(logits.device):
+        _check(lib().rlhf_topk_logprobs(logits.data_ptr(), DTYPES[logits.dtype], sb, st, lengths.data_ptr(), B, T, V, k,
+                                        temperature, out.ids.data_ptr(), out.logprobs.data_ptr(), wp, wn,
+                                        _stream(logits)), "rlhf_topk_logprobs")
+    return out
 
 
 class PolicyKlOutputs:

@@ -17,6 +17,7 @@
 #include "kernels_warp.cuh"
 #include "kernels_small.cuh"
 #include "kernels_objective.cuh"
+#include "kernels_topk.cuh"
 
 namespace {
 
@@ -47,6 +48,7 @@ constexpr size_t kRowLossOffset = 24576;
 constexpr int kMaxFusedBlocks = (int)((kRowLossOffset - kPartialsOffset) / 16);   // block partials that fit the header
 
 constexpr long long kMaxTokens = 1ll << 29;
+static_assert(RLHF_TOPK_MAX == kTopkMax, "the public bound and the kernels' agree");
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -485,6 +487,25 @@ int launch_check(const char* what)
     return RLHF_OK;
 }
 
+template <int NT, bool kF16>
+int launch_topk_as(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
+{
+    if (int e = keep_max_carveout(topk_logprobs_kernel<NT, kF16>)) return e;
+    const long long blocks = (long long)dev.sm_count * std::max(1, 1024 / NT);
+    const int grid = (int)std::min<long long>((long long)ta.B * ta.T, blocks);
+    RLHF_CUDA(launch_kernel(topk_logprobs_kernel<NT, kF16>, grid, NT, 0, s, ta));
+    return launch_check("topk_logprobs_kernel");
+}
+
+// Threads per row: 256 and four rows per SM, or 1024 where there are no more rows than SMs.
+template <bool kF16>
+int launch_topk(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
+{
+    if ((long long)ta.B * ta.T <= dev.sm_count && ta.V > 16384) return launch_topk_as<1024, kF16>(ta, dev, s);
+    return launch_topk_as<256, kF16>(ta, dev, s);
+}
+
+
 // Launches the row kernel for an objective with one generated token per row.  Sets a.fused if that kernel also does
 // the finalisation (the losses; value loss and dvalues in step 4); otherwise it leaves per-token terms in a.row_loss
 // (and a.row_kl).
@@ -648,6 +669,37 @@ int rlhf_gather_logprobs(const void* logits, long long stride_b, long long strid
 {
     return rlhf_gather_logprobs_ex(logits, RLHF_BF16, stride_b, stride_t, ids, ids_stride_b, lengths, B, T, V,
                                    out_logprobs, nullptr, workspace, workspace_bytes, stream);
+}
+
+int rlhf_topk_logprobs(const void* logits, int logits_dtype, long long stride_b, long long stride_t, const int* lengths,
+                       int B, int T, int V, int K, float temperature, int* out_ids, float* out_logprobs,
+                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !lengths || !out_ids || !out_logprobs) return RLHF_ERR_NULL;
+    if (logits_dtype != RLHF_BF16 && logits_dtype != RLHF_F16) return RLHF_ERR_SCALAR;
+    if (int e = check_shape(B, T, V)) return e;
+    if (K <= 0 || K > RLHF_TOPK_MAX) return RLHF_ERR_SHAPE;
+    if (stride_b < 0 || stride_t < 0 || (T > 1 && stride_t < V)) return RLHF_ERR_STRIDE;
+    if (!std::isfinite(temperature) || !(temperature > 0.f)) return RLHF_ERR_SCALAR;
+    if (!aligned(logits, 2) || !aligned(lengths, 4) || !aligned(out_ids, 4) || !aligned(out_logprobs, 4)) return RLHF_ERR_ALIGN;
+    if (int e = check_workspace(workspace, workspace_bytes, rlhf_workspace_bytes(B, T))) return e;
+    DeviceInfo dev;
+    if (int e = device_info(dev)) return e;
+    char* ws = (char*)workspace;
+    TopkArgs a{};
+    a.logits = (const uint16_t*)logits;
+    a.stride_b = stride_b;
+    a.stride_t = stride_t;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V; a.K = K;
+    a.scale = (float)(1.4426950408889634 / (double)temperature);
+    a.ids = out_ids;
+    a.logprobs = out_logprobs;
+    a.status = (unsigned*)ws;
+    a.ticket = (unsigned*)(ws + 4);
+    a.row_counter = (unsigned*)(ws + 16);
+    cudaStream_t s = (cudaStream_t)stream;
+    return logits_dtype == RLHF_F16 ? launch_topk<true>(a, dev, s) : launch_topk<false>(a, dev, s);
 }
 
 int rlhf_kl_reward(const float* lp_old, const float* lp_ref, const float* score, const int* lengths,

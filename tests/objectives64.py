@@ -82,3 +82,19 @@ def row_logits(B, T, V, dtype, gen, device, sigma=3.0, prompt=0, offset=0, pitch
     z = full[:, prompt:, :V]
     z.copy_(sigma * torch.randn((B, T, V), generator=gen, device=device))
     return z, store
+
+
+def topk(z, lengths, K, temperature):
+    """ids (int64) and log-probs of the K largest entries: value descending, then entry ascending; -1 / -inf left over."""
+    B, T, V = z.shape
+    lq = torch.log_softmax(z / temperature, dim=2)
+    top, at = z.sort(dim=2, descending=True, stable=True)
+    k = min(K, V)
+    ids = torch.full((B, T, K), -1, dtype=torch.int64, device=z.device)
+    lp = torch.full((B, T, K), float("-inf"), dtype=torch.float64, device=z.device)
+    keep = top[..., :k] > float("-inf")
+    ids[..., :k] = torch.where(keep, at[..., :k], -1)
+    lp[..., :k] = torch.where(keep, lq.gather(2, at[..., :k]), float("-inf"))
+    pad = ~valid_mask(lengths, T)
+    ids[pad], lp[pad] = 0, 0.0
+    return ids, lp

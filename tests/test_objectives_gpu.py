@@ -249,3 +249,77 @@ def test_repeated_calls_give_the_same_bits_and_leave_the_workspace_usable():
         for r in runs[1:]:
             assert all(torch.equal(x, y) for x, y in zip(runs[0], r))
         assert lib.poll_status(ws) == 0
+
+
+# ---------------------------------------------------------------- the teacher's top log-probs
+def check_topk(z, lengths, K, temperature):
+    B, T, V = z.shape
+    ws = lib.workspace(B, T, DEV)
+    got = lib.topk_logprobs(z, lengths, K, temperature, ws)
+    ids, lp = ref.topk(z.double(), lengths, K, temperature)
+    assert torch.equal(got.ids.long(), ids)
+    assert torch.equal(torch.isinf(got.logprobs), torch.isinf(lp))
+    fine = torch.isfinite(lp)
+    # LP bounds the log of the sum.  The entry itself, ln2 * ((z - maximum) * log2(e) / temperature - log2(sum)), takes four
+    # roundings that are relative to its size (the factor, the fused product, ln2, the result; 2^-24 each): 2^-22 |lp|,
+    # which exceeds LP at the -60000 of a row with one entry of 60000, where half a step of fp32 alone is 0.002.
+    assert ((got.logprobs.double() - lp).abs()[fine] <= LP * max(1.0, 1 / temperature) + 2.0 ** -22 * lp[fine].abs()).all()
+    return got, ws
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("B,T,V,K", [(1, 1, 1, 1), (2, 3, 7, 9), (1, 1, 50272, 20), (3, 5, 1000, 256), (3, 5, 1001, 1), (2, 9, 2047, 100),
+                                     (3, 70, 8200, 33), (4, 60, 32000, 64), (2, 3, 50257, 50), (2, 200, 50257, 7),
+                                     (2, 3, 128256, 256), (3, 101, 128256, 128), (1, 2, 300001, 256)])
+def test_topk_sizes(B, T, V, K, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(V + K)
+    z, _ = ref.row_logits(B, T, V, dtype, gen, DEV, prompt=1 if V < 60000 else 0, pitch=3 if V % 2 else 0)
+    lengths = mixed_lengths(B, T)
+    _, ws = check_topk(z, lengths, K, 1.0 if V % 2 else 2.0)
+    assert lib.poll_status(ws) == 0
+
+
+def test_topk_ties_runs_and_deleted_entries():
+    gen = torch.Generator(device=DEV).manual_seed(31)
+    B, T, V = 12, 2, 20003
+    for dtype in (BF, HF):
+        z, _ = ref.row_logits(B, T, V, dtype, gen, DEV, pitch=2)
+        z[0] = 0.0                                           # all entries equal
+        z[1] = -0.0
+        z[1, :, 1::2] = 0.0                                  # the two zeros are the same value
+        z[2] = z[2].round()                                  # a few values, each many times
+        z[3] = torch.linspace(-4, 4, V, device=DEV)          # ascending: the top sits in neighbouring vectors
+        z[4] = torch.linspace(4, -4, V, device=DEV)
+        z[5] = float("-inf")
+        z[5, :, V - 3:] = 1.0                                # three entries left
+        z[6, :, ::3] = float("-inf")
+        z[7, :, 8:16] = 50.0                                 # one vector far above the rest
+        z[8] = -3.0
+        z[8, :, -300:] = -2.0                                # more equal entries than K, at the end
+        z[9, :, 0] = 60000.0 if dtype == HF else 1e30
+        z[10] = -1000.0
+        z[10, 1, 77] = 900.0
+        z[11, :, 5::1024] = 20.0                             # the top in one thread's vectors
+        lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+        for K in (1, 5, 64, 256):
+            check_topk(z, lengths, K, 1.0)
+
+
+def test_topk_lengths_out_of_range_and_non_finite_logits():
+    gen = torch.Generator(device=DEV).manual_seed(32)
+    B, T, V, K = 3, 3, 9000, 16
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    lengths = torch.tensor([T + 4, -1, 2], dtype=torch.int32, device=DEV)
+    _, ws = check_topk(z, lengths, K, 0.7)
+    assert lib.poll_status(ws) == 32
+    # rows with NaN or +inf give NaN in their own outputs, never a fault, and leave the other rows alone
+    z[0, 0, 7] = float("nan")
+    z[0, 1, 8] = float("inf")
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    got = lib.topk_logprobs(z, lengths, K, 1.0, ws)
+    ids, lp = ref.topk(z.double(), lengths, K, 1.0)
+    clean = torch.ones((B, T), dtype=torch.bool, device=DEV)
+    clean[0, :2] = False
+    assert torch.equal(got.ids.long()[clean], ids[clean])
+    assert torch.isnan(got.logprobs[0, :2]).any()
+    assert lib.poll_status(ws) == 0
