@@ -313,6 +313,39 @@ int rlhf_topk_logprobs(const void* logits, int logits_dtype, long long stride_b,
                        int B, int T, int V, int K, float temperature, int* out_ids, float* out_logprobs,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* How the teacher's K entries of a token, with log-probs lt_k, stand for its whole distribution. */
+typedef enum {
+    RLHF_DISTILL_PLAIN = 0,       /* as they are: p_k = exp(lt_k) */
+    RLHF_DISTILL_NORMALISED = 1,  /* scaled to sum 1: p_k = exp(lt_k) / sum_j exp(lt_j) */
+    RLHF_DISTILL_TAIL = 2         /* as they are, and the mass p_0 = max(0, 1 - sum_k p_k) outside them as one more class */
+} rlhf_distill_t;
+
+/*
+ * Distillation from a teacher's entries (rlhf_topk_logprobs, or any others), and its gradient.  For each valid token,
+ * with q = softmax(logits[b,t,:] / temperature), p as above, S the set of the token's entries and q_0 = sum_{v not in S} q_v,
+ *     L = sum_k p_k (log p_k - log q_{id_k})  [+ p_0 (log p_0 - log q_0) in the tail mode]
+ *     *out_loss = (1/N) sum temperature^2 L
+ *     out_dlogits[b,t,v] = grad_scale * temperature / N * (W q_v - p_v)        v in S
+ *                        = grad_scale * temperature / N * (W - p_0 / q_0) q_v   otherwise
+ * with W = p_0 + sum_k p_k (p_0 = 0 outside the tail mode); the gradient is that of *out_loss, times grad_scale.  An entry
+ * named twice has the sum of its weights (log p_k stays that of each mention).  Entries -1 are unused; others outside
+ * [0,V) set RLHF_ERR_ID_RANGE and count as unused.  A token without entries adds 0 to a plain or normalised loss.  Where no
+ * vocabulary entry is left outside S, or their mass is below the range of fp32, the tail term is left out.  A deleted
+ * student entry (-inf) with p_k > 0 makes the loss infinite, as the definition has it.
+ *   logits, lengths, out_dlogits   as step 4 (logits_dtype: rlhf_dtype_t of both tensors; in place allowed)
+ *   topk_ids, topk_logprobs   int32 / fp32, [b*topk_stride_b + t*topk_stride_t + k], strides >= 0 in elements; the
+ *                  log-probs are the teacher's at this temperature                                    read
+ *   out_loss       fp32 scalar (device)                                                               written
+ *   out_row_loss   fp32 [B,T] or NULL: temperature^2 L of every token, 0 at padding                   written if given
+ *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE); temperature > 0, finite.   workspace as for step 1.
+ */
+int rlhf_distill_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                              const int* topk_ids, const float* topk_logprobs, long long topk_stride_b,
+                              long long topk_stride_t, int K, const int* lengths, int B, int T, int V, int mode,
+                              float temperature, float grad_scale, float* out_loss, float* out_row_loss,
+                              void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 /* What a loss is a mean over. */
 typedef enum {
     RLHF_MEAN_TOKENS = 0,       /* every valid token weighs 1/N */

@@ -50,6 +50,8 @@ SIGNATURES = {
                                              _int, _int, _int, _f32, _f32, _f32, _vp, _vp,
                                              _vp, _i64, _i64, _vp, _vp, _vp, _vp]),
     "rlhf_topk_logprobs": (_int, [_vp, _int, _i64, _i64, _vp, _int, _int, _int, _int, _f32, _vp, _vp, _vp, _sz, _vp]),
+    "rlhf_distill_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _vp, _i64, _i64, _int, _vp, _int, _int, _int, _int,
+                                         _f32, _f32, _vp, _vp, _vp, _i64, _i64, _vp, _sz, _vp]),
     "rlhf_policy_kl_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64,
                                            _int, _int, _int, _f32, _f32, _f32, _int, _f32, _vp, _vp,
                                            _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
@@ -60,6 +62,7 @@ SIGNATURES = {
 
 NOALLOC_MAX_TOKENS = 65536
 MEAN_TOKENS, MEAN_SEQUENCES = 0, 1                    # rlhf_reduction_t
+DISTILL_PLAIN, DISTILL_NORMALISED, DISTILL_TAIL = 0, 1, 2   # rlhf_distill_t
 PREF_SIGMOID, PREF_HINGE, PREF_SQUARED = 0, 1, 2      # rlhf_preference_t
 
 _lib = None
@@ -459,6 +462,46 @@ def topk_logprobs(logits: torch.Tensor, lengths: torch.Tensor, k: int, temperatu
         _check(lib().rlhf_topk_logprobs(logits.data_ptr(), DTYPES[logits.dtype], sb, st, lengths.data_ptr(), B, T, V, k,
                                         temperature, out.ids.data_ptr(), out.logprobs.data_ptr(), wp, wn,
                                         _stream(logits)), "rlhf_topk_logprobs")
+    return out
+
+
+class DistillOutputs:
+    """Buffers written by distill_loss_fwd_bwd; reusable from call to call."""
+
+    def __init__(self, logits: torch.Tensor, in_place: bool = False, want_row_loss: bool = True):
+        B, T = logits.shape[0], logits.shape[1]
+        self.loss = torch.empty(1, dtype=torch.float32, device=logits.device)
+        self.dlogits = logits if in_place else torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        self.row_loss = torch.empty((B, T), dtype=torch.float32, device=logits.device) if want_row_loss else None
+
+
+def distill_loss_fwd_bwd(logits: torch.Tensor, topk_ids: torch.Tensor, topk_logprobs: torch.Tensor, lengths: torch.Tensor,
+                         mode: int, temperature: float, grad_scale: float, ws: torch.Tensor,
+                         out: Optional[DistillOutputs] = None) -> DistillOutputs:
+    """rlhf_distill_loss_fwd_bwd.  topk_ids (int32) and topk_logprobs (fp32) are [B,T,K] with equal strides and a contiguous
+    last axis; `mode` is DISTILL_PLAIN, DISTILL_NORMALISED or DISTILL_TAIL."""
+    B, T, V, sb, st = _logits(logits, "logits")
+    _lengths(lengths, B)
+    _dev(topk_ids, torch.int32, "topk_ids")
+    _dev(topk_logprobs, torch.float32, "topk_logprobs")
+    if topk_ids.dim() != 3 or tuple(topk_ids.shape[:2]) != (B, T) or topk_ids.shape != topk_logprobs.shape:
+        raise ValueError(f"topk_ids and topk_logprobs must be [{B},{T},K]")
+    K = topk_ids.shape[2]
+    if topk_ids.stride() != topk_logprobs.stride() or (K > 1 and topk_ids.stride(2) != 1):
+        raise ValueError("topk_ids and topk_logprobs must have the same strides and a contiguous last axis")
+    if out is None:
+        out = DistillOutputs(logits)
+    dsb, dst = _dlogits(out.dlogits, logits)
+    loss = _vector(out.loss, 1, "out.loss")
+    row_ptr = _bt(out.row_loss, B, T, "out.row_loss").data_ptr() if out.row_loss is not None else None
+    _together(logits, ("topk_ids", topk_ids), ("topk_logprobs", topk_logprobs), ("lengths", lengths), ("ws", ws),
+              ("out.loss", out.loss), ("out.dlogits", out.dlogits), ("out.row_loss", out.row_loss))
+    wp, wn = _ws(ws)
+    with torch.cuda.device(logits.device):
+        _check(lib().rlhf_distill_loss_fwd_bwd(
+            logits.data_ptr(), DTYPES[logits.dtype], sb, st, topk_ids.data_ptr(), topk_logprobs.data_ptr(),
+            topk_ids.stride(0), topk_ids.stride(1), K, lengths.data_ptr(), B, T, V, mode, temperature, grad_scale,
+            loss, row_ptr, out.dlogits.data_ptr(), dsb, dst, wp, wn, _stream(logits)), "rlhf_distill_loss_fwd_bwd")
     return out
 
 

@@ -18,6 +18,7 @@
 #include "kernels_small.cuh"
 #include "kernels_objective.cuh"
 #include "kernels_topk.cuh"
+#include "kernels_distill.cuh"
 
 namespace {
 
@@ -48,7 +49,7 @@ constexpr size_t kRowLossOffset = 24576;
 constexpr int kMaxFusedBlocks = (int)((kRowLossOffset - kPartialsOffset) / 16);   // block partials that fit the header
 
 constexpr long long kMaxTokens = 1ll << 29;
-static_assert(RLHF_TOPK_MAX == kTopkMax, "the public bound and the kernels' agree");
+static_assert(RLHF_TOPK_MAX == kTopkMax && RLHF_TOPK_MAX == kDistillMax, "the public bound and the kernels' agree");
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -192,7 +193,8 @@ struct CregPlan {
     size_t smem_bytes = 0;
 };
 
-CregPlan plan_creg(unsigned row_bytes, const DeviceInfo& dev)
+// K: teacher entries per row, 0 for the objectives of one generated token.
+CregPlan plan_creg(unsigned row_bytes, const DeviceInfo& dev, int K = 0)
 {
     CregPlan pl;
     if (row_bytes < 16384 || row_bytes % 16 != 0) return pl;
@@ -202,13 +204,14 @@ CregPlan plan_creg(unsigned row_bytes, const DeviceInfo& dev)
         const unsigned sv = (row_vecs + c - 1) / c;
         if (sv > cap) continue;
         int nb = kCregMaxBufs;
-        while (nb >= 2 && creg_smem_bytes(sv, kCregWarps, nb) + 2048 > (size_t)dev.max_smem_optin) --nb;
+        // (2 KB of static shared memory; the distillation variant has half a kilobyte more)
+        while (nb >= 2 && creg_smem_bytes(sv, kCregWarps, nb, K) + (K > 0 ? 2816 : 2048) > (size_t)dev.max_smem_optin) --nb;
         if (nb < 2) continue;
         pl.cluster = c;
         pl.slice_vecs = sv;
         pl.tmem_cols = creg_tmem_cols(sv, kCregWarps);
         pl.n_buf = nb;
-        pl.smem_bytes = creg_smem_bytes(sv, kCregWarps, nb);
+        pl.smem_bytes = creg_smem_bytes(sv, kCregWarps, nb, K);
         return pl;
     }
     return pl;
@@ -216,7 +219,7 @@ CregPlan plan_creg(unsigned row_bytes, const DeviceInfo& dev)
 
 // Clusters of the kernel that the device holds at once (one block per SM); looked up once per device and
 // cluster size.  It only sizes the persistent grid: a larger grid would still be correct.
-template <int NW, int C, bool kTmem, bool kF16, bool kAny>
+template <int NW, int C, bool kTmem, bool kF16, bool kAny, bool kDistill>
 int creg_resident_clusters(const CregPlan& pl, const DeviceInfo& dev, int& out)
 {
     if (C == 1) { out = dev.sm_count; return RLHF_OK; }
@@ -229,8 +232,8 @@ int creg_resident_clusters(const CregPlan& pl, const DeviceInfo& dev, int& out)
         int n = 0;
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
-        fill_launch_config(cfg, attr, dev.sm_count / C * C, NW * 32 + 32, pl.smem_bytes, C, nullptr);
-        RLHF_CUDA(cudaOccupancyMaxActiveClusters(&n, loss_creg_kernel<NW, C, kTmem, kF16, kAny>, &cfg));
+        fill_launch_config(cfg, attr, dev.sm_count / C * C, NW * 32 + (kDistill ? 96 : 32), pl.smem_bytes, C, nullptr);
+        RLHF_CUDA(cudaOccupancyMaxActiveClusters(&n, loss_creg_kernel<NW, C, kTmem, kF16, kAny, kDistill>, &cfg));
         if (n < 1) n = 1;
         if (d < 0 || d >= 64) { out = n; return RLHF_OK; }
         cached[d] = n;
@@ -239,10 +242,12 @@ int creg_resident_clusters(const CregPlan& pl, const DeviceInfo& dev, int& out)
     return RLHF_OK;
 }
 
-template <int NW, int C, bool kTmem, bool kF16, bool kAny = false>
-int launch_creg(const RowArgs& a, const CregPlan& pl, const DeviceInfo& dev, cudaStream_t s)
+template <int NW, int C, bool kTmem, bool kF16, bool kAny = false, bool kDistill = false>
+int launch_creg(const RowArgs& a, const CregPlan& pl, const DeviceInfo& dev, cudaStream_t s, const DistillArgs& d = DistillArgs{})
 {
+    auto kernel = loss_creg_kernel<NW, C, kTmem, kF16, kAny, kDistill>;
     CregArgs ca{};
+    ca.distill = d;
     ca.row = a;
     ca.row_bytes = 2u * (unsigned)a.V;
     ca.slice_vecs = pl.slice_vecs;
@@ -250,13 +255,12 @@ int launch_creg(const RowArgs& a, const CregPlan& pl, const DeviceInfo& dev, cud
     ca.tmem_cols = pl.tmem_cols;
     ca.n_buf = pl.n_buf;
     ca.row_counter = (unsigned*)((char*)a.status + 16);
-    RLHF_CUDA(cudaFuncSetAttribute(loss_creg_kernel<NW, C, kTmem, kF16, kAny>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)pl.smem_bytes));
+    RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pl.smem_bytes));
     int clusters = 0;
-    if (int e = creg_resident_clusters<NW, C, kTmem, kF16, kAny>(pl, dev, clusters)) return e;
+    if (int e = creg_resident_clusters<NW, C, kTmem, kF16, kAny, kDistill>(pl, dev, clusters)) return e;
     const long long rows = (long long)a.B * a.T;
     const int grid = (int)std::min<long long>(rows, clusters) * C;
-    RLHF_CUDA(launch_kernel_cluster(loss_creg_kernel<NW, C, kTmem, kF16, kAny>, grid, NW * 32 + 32, pl.smem_bytes, C, s, ca));
+    RLHF_CUDA(launch_kernel_cluster(kernel, grid, NW * 32 + (kDistill ? 96 : 32), pl.smem_bytes, C, s, ca));
     return RLHF_OK;
 }
 
@@ -365,10 +369,10 @@ int launch_cring_cluster(const RowArgs& a, const CringPlan& pl, const DeviceInfo
 // cluster) fits, else the chunk ring.
 // Rows off 16-byte boundaries: the kernel loads the aligned span around a row, at most 14 bytes before it and 14 after;
 // only single blocks take such rows.
-CregPlan plan_creg_any(int V, const DeviceInfo& dev)
+CregPlan plan_creg_any(int V, const DeviceInfo& dev, int K = 0)
 {
     const unsigned span = (14u + 2u * (unsigned)V + 15u) & ~15u;
-    CregPlan pl = plan_creg(span, dev);
+    CregPlan pl = plan_creg(span, dev, K);
     if (pl.cluster != 1) pl.cluster = 0;
     return pl;
 }
@@ -485,6 +489,48 @@ int launch_check(const char* what)
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, what);
     return RLHF_OK;
+}
+
+// Distillation rows on the on-chip-exponentials kernel.
+template <bool kTmem, bool kF16>
+int launch_distill_creg(const RowArgs& a, const DistillArgs& d, const CregPlan& pl, bool any, const DeviceInfo& dev, cudaStream_t s)
+{
+    constexpr int NW = kCregWarps;
+    if (any) return launch_creg<NW, 1, kTmem, kF16, true, true>(a, pl, dev, s, d);
+    switch (pl.cluster) {
+        case 1: return launch_creg<NW, 1, kTmem, kF16, false, true>(a, pl, dev, s, d);
+        case 2: return launch_creg<NW, 2, kTmem, kF16, false, true>(a, pl, dev, s, d);
+        case 3: return launch_creg<NW, 3, kTmem, kF16, false, true>(a, pl, dev, s, d);
+        default: return launch_creg<NW, 4, kTmem, kF16, false, true>(a, pl, dev, s, d);
+    }
+}
+
+// Launches the distillation row kernel; sets a.fused if it also forms the mean.
+int launch_distill_rows(RowArgs& a, const DistillArgs& d, bool f16, const DeviceInfo& dev, char* ws, cudaStream_t s)
+{
+    const bool all_16B = rows_16B(a.logits, a.stride_b, a.stride_t, a.V) && rows_16B(a.dlogits, a.dl_stride_b, a.dl_stride_t, a.V);
+    const bool same_offsets = ((reinterpret_cast<uintptr_t>(a.dlogits) - reinterpret_cast<uintptr_t>(a.logits)) % 16) == 0 &&
+                              ((a.dl_stride_b - a.stride_b) % 8) == 0 && ((a.dl_stride_t - a.stride_t) % 8) == 0;
+    CregPlan pl;
+    if (all_16B) pl = plan_creg(2u * (unsigned)a.V, dev, d.K);
+    else if (same_offsets) pl = plan_creg_any(a.V, dev, d.K);
+    if (pl.cluster > 0 && dev.sm_count * 7 <= kMaxFusedBlocks) {
+        a.fused = 1;
+        a.ticket = (unsigned*)(ws + 4);
+        a.partials = (double*)(ws + kPartialsOffset);
+        int e;
+        if (pl.tmem_cols != 0) e = f16 ? launch_distill_creg<true, true>(a, d, pl, !all_16B, dev, s) : launch_distill_creg<true, false>(a, d, pl, !all_16B, dev, s);
+        else e = f16 ? launch_distill_creg<false, true>(a, d, pl, !all_16B, dev, s) : launch_distill_creg<false, false>(a, d, pl, !all_16B, dev, s);
+        return e ? e : launch_check("loss_creg_kernel<distill>");
+    }
+    DistillRowArgs da{};
+    da.row = a;
+    da.distill = d;
+    da.same_offsets = same_offsets ? 1 : 0;
+    const int grid = (int)std::min<long long>((long long)a.B * a.T, (long long)dev.sm_count * 8);
+    if (f16) RLHF_CUDA(launch_kernel(distill_row_kernel<true>, grid, kDistillThreads, 0, s, da));
+    else RLHF_CUDA(launch_kernel(distill_row_kernel<false>, grid, kDistillThreads, 0, s, da));
+    return launch_check("distill_row_kernel");
 }
 
 template <int NT, bool kF16>
@@ -1126,6 +1172,72 @@ int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long
     RLHF_CUDA(launch_kernel(preference_pair_kernel, std::min(B / 2, 1184), kPairThreads, 0, s, pa));
     if (int e = launch_check("preference_pair_kernel")) return e;
     return launch_objective_rows(a, f16, dev, ws, s);
+}
+
+int rlhf_distill_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                              const int* topk_ids, const float* topk_logprobs, long long topk_stride_b,
+                              long long topk_stride_t, int K, const int* lengths, int B, int T, int V, int mode,
+                              float temperature, float grad_scale, float* out_loss, float* out_row_loss,
+                              void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                              void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !topk_ids || !topk_logprobs || !lengths || !out_loss || !out_dlogits) return RLHF_ERR_NULL;
+    if (K <= 0 || K > RLHF_TOPK_MAX) return RLHF_ERR_SHAPE;
+    if (int e = check_rows(logits, logits_dtype, stride_b, stride_t, 0, B, T, V, out_dlogits, dl_stride_b, dl_stride_t))
+        return e;
+    if (topk_stride_b < 0 || topk_stride_t < 0) return RLHF_ERR_STRIDE;
+    if ((mode != RLHF_DISTILL_PLAIN && mode != RLHF_DISTILL_NORMALISED && mode != RLHF_DISTILL_TAIL) ||
+        !std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(grad_scale))
+        return RLHF_ERR_SCALAR;
+    if (!aligned(topk_ids, 4) || !aligned(topk_logprobs, 4) || !aligned(lengths, 4) || !aligned(out_loss, 4) ||
+        !aligned(out_row_loss, 4))
+        return RLHF_ERR_ALIGN;
+    if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
+    DeviceInfo dev;
+    if (int e = device_info(dev)) return e;
+
+    char* ws = (char*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    RowArgs a{};
+    a.objective = kObjDistill;
+    a.logits = (const uint16_t*)logits;
+    a.stride_b = stride_b;
+    a.stride_t = stride_t;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.status = (unsigned*)ws;
+    a.wait_limit_ns = kWaitLimitNs;
+    a.grad_scale = grad_scale;
+    a.dlogits = (uint16_t*)out_dlogits;
+    a.dl_stride_b = dl_stride_b;
+    a.dl_stride_t = dl_stride_t;
+    a.row_loss = (float*)(ws + kRowLossOffset);
+    a.out_lp_new = out_row_loss;
+    a.out_loss_pg = out_loss;
+    DistillArgs d{};
+    d.ids = topk_ids;
+    d.logprobs = topk_logprobs;
+    d.stride_b = topk_stride_b;
+    d.stride_t = topk_stride_t;
+    d.K = K;
+    d.mode = mode;
+    d.tau = temperature;
+    d.scale = (float)(1.4426950408889634 / (double)temperature);
+    if (int e = launch_distill_rows(a, d, logits_dtype == RLHF_F16, dev, ws, s)) return e;
+    if (a.fused) return RLHF_OK;
+
+    RowSumArgs f{};
+    f.lengths = lengths;
+    f.B = B; f.T = T;
+    f.row_loss = a.row_loss;
+    f.out_lp_new = out_row_loss;
+    f.out_loss = out_loss;
+    f.ticket = (unsigned*)(ws + 4);
+    f.partials = (double*)(ws + kPartialsOffset);
+    const int fgrid = (int)std::min<long long>(((long long)B * T + 1023) / 1024, kFinalMaxBlocks);
+    if (int e = keep_max_carveout(row_sums_kernel)) return e;
+    RLHF_CUDA(launch_kernel(row_sums_kernel, fgrid, kFinalThreads, 0, s, f));
+    return launch_check("row_sums_kernel");
 }
 
 }  // extern "C"

@@ -40,6 +40,14 @@
 // (RowArgs::wait_limit_ns); if one runs out the thread flags RLHF_ERR_TIMEOUT, stops waiting and lets the
 // block drain.  The tensor-memory columns are released by the warp that took them, after all consumers
 // have passed a block barrier at the end of the kernel.
+//
+// kDistill: the row's loss is distillation from up to 256 teacher entries instead of an objective of one generated
+// token.  Two more warps serve it.  The target warp turns the entries of a row into weights while the row is still on
+// its way, then takes the logits of those entries out of the buffer (they become -inf, as the generated token's does
+// above, so that the sum over the other entries -- the student's mass outside the teacher's entries -- comes without
+// cancellation).  The consumers' two passes are as above, with one factor for all entries that are not the teacher's.
+// The patch warp then writes the gradients of the teacher's entries into the finished buffer and forms the row's loss,
+// while the consumers are on the next row; the producer drains the buffer when it is done.
 #pragma once
 #include "kernels_ring.cuh"
 
@@ -54,6 +62,7 @@ struct RowInfo {
     int y;                  // generated token (0 if it was out of range)
     int bad_id;
     RowScalars sc;
+    long long entries;      // kDistill: element offset of the row's teacher entries
     unsigned mis;           // bytes between the 16-byte boundary below the row's first logit and that logit
     unsigned pad;
 };
@@ -101,6 +110,43 @@ constexpr int kCregZeroBytes = 16384;  // zeroed buffer that feeds the bulk zero
 #define RLHF_CREG_PIECE 16384
 #endif
 
+constexpr int kDistillMax = 256;       // teacher entries per row
+constexpr int kDistillZeroBytes = 4096;
+constexpr int kDistillPlain = 0, kDistillNormalised = 1, kDistillTail = 2;
+
+struct DistillArgs {
+    const int* ids;          // teacher entries of row (b,t): [b*stride_b + t*stride_t + k], k < K; < 0 = unused
+    const float* logprobs;
+    long long stride_b, stride_t;
+    int K, mode;
+    float tau, scale;        // temperature, log2(e) / temperature
+};
+
+// What the target warp knows of a row's teacher entries.
+struct TargetInfo {
+    double H;                // sum p log p over the entries
+    float P, p0, W;          // sum p; mass outside them (tail mode); P + p0
+    float pr[4];             // sum p over the entries of each block's slice
+};
+
+// Factor of a row's entries that are not the teacher's: d loss / d z_v = factor * q_v / tau.  s: the student's mass on
+// them, relative; q0 = s / (s + ey).  No such entry, or a mass below the fp32 range: the tail term is left out.
+__device__ __forceinline__ float distill_factor(const TargetInfo& ti, float s, float q0)
+{
+    return ti.p0 > 0.f && s > 0.f ? ti.W - ti.p0 / q0 : ti.P;
+}
+
+// Loss of a row.  With x the scaled logits and M a reference, zy = sum_k p_k (x_k - M); s and ey are the sums of 2^(x-M)
+// over the other and over the teacher's entries.
+__device__ inline double distill_loss(const TargetInfo& ti, float zy, float s, float ey)
+{
+    constexpr double ln2 = 0.6931471805599453;
+    const double l2 = log2((double)s + (double)ey);
+    double L = ti.H - ln2 * ((double)zy - (double)ti.P * l2);
+    if (ti.p0 > 0.f && s > 0.f) L += (double)ti.p0 * (log((double)ti.p0) - ln2 * (log2((double)s) - l2));
+    return L;
+}
+
 struct CregArgs {
     RowArgs row;
     unsigned row_bytes;      // 2*V, a multiple of 16
@@ -109,6 +155,7 @@ struct CregArgs {
     unsigned tmem_cols;      // tensor-memory columns to take: 0, or a power of two from 32 to 512
     int n_buf;               // slice buffers per block: 2 or 3
     unsigned* row_counter;   // workspace word, zero between calls: next row to hand out (kCluster == 1)
+    DistillArgs distill;     // kDistill
 };
 
 // A slice buffer holds the same number of vectors for every consumer thread; the vectors past the end of the
@@ -120,9 +167,12 @@ inline size_t creg_buf_stride(unsigned slice_vecs, int consumer_warps)
     return (slice_vecs + per_round - 1) / per_round * per_round * 16;
 }
 constexpr int kCregMaxBufs = 3;
-inline size_t creg_smem_bytes(unsigned slice_vecs, int consumer_warps, int n_buf)
+// K: teacher entries per row (0: not distillation), for each of which a buffer carries position, weight and logit.
+inline int distill_pad(int K) { return (K + 31) / 32 * 32; }
+inline size_t creg_smem_bytes(unsigned slice_vecs, int consumer_warps, int n_buf, int K = 0)
 {
-    return (size_t)n_buf * creg_buf_stride(slice_vecs, consumer_warps) + kCregZeroBytes + 64;
+    return (size_t)n_buf * (creg_buf_stride(slice_vecs, consumer_warps) + 12 * (size_t)distill_pad(K)) +
+           (K > 0 ? kDistillZeroBytes : kCregZeroBytes) + 64;
 }
 // Columns of tensor memory that a block needs for slices of `slice_vecs` vectors: each warp stores 8 columns per
 // vector beyond the first kRegVecsTmem; warps w, w+4, w+8, ... share 32 lanes and take consecutive column ranges.
@@ -245,13 +295,15 @@ __device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::
 // loaded, the entries of its first and last vector that belong to neighbouring rows are turned into -inf in the
 // buffer before the first pass, and only the row's own bytes are stored: whole vectors by bulk store, the ragged
 // ends by 2-byte stores.
-template <int NW, int kCluster, bool kTmem, bool kF16, bool kAny = false>
-__global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
+// kDistill: see the head of the file.
+template <int NW, int kCluster, bool kTmem, bool kF16, bool kAny = false, bool kDistill = false>
+__global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_kernel(CregArgs ca)
 {
     static_assert(!kAny || kCluster == 1, "rows off 16-byte boundaries are not split over a cluster");
     constexpr int kRegVecs = kTmem ? kRegVecsTmem : kRegVecsOnly;
     constexpr int kCons = NW * 32;
-    constexpr int kThreads = kCons + 32;
+    constexpr int kThreads = kCons + (kDistill ? 96 : 32);
+    constexpr int kZeroBytesHere = kDistill ? kDistillZeroBytes : kCregZeroBytes;
     constexpr uint32_t kPiece = RLHF_CREG_PIECE;  // size of one bulk copy
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ long long s_cnt[33];
@@ -267,8 +319,16 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
     static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     static_assert(kCregMaxBufs * 16 <= 64, "the mbarriers of the buffers take the 64 bytes after the zero buffer");
     __shared__ uint32_t s_tmem_base;
+    // kDistill: barriers announced / ready / patched of every buffer, and what target warp, consumers and patch warp hand on
+    constexpr int kBufsHere = kDistill ? kCregMaxBufs : 1;
+    __shared__ __align__(8) unsigned long long s_dbar[3 * kBufsHere];
+    __shared__ TargetInfo s_target[kBufsHere];
+    __shared__ LabelInfo s_tlab[kBufsHere];
+    __shared__ float4 s_total[kBufsHere];
 
     const RowArgs& p = ca.row;
+    const DistillArgs& dt = ca.distill;
+    const float xscale = kDistill ? dt.scale : kLog2e;       // logit -> base-2 exponent
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int NB = ca.n_buf;
     const uint32_t crank = kCluster > 1 ? cluster_ctarank() : 0u;
@@ -281,22 +341,35 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
 
     const uint32_t buf_addr = smem_u32(smem);
     unsigned char* zero_buf = smem + (size_t)NB * ca.buf_stride;
-    const uint32_t bar_addr = smem_u32(zero_buf + kCregZeroBytes);
+    const uint32_t bar_addr = smem_u32(zero_buf + kZeroBytesHere);
     auto landed = [&](int buf) { return bar_addr + 8u * buf; };
     auto computed = [&](int buf) { return bar_addr + 8u * (kCregMaxBufs + buf); };
     const uint32_t xbar_addr = smem_u32(s_xbar);
+    auto announced = [&](int buf) { return smem_u32(s_dbar) + 8u * buf; };               // the row's info is there
+    auto ready = [&](int buf) { return smem_u32(s_dbar) + 8u * (kBufsHere + buf); };     // teacher entries taken out
+    auto patched = [&](int buf) { return smem_u32(s_dbar) + 8u * (2 * kBufsHere + buf); };
+    const int Kpad = kDistill ? (dt.K + 31) / 32 * 32 : 0;
+    // teacher entries of a buffer: position in it (or -1), weight, logit
+    auto t_pos = [&](int buf) { return (int*)(zero_buf + kZeroBytesHere + 64) + 3 * buf * Kpad; };
+    auto t_p = [&](int buf) { return (float*)t_pos(buf) + Kpad; };
+    auto t_z = [&](int buf) { return (float*)t_pos(buf) + 2 * Kpad; };
 
     if (tid == 0) {
         for (int b = 0; b < NB; ++b) {
             mbar_init(landed(b), 1);
             mbar_init(computed(b), NW);
+            if (kDistill) {
+                mbar_init(announced(b), 1);
+                mbar_init(ready(b), 1);
+                mbar_init(patched(b), 1);
+            }
         }
         mbar_init(xbar_addr, 1);
         mbar_init(xbar_addr + 8u, 1);
         fence_mbar_init();
     }
     if (kTmem && warp == 0) tmem_alloc(smem_u32(&s_tmem_base), ca.tmem_cols);
-    for (int i = tid; i < kCregZeroBytes / 16; i += kThreads) ((uint4*)zero_buf)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < kZeroBytesHere / 16; i += kThreads) ((uint4*)zero_buf)[i] = make_uint4(0, 0, 0, 0);
     // the vectors of every buffer past the end of the slice: -inf, a term of 0 in every sum
     for (int b = 0; b < NB; ++b)
         for (uint32_t v = nvec + tid; v < ca.buf_stride / 16u; v += kThreads)
@@ -335,8 +408,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                     for (uint32_t o = 0; o < lo; o += 2) *(uint16_t*)(drow + o) = 0;
                     for (uint32_t o = hi; o < ca.row_bytes; o += 2) *(uint16_t*)(drow + o) = 0;
                 }
-                for (uint32_t off = lo; off < hi; off += kCregZeroBytes)
-                    bulk_store(drow + off, smem_u32(zero_buf), min((uint32_t)kCregZeroBytes, hi - off));
+                for (uint32_t off = lo; off < hi; off += kZeroBytesHere)
+                    bulk_store(drow + off, smem_u32(zero_buf), min((uint32_t)kZeroBytesHere, hi - off));
                 bulk_commit();
             };
             auto zero_fill_next = [&]() {
@@ -348,7 +421,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
             // engine and waits until it has been read out of shared memory.
             auto drain = [&](int i) {
                 const int buf = i % NB;
-                mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+                mbar_wait(kDistill ? patched(buf) : computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
                 if (aborted) return;
                 const uint32_t srcb = buf_addr + (uint32_t)buf * ca.buf_stride;
                 unsigned char* drow = (unsigned char*)(p.dlogits + s_row[buf].dl_offset) + slice_off;
@@ -397,8 +470,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 }
                 if (a.ok) {
                     const long long f = (long long)a.b * p.T + a.t;
-                    a.y = __ldg(p.ids + (long long)a.b * p.ids_stride_b + a.t);
-                    a.sc = load_row_scalars(p, a.b, a.t, f);
+                    a.y = kDistill ? 0 : __ldg(p.ids + (long long)a.b * p.ids_stride_b + a.t);
+                    if (!kDistill) a.sc = load_row_scalars(p, a.b, a.t, f);
                 }
                 return a;
             };
@@ -415,7 +488,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 ri.dl_offset = (long long)a.b * p.dl_stride_b + (long long)a.t * p.dl_stride_t;
                 ri.bad_id = (a.y < 0 || a.y >= p.V) ? 1 : 0;
                 ri.y = ri.bad_id ? 0 : (int)a.y;
-                ri.sc = a.sc;
+                if (!kDistill) ri.sc = a.sc;
+                ri.entries = kDistill ? (long long)a.b * dt.stride_b + (long long)a.t * dt.stride_t : 0;
                 ri.mis = kAny ? (unsigned)((uintptr_t)row & 15u) : 0u;
                 ri.pad = 0;
                 if (ri.bad_id && crank == 0) atomicOr(p.status, kErrIdRange);
@@ -423,6 +497,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 if (i >= NB) drain(i - NB);                              // the buffer's previous slice goes out first
                 if (aborted) break;
                 s_row[buf] = ri;
+                if (kDistill) mbar_arrive(announced(buf));
                 const uint32_t dst = buf_addr + (uint32_t)buf * ca.buf_stride;
                 // kAny: the aligned span around the row (it stays inside the 16-byte blocks that hold the row's ends)
                 const uint32_t load_bytes = kAny ? ((ri.mis + ca.row_bytes + 15u) & ~15u) : slice_bytes;
@@ -441,6 +516,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 if (i >= NB) drain(i - NB);
                 if (!aborted) {
                     s_row[buf].flat = -1;
+                    if (kDistill) mbar_arrive(announced(buf));
                     mbar_arrive_expect_tx(landed(buf), 0);
                 }
             }
@@ -448,6 +524,197 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
             bulk_wait_all();
             if (kCluster > 1) cluster_sync_unaligned();                 // no block leaves while a peer may still write to it
         }
+        return;
+    }
+
+    if (kDistill && warp == NW + 1) {
+        // ------------------------------------------------------------ target warp
+        constexpr int kPer = kDistillMax / 32;                       // entries per lane
+        for (int i = 0; !aborted; ++i) {
+            const int buf = i % NB;
+            mbar_wait(announced(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+            if (aborted) break;
+            const long long entries = s_row[buf].entries;
+            const uint32_t eoff = kAny ? (s_row[buf].mis >> 1) : 0u;
+            if (s_row[buf].flat < 0) {
+                if (lane == 0) mbar_arrive(ready(buf));
+                break;
+            }
+            // the entries' weights
+            int pos[kPer];
+            float pk[kPer], lt[kPer];
+            bool bad = false;
+            float lmax = kFloorM;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int k = lane + 32 * j;
+                pos[j] = -1;
+                lt[j] = __uint_as_float(0xff800000u);
+                if (k < dt.K) {
+                    pos[j] = __ldg(dt.ids + entries + k);
+                    lt[j] = __ldg(dt.logprobs + entries + k);
+                    bad |= pos[j] < -1 || pos[j] >= p.V;
+                    if (pos[j] < 0 || pos[j] >= p.V) { pos[j] = -1; lt[j] = __uint_as_float(0xff800000u); }
+                    lmax = fmaxf(lmax, lt[j]);
+                }
+            }
+            if (__any_sync(0xffffffffu, bad) && lane == 0 && crank == 0) atomicOr(p.status, kErrIdRange);
+            double P = 0.0;
+            if (dt.mode == kDistillNormalised) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) lmax = fmaxf(lmax, __shfl_xor_sync(0xffffffffu, lmax, o));
+            }
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                pk[j] = 0.f;
+                if (32 * j >= dt.K) continue;
+                // tail: 1 - sum p is what the mass outside is worth, so the sum is formed of terms in double precision
+                if (dt.mode == kDistillTail) { const double e = exp((double)lt[j]); P += e; pk[j] = (float)e; }
+                else { pk[j] = expf(dt.mode == kDistillNormalised ? lt[j] - lmax : lt[j]); P += (double)pk[j]; }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) P += __shfl_xor_sync(0xffffffffu, P, o);
+            if (dt.mode == kDistillNormalised) {
+                const float inv = P > 0.0 ? (float)(1.0 / P) : (P == P ? 0.f : (float)P), lse = lmax + (float)log(P);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) { pk[j] *= inv; lt[j] -= lse; }
+                P = P > 0.0 ? 1.0 : (P == P ? 0.0 : P);
+            }
+            double H = 0.0;
+            float pr[kCluster];
+#pragma unroll
+            for (int c = 0; c < kCluster; ++c) pr[c] = 0.f;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                if (!(pk[j] == 0.f)) H += (double)pk[j] * (double)lt[j];
+                const uint32_t v = pos[j] < 0 ? 0xffffffffu : (eoff + (uint32_t)pos[j]) >> 3;
+#pragma unroll
+                for (int c = 0; c < kCluster; ++c)
+                    if (v - (uint32_t)c * ca.slice_vecs < ca.slice_vecs) pr[c] += pk[j];
+                // position in this block's buffer, or -1
+                pos[j] = v - v0 < nvec ? (int)(eoff + (uint32_t)pos[j] - v0 * 8u) : -1;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                H += __shfl_xor_sync(0xffffffffu, H, o);
+#pragma unroll
+                for (int c = 0; c < kCluster; ++c) pr[c] += __shfl_xor_sync(0xffffffffu, pr[c], o);
+            }
+            // the logits leave the buffer.  Every entry leaves its number in its place and looks whether it is still
+            // there: if not, the same entry is named twice.
+            mbar_wait(landed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+            if (aborted) break;
+            uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
+            int* tp = t_pos(buf);
+            float *tw = t_p(buf), *tz = t_z(buf);
+            float z[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) z[j] = pos[j] >= 0 ? El<kF16>::widen(row16[pos[j]]) : 0.f;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (pos[j] >= 0) row16[pos[j]] = (uint16_t)(lane + 32 * j);
+            __syncwarp();
+            bool twice = false;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) twice |= pos[j] >= 0 && row16[pos[j]] != (uint16_t)(lane + 32 * j);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                if (pos[j] >= 0) row16[pos[j]] = (uint16_t)El<kF16>::kNegInf;
+                if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; tz[lane + 32 * j] = z[j]; }
+            }
+            if (__any_sync(0xffffffffu, twice)) {
+                // the first of several equal entries takes the weight of all, added in the order of the list
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    const int k = lane + 32 * j, mine = pos[j];
+                    if (mine < 0) continue;
+                    for (int o = 0; o < k; ++o)
+                        if (tp[o] == mine) { pos[j] = -1; break; }
+                    if (pos[j] < 0) { pk[j] = 0.f; continue; }
+                    for (int o = k + 1; o < dt.K; ++o)
+                        if (tp[o] == mine) pk[j] += tw[o];
+                }
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; }
+            }
+            float Mt = kFloorM;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (pos[j] >= 0) Mt = fmaxf(Mt, z[j] * xscale);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) Mt = fmaxf(Mt, __shfl_xor_sync(0xffffffffu, Mt, o));
+            float ey = 0.f, zy = 0.f;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (pos[j] >= 0) {
+                    const float x = fmaf(z[j], xscale, -Mt);
+                    ey += ex2(x);
+                    if (!(pk[j] == 0.f)) zy = fmaf(pk[j], x, zy);
+                }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                ey += __shfl_xor_sync(0xffffffffu, ey, o);
+                zy += __shfl_xor_sync(0xffffffffu, zy, o);
+            }
+            if (lane == 0) {
+                TargetInfo ti;
+                ti.H = H;
+                ti.P = (float)P;
+                ti.p0 = dt.mode == kDistillTail ? (float)(1.0 - P > 0.0 ? 1.0 - P : 0.0) : 0.f;
+                ti.W = dt.mode == kDistillTail ? (float)(P > 1.0 ? P : 1.0) : (float)P;
+                if (!(P == P)) ti.W = ti.P;
+                for (int c = 0; c < 4; ++c) ti.pr[c] = c < kCluster ? pr[c < kCluster ? c : 0] : 0.f;
+                s_target[buf] = ti;
+                s_tlab[buf] = LabelInfo{zy, ey, Mt, s_target[buf].pr[crank]};
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ready(buf));
+        }
+        return;
+    }
+
+    if (kDistill && warp == NW + 2) {
+        // ------------------------------------------------------------ patch warp
+        const float row_scale = N > 0 ? p.grad_scale * dt.tau / (float)N : 0.f;
+        for (int i = 0; !aborted; ++i) {
+            const int buf = i % NB;
+            mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+            if (aborted) break;
+            const long long flat = s_row[buf].flat;
+            if (flat < 0) break;
+            const float4 tot = s_total[buf];                         // M, mass outside, mass of the entries, sum p (x - M)
+            const TargetInfo ti = s_target[buf];
+            const float l2 = log2f(tot.y + tot.z);
+            uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
+            const int* tp = t_pos(buf);
+            const float *tw = t_p(buf), *tz = t_z(buf);
+            for (int k = lane; k < dt.K; k += 32) {
+                const int at = tp[k];
+                if (at < 0) continue;
+                const float q = ex2(fmaf(tz[k], xscale, -tot.x) - l2);
+                row16[at] = (uint16_t)(El<kF16>::pack2(row_scale * fmaf(ti.W, q, -tw[k]), 0.f) & 0xffffu);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(patched(buf));
+                if (crank == 0) {
+                    const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot.w, tot.y, tot.z));
+                    p.row_loss[flat] = L;
+                    if (p.out_lp_new) p.out_lp_new[flat] = L;
+                }
+            }
+        }
+        __threadfence();
+        asm volatile("bar.sync 2, %0;" ::"n"(kCons + 32) : "memory");   // the row losses are written
         return;
     }
 
@@ -469,10 +736,14 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
         const int buf = i % NB, par = i & 1;
         const uint32_t use = (uint32_t)(i >> 1) & 1u;                // of the exchange barrier, which alternates by row
         mbar_wait(landed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+        if (kDistill) mbar_wait(ready(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
         aborted = __any_sync(0xffffffffu, aborted);                 // a warp gives up as a whole
         RowInfo ri = s_row[buf];
         if (aborted) { ri.y = 0; ri.bad_id = 1; ri.flat = 0; }      // stale row info: touch nothing
-        if (ri.flat < 0) break;                                      // the producer has no more rows (the same for every thread)
+        if (ri.flat < 0) {                                           // the producer has no more rows (the same for every thread)
+            if (kDistill && lane == 0) mbar_arrive(computed(buf));   // tells the patch warp
+            break;
+        }
         unsigned char* rowbuf = smem + (size_t)buf * ca.buf_stride;
         const uint4* src = (const uint4*)rowbuf + tid;
 
@@ -491,7 +762,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
         // where the generated token sits: vector ylocal of this slice (if < nvec), entry yj
         const uint32_t ylocal = ((eoff + (uint32_t)ri.y) >> 3) - v0;
         const int yj = (int)((eoff + (uint32_t)ri.y) & 7u);
-        const bool label_here = ylocal < nvec;
+        const bool label_here = !kDistill && ylocal < nvec;
         const bool owner = label_here && (ylocal % kCons) == (uint32_t)tid;
         const int jy = owner ? (int)(ylocal / kCons) : -1;
 
@@ -502,7 +773,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
             uint4 q0 = *(const uint4*)rowbuf;
             if (kAny) q0 = mask_vec_outside<kF16>(q0, (int)eoff, 8);
             if (label_here && ylocal == 0) q0 = mask_vec_entry<kF16>(q0, yj);
-            Mref = max8_scaled<kF16>(q0);
+            Mref = max8_scaled<kF16>(q0, xscale);
         }
         // The owner takes the generated token's logit out of the row (it becomes -inf, a term of 0), so that
         // the sums below are sums over the other entries and 1 - p_y comes without cancellation.
@@ -526,7 +797,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
-                        const float2 x = __ffma2_rn(El<kF16>::unpack2(w[h]), splat2(kLog2e), splat2(negM));
+                        const float2 x = __ffma2_rn(El<kF16>::unpack2(w[h]), splat2(xscale), splat2(negM));
                         e[j][h] = make_float2(ex2(x.x), ex2(x.y));
                     }
                     acc0 = __fadd2_rn(acc0, e[j][0]);
@@ -545,7 +816,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 float2 et[4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const float2 x = __ffma2_rn(El<kF16>::unpack2(w[h]), splat2(kLog2e), splat2(negM));
+                    const float2 x = __ffma2_rn(El<kF16>::unpack2(w[h]), splat2(xscale), splat2(negM));
                     et[h] = make_float2(ex2(x.x), ex2(x.y));
                 }
                 tmem_store8(tmem_addr + (uint32_t)j * 8u, et);
@@ -568,14 +839,14 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
             if (redo) {
                 // a reference of this thread's own: its largest scaled entry
                 float m = xy;
-                for (int j = 0; j < nj; ++j) m = fmaxf(m, max8_scaled<kF16>(src[(size_t)j * kCons]));
+                for (int j = 0; j < nj; ++j) m = fmaxf(m, max8_scaled<kF16>(src[(size_t)j * kCons], xscale));
                 M = m;
             }
         }
         if (cnt == 0 && !owner) { M = Mref; vs = 0.f; }
         const bool diverged = M != Mref;
 
-        if (label_here ? owner : tid == 0)
+        if (!kDistill && (label_here ? owner : tid == 0))
             s_lab[par] = label_here ? LabelInfo{zy, ex2(fmaf(zy, kLog2e, -M)), M, 0.f} : LabelInfo{0.f, 0.f, kFloorM, 0.f};
         float ws = vs;
 #pragma unroll
@@ -585,13 +856,21 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
         if (!consumer_barrier_or<NW>(diverged || aborted)) {
             tot.M = Mref;
             tot.s = sum_warp_sums<NW>(s_sum[par]);
-            tot.ey = s_lab[par].ey;
+            if (kDistill) {
+                const LabelInfo li = s_tlab[buf];
+                tot.M = fmaxf(Mref, li.M);
+                tot.s *= ex2(Mref - tot.M);
+                tot.ey = li.ey * ex2(li.M - tot.M);
+            } else {
+                tot.ey = s_lab[par].ey;
+            }
         } else {
             // a wait that ran out somewhere in the block ends the block's work here, for all its threads alike
             if (consumer_barrier_or<NW>(aborted)) { aborted = true; break; }
-            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], &s_lab[par], warp, lane);
+            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], kDistill ? &s_tlab[buf] : &s_lab[par], warp, lane);
         }
-        float zy_row = s_lab[par].zy;
+        // the generated token's logit; kDistill: sum over the slice's teacher entries of p (x - M), M the total's reference
+        float zy_row = kDistill ? fmaf(s_tlab[buf].pad, s_tlab[buf].M - tot.M, s_tlab[buf].zy) : s_lab[par].zy;
 
         if (kCluster > 1) {
             // every block of the cluster sends its slice's (M, s, ey, zy) to every block, itself included
@@ -616,7 +895,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
                 const float sc = ex2(part.x - Mx);
                 sx = fmaf(part.y, sc, sx);
                 eyx = fmaf(part.z, sc, eyx);
-                zx += part.w;
+                zx += kDistill ? fmaf(s_target[buf].pr[r], part.x - Mx, part.w) : part.w;
             }
             tot = Acc{Mx, sx, eyx};
             zy_row = zx;
@@ -624,8 +903,13 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
         RowResult r = row_finish_fast(tot, zy_row);
 
         float loss = 0.f, kl = 0.f, g = 0.f;
-        if (!ri.bad_id) row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
-        if (tid == 0 && crank == 0 && !aborted) {
+        if (kDistill) {
+            g = -(scale_over_N * dt.tau) * distill_factor(s_target[buf], tot.s, r.one_m_py);
+            if (tid == 0) s_total[buf] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+        } else if (!ri.bad_id) {
+            row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
+        }
+        if (!kDistill && tid == 0 && crank == 0 && !aborted) {
             if (p.row_loss) p.row_loss[ri.flat] = loss;
             if (p.row_kl) p.row_kl[ri.flat] = kl;
             if (p.out_lp_new) p.out_lp_new[ri.flat] = ri.bad_id ? 0.f : r.lp;
@@ -668,6 +952,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_creg_kernel(CregArgs ca)
     // The two losses.  Every block leaves its share of the value loss in the workspace; the block that finishes last
     // adds the per-token policy terms (and KL terms, where the objective has them) of the whole batch (all its consumer
     // threads, fixed shares, fixed tree) and the blocks' value-loss shares in block order.
+    if (kDistill) asm volatile("bar.sync 2, %0;" ::"n"(kCons + 32) : "memory");   // the patch warp has written the row losses
     if (p.fused) {
         if (tid == 0) {
             p.partials[2 * blockIdx.x] = 0.0;

@@ -50,7 +50,7 @@ struct RowArgs {
 };
 
 // ---------------------------------------------------------------- objectives of a row with one generated token
-constexpr int kObjPpo = 0, kObjPolicyKl = 1, kObjPreference = 2;
+constexpr int kObjPpo = 0, kObjPolicyKl = 1, kObjPreference = 2, kObjDistill = 3;
 
 // What a row's objective needs beside its log-prob; loaded ahead of the row.
 struct RowScalars {

@@ -336,12 +336,12 @@ __device__ __forceinline__ float exp_sum_vecs(const uint4 (&q)[U], float negM)
 }
 
 template <bool kF16 = false>
-__device__ __forceinline__ float max8_scaled(const uint4& q)
+__device__ __forceinline__ float max8_scaled(const uint4& q, float scale = kLog2e)
 {
     float z[8];
     unpack8<kF16>(q, z);
     float m = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-    return fmaxf(m * kLog2e, kFloorM);
+    return fmaxf(m * scale, kFloorM);
 }
 
 // Dynamic shared memory: [n_slots * chunk][full barriers n_slots * 8][empty barriers n_slots * 8][zero buffer].

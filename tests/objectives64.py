@@ -98,3 +98,41 @@ def topk(z, lengths, K, temperature):
     pad = ~valid_mask(lengths, T)
     ids[pad], lp[pad] = 0, 0.0
     return ids, lp
+
+
+def distill(z, topk_ids, topk_logprobs, lengths, mode, temperature, grad_scale):
+    """loss, row losses, dlogits and, entry by entry, the absolute parts of the gradient."""
+    B, T, V = z.shape
+    valid = valid_mask(lengths, T)
+    ids = topk_ids.long()
+    used = (ids >= 0) & (ids < V)
+    at = torch.where(used, ids, 0)
+    lt = torch.where(used, topk_logprobs.double(), float("-inf"))
+    if mode == 1:
+        norm = torch.logsumexp(lt, dim=2, keepdim=True)
+        lt = torch.where(torch.isinf(norm), float("-inf"), lt - norm)
+    p = torch.exp(lt)
+    lq = torch.log_softmax(z / temperature, dim=2)
+    named = torch.zeros_like(lq).scatter_add_(2, at, used.double()) > 0
+    target = torch.zeros_like(lq).scatter_add_(2, at, p)
+    P = p.sum(dim=2, keepdim=True)
+    L = torch.where(p > 0, p * (lt - lq.gather(2, at)), 0.0).sum(dim=2)
+    q = lq.exp()
+    W, out = P, P
+    if mode == 2:
+        p0 = (1 - P).clamp(min=0)
+        l0 = torch.logsumexp(lq.masked_fill(named, float("-inf")), dim=2, keepdim=True)
+        there = (p0 > 0) & (l0 > float("-inf"))
+        L = L + torch.where(there, p0 * (torch.log(p0) - l0), 0.0)[..., 0]
+        W = P + p0
+        out = torch.where(there, W - p0 * torch.exp(-l0), P)
+        size = torch.where(there, W + p0 * torch.exp(-l0), P)
+    else:
+        size = P
+    N = valid.sum().clamp(min=1)
+    k = grad_scale * temperature / N
+    d = k * (torch.where(named, W, out) * q - target)
+    parts = abs(k) * (torch.where(named, W, size) * q + target)
+    d = torch.where(valid[..., None], d, 0.0)
+    rows = torch.where(valid, temperature ** 2 * L, 0.0)
+    return rows.sum() / N, rows, d, torch.where(valid[..., None], parts, 0.0)

@@ -47,3 +47,16 @@ def test_preference_gradient(kind, smoothing, length_mean):
     f = lambda x: ref.preference(x, ids, lengths, lp_ref, kind, 0.7, 0.2, smoothing, length_mean, 1.0)  # noqa: E731
     want = _differences(lambda x: f(x)[0], z, lengths)
     assert (f(z)[2] - want).abs().max() < 1e-8
+
+
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("temperature", [1.0, 2.5])
+def test_distill_gradient(mode, temperature):
+    g, z, _, lengths, _, r = _batch(3)
+    teacher = torch.log_softmax((z + r(4, 5, 11)) / temperature, dim=2)
+    lt, ids = teacher.topk(4, dim=2)
+    ids[0, 0, 2] = -1                                    # unused
+    ids[0, 1, 3] = ids[0, 1, 1]                          # named twice
+    f = lambda x: ref.distill(x, ids, lt, lengths, mode, temperature, 1.0)  # noqa: E731
+    want = _differences(lambda x: f(x)[0], z, lengths)
+    assert (f(z)[2] - want).abs().max() < 1e-8

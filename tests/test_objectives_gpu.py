@@ -323,3 +323,151 @@ def test_topk_lengths_out_of_range_and_non_finite_logits():
     assert torch.equal(got.ids.long()[clean], ids[clean])
     assert torch.isnan(got.logprobs[0, :2]).any()
     assert lib.poll_status(ws) == 0
+
+
+# ---------------------------------------------------------------- distillation
+def teacher_entries(z, K, temperature, gen, noise=1.0):
+    t = (z.float() + noise * torch.randn(z.shape, generator=gen, device=DEV)) / temperature
+    k = min(K, z.shape[2])
+    top, at = t.topk(k, dim=2)
+    top = top - torch.logsumexp(t, dim=2, keepdim=True)
+    ids = torch.full(z.shape[:2] + (K,), -1, dtype=torch.int32, device=DEV)
+    lt = torch.zeros(z.shape[:2] + (K,), device=DEV)
+    ids[..., :k] = torch.where(top > float("-inf"), at, -1).int()
+    lt[..., :k] = top
+    return ids, lt
+
+
+def check_distill(z, ids, lt, lengths, mode, temperature, scale, out=None, z64=None):
+    B, T, V = z.shape
+    z64 = z.double() if z64 is None else z64
+    ws = lib.workspace(B, T, DEV)
+    got = lib.distill_loss_fwd_bwd(z, ids, lt, lengths, mode, temperature, scale, ws, out)
+    loss, rows, d, parts = ref.distill(z64, ids, lt, lengths, mode, temperature, scale)
+    # a row's loss is a sum of p (log p - log q) with sum p <= 1 (+ p_0 of the same kind): every log is off by LP at most,
+    # and the weights' relative errors (2^-22) meet logs below 64
+    each = temperature ** 2 * (2 * LP + 2 ** -22 * 64)
+    if got.row_loss is not None:
+        off = (got.row_loss.double() - rows).abs()
+        assert (off <= each + 2 ** -23 * rows.abs()).all(), off.max().item()
+    assert abs(got.loss.item() - loss.item()) <= each + 2 ** -23 * abs(loss.item())
+    check_gradient(got.dlogits, d, parts)
+    return got, ws
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("B,T,V", [s for s in SIZES if s[2] > 1])
+def test_distill_sizes(B, T, V, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(V + T)
+    z, _ = ref.row_logits(B, T, V, dtype, gen, DEV)
+    lengths = mixed_lengths(B, T)
+    for mode, K, temperature in ((0, 1, 1.0), (1, 50, 2.0), (2, 256, 1.0), (2, 33, 1.5)):
+        ids, lt = teacher_entries(z, K, temperature, gen)
+        got, ws = check_distill(z, ids, lt, lengths, mode, temperature, 1000.0)
+        assert lib.poll_status(ws) == 0
+        pads = ~ref.valid_mask(lengths, T)
+        assert (got.dlogits[pads] == 0).all() and (got.row_loss[pads] == 0).all()
+
+
+@pytest.mark.parametrize("mode", [lib.DISTILL_PLAIN, lib.DISTILL_NORMALISED, lib.DISTILL_TAIL])
+@pytest.mark.parametrize("layout", ["prompt", "pitch", "in_place", "other_offset", "strided_entries", "no_rows"])
+@pytest.mark.parametrize("V", [1001, 20008])
+def test_distill_layouts(layout, mode, V):
+    gen = torch.Generator(device=DEV).manual_seed(41)
+    B, T, K = 5, 6, 20
+    kw = {"prompt": dict(prompt=3), "pitch": dict(pitch=5), "in_place": dict(prompt=2, offset=1, pitch=3)}
+    z, store = ref.row_logits(B, T, V, BF, gen, DEV, **kw.get(layout, {}))
+    lengths = mixed_lengths(B, T)
+    ids, lt = teacher_entries(z, K, 1.0, gen)
+    before, z64 = store.clone(), z.double()
+    out = lib.DistillOutputs(z, in_place=layout == "in_place", want_row_loss=layout != "no_rows")
+    if layout == "other_offset":
+        out.dlogits = torch.full((B * T * V + 3,), 7.0, dtype=BF, device=DEV)[3:].view(B, T, V)
+    if layout == "strided_entries":
+        wide_i, wide_l = torch.zeros((T, B, K + 9), dtype=torch.int32, device=DEV), torch.zeros((T, B, K + 9), device=DEV)
+        wide_i[..., 3:3 + K], wide_l[..., 3:3 + K] = ids.transpose(0, 1), lt.transpose(0, 1)
+        ids, lt = wide_i[..., 3:3 + K].transpose(0, 1), wide_l[..., 3:3 + K].transpose(0, 1)
+    check_distill(z, ids, lt, lengths, mode, 1.0, 100.0, out, z64)
+    if layout == "in_place":
+        keep = torch.ones_like(store, dtype=torch.bool)
+        keep.as_strided(z.shape, z.stride(), z.storage_offset())[...] = False
+        assert torch.equal(store.view(torch.int16)[keep], before.view(torch.int16)[keep])
+
+
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("V", [1000, 20000, 50257, 128256])
+def test_distill_entries_that_are_unused_out_of_range_or_repeated(V, mode):
+    gen = torch.Generator(device=DEV).manual_seed(42)
+    B, T, K = 3, 4, 70
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    ids, lt = teacher_entries(z, K, 1.0, gen)
+    lt = lt - 0.5
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    ids[0, 0] = -1                                       # a token without entries
+    ids[0, 1, 1:] = -1
+    ids[0, 2, 40:] = ids[0, 2, :30]                      # the same index twice
+    ids[0, 3, 1::2] = ids[0, 3, 0]                       # the same index many times
+    lt[0, 3] = -5.0
+    lt[1, 0, 10:] = float("-inf")                        # entries of no weight
+    z[1, 1, ids[1, 1, 5].long()] = float("-inf")         # deleted by the student, no weight in the teacher
+    lt[1, 1, 5] = float("-inf")
+    z[1, 2, :V // 2] = float("-inf")
+    ids[1, 2], lt[1, 2] = torch.arange(V - K, V, device=DEV).int(), -5.0
+    ids[2, 0] = torch.arange(K, device=DEV).int()        # neighbours, the row's first vectors
+    lt[2, 0] = -4.5
+    runs = [check_distill(z, ids, lt, lengths, mode, 1.0, 1.0) for _ in range(2)]
+    assert lib.poll_status(runs[0][1]) == 0
+    assert torch.equal(runs[0][0].dlogits, runs[1][0].dlogits) and torch.equal(runs[0][0].row_loss, runs[1][0].row_loss)
+    ids[2, 1, 3], ids[2, 1, 4] = V, -2
+    _, ws = check_distill(z, ids, lt, lengths, mode, 1.0, 1.0)
+    assert lib.poll_status(ws) == 16
+
+
+@pytest.mark.parametrize("mode", [0, 1, 2])
+@pytest.mark.parametrize("V", [1000, 20000, 128256])
+def test_distill_peaked_rows(V, mode):
+    """A student with almost all of its mass on, or off, the teacher's entries: the sums must not be differences."""
+    gen = torch.Generator(device=DEV).manual_seed(43)
+    B, T, K = 2, 4, 16
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV, sigma=0.5)
+    ids, lt = teacher_entries(z, K, 1.0, gen)
+    lt = torch.log_softmax(lt, dim=2) - 0.1
+    for b, t, lift in ((0, 0, 25.0), (0, 1, -40.0), (0, 2, 60.0), (1, 0, 200.0)):
+        z[b, t, ids[b, t].long()] += lift
+    z[1, 1, :8] = 250.0                                  # far above the entries, in the row's first vector
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    if mode == 2:                                        # 200 above: the mass outside leaves the range of fp32
+        lengths[1] = 0
+    got, _ = check_distill(z, ids, lt, lengths, mode, 1.0, 10.0)
+    assert torch.isfinite(got.loss).all()
+
+
+def test_distill_whole_vocabulary_named():
+    """No entry outside the teacher's: the tail term is left out."""
+    gen = torch.Generator(device=DEV).manual_seed(44)
+    B, T, V = 2, 3, 100
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    ids, lt = teacher_entries(z, 120, 1.0, gen)
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    for mode in (0, 1, 2):
+        got, ws = check_distill(z, ids, lt - 0.2, lengths, mode, 1.0, 10.0)
+        assert torch.isfinite(got.loss).all() and lib.poll_status(ws) == 0
+    # the same where a deleted vocabulary leaves nothing else, on the kernel of long rows
+    z, _ = ref.row_logits(B, T, 20000, BF, gen, DEV)
+    ids, lt = teacher_entries(z, 64, 1.0, gen)
+    keep = torch.zeros(z.shape, dtype=torch.bool, device=DEV).scatter_(2, ids.long(), True)
+    z[~keep] = float("-inf")
+    for mode in (0, 1, 2):
+        got, ws = check_distill(z, ids, lt, lengths, mode, 1.0, 10.0)
+        assert torch.isfinite(got.loss).all() and lib.poll_status(ws) == 0
+
+
+def test_distill_without_tokens_and_lengths_out_of_range():
+    gen = torch.Generator(device=DEV).manual_seed(45)
+    for V in (1000, 20000):
+        z, _ = ref.row_logits(3, 4, V, BF, gen, DEV)
+        ids, lt = teacher_entries(z, 8, 1.0, gen)
+        got, ws = check_distill(z, ids, lt, torch.zeros(3, dtype=torch.int32, device=DEV), 2, 1.0, 1.0)
+        assert (got.loss == 0).all() and (got.dlogits == 0).all() and lib.poll_status(ws) == 0
+        _, ws = check_distill(z, ids, lt, torch.tensor([9, -1, 2], dtype=torch.int32, device=DEV), 2, 1.0, 1.0)
+        assert lib.poll_status(ws) == 32
