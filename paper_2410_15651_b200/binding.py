@@ -405,33 +405,80 @@ def ppo_loss_fwd_bwd_noalloc(logits: torch.Tensor, ids: torch.Tensor, lengths: t
 
 
 # ---------------------------------------------------------------- objectives beside the PPO step
-def _together(logits: torch.Tensor, *named) -> None:
-    """Every tensor of a call lives on the device of the logits, and the call is made with that device current."""
-    for name, t in named:
-        if t is not None and t.device != logits.device:
-            raise ValueError(f"{name} is on {t.device}, the logits on {logits.device}")
+# On small batches a call costs the host more than the device, so these wrappers look at each argument in one
+# expression and say what is wrong only where something is.
+_F32 = torch.float32
 
 
-def _ws(ws: torch.Tensor) -> Tuple[int, int]:
+def _rows(t: torch.Tensor) -> Tuple[int, int, int, int, int, int]:
+    """(B, T, V, stride_b, stride_t, device index) of a logits tensor."""
+    if t.dtype not in DTYPES or not t.is_cuda or t.dim() != 3:
+        _logits(t, "logits")
+    B, T, V = t.shape
+    sb, st, sv = t.stride()
+    if sv != 1 and V > 1:
+        _logits(t, "logits")
+    return B, T, V, sb, st, t.get_device()
+
+
+def _arg(t: torch.Tensor, shape: Tuple[int, ...], dtype, dev: int, what: str) -> int:
+    """Address of a contiguous tensor of this shape and type on the device of the logits."""
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, dtype, what)
+    _same_device(t, dev, what)
+    raise ValueError(f"{what} must be a contiguous {list(shape)} tensor")
+
+
+def _opt(t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype, dev: int, what: str) -> Optional[int]:
+    return None if t is None else _arg(t, shape, dtype, dev, what)
+
+
+def _same_device(t: torch.Tensor, dev: int, what: str) -> None:
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, the logits on cuda:{dev}")
+
+
+def _ids_arg(t: torch.Tensor, B: int, T: int, dev: int) -> Tuple[int, int]:
+    """(address, stride between sequences) of the generated tokens."""
+    stride = _ids(t, B, T)
+    _same_device(t, dev, "ids")
+    return t.data_ptr(), stride
+
+
+def _ws(ws: torch.Tensor, dev: int) -> Tuple[int, int]:
     if not ws.is_cuda or not ws.is_contiguous():
         raise ValueError("ws must be a contiguous CUDA tensor (see workspace())")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    _same_device(ws, dev, "ws")
+    return ws.data_ptr(), ws.nbytes
 
 
-def _dlogits(t: torch.Tensor, logits: torch.Tensor) -> Tuple[int, int]:
-    """Strides of the gradient tensor, which has the shape and type of the logits."""
-    if t.dtype != logits.dtype:
+def _dlogits(t: torch.Tensor, logits: torch.Tensor, dev: int) -> Tuple[int, int, int]:
+    """(address, stride_b, stride_t) of the gradient tensor, which has the shape and type of the logits."""
+    if t.dtype is not logits.dtype:
         raise TypeError("out.dlogits must have the element type of logits")
-    if tuple(t.shape) != tuple(logits.shape):
+    if t.shape != logits.shape:
         raise ValueError("out.dlogits must have the shape of logits")
-    return _logits(t, "out.dlogits")[3:]
+    _same_device(t, dev, "out.dlogits")
+    sb, st, sv = t.stride()
+    if sv != 1 and t.shape[2] > 1:
+        raise ValueError("out.dlogits must have a contiguous vocabulary axis")
+    return t.data_ptr(), sb, st
 
 
-def _vector(t: torch.Tensor, n: int, what: str) -> int:
-    _dev(t, torch.float32, what)
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous tensor of {n} floats")
-    return t.data_ptr()
+def _like(logits: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(logits, memory_format=torch.contiguous_format)
+
+
+def _call(name: str, dev: int, *args) -> None:
+    """Calls the entry point with the device of its tensors current and that device's current stream."""
+    if torch.cuda.current_device() == dev:
+        status = getattr(lib(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = getattr(lib(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if status != 0:
+        raise RlhfError(status, name)
 
 
 TOPK_MAX = 256
@@ -442,26 +489,19 @@ class TopK:
 
     def __init__(self, B: int, T: int, K: int, device):
         self.ids = torch.empty((B, T, K), dtype=torch.int32, device=device)
-        self.logprobs = torch.empty((B, T, K), dtype=torch.float32, device=device)
+        self.logprobs = torch.empty((B, T, K), dtype=_F32, device=device)
 
 
 def topk_logprobs(logits: torch.Tensor, lengths: torch.Tensor, k: int, temperature: float, ws: torch.Tensor,
                   out: Optional[TopK] = None) -> TopK:
     """rlhf_topk_logprobs: the k largest log-probs of every row and their entries (1 <= k <= TOPK_MAX)."""
-    B, T, V, sb, st = _logits(logits, "logits")
-    _lengths(lengths, B)
+    B, T, V, sb, st, dev = _rows(logits)
     if out is None:
         out = TopK(B, T, max(k, 0), logits.device)
-    for name, t, dtype in (("out.ids", out.ids, torch.int32), ("out.logprobs", out.logprobs, torch.float32)):
-        _dev(t, dtype, name)
-        if tuple(t.shape) != (B, T, k) or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous [{B},{T},{k}] tensor")
-    _together(logits, ("lengths", lengths), ("ws", ws), ("out.ids", out.ids), ("out.logprobs", out.logprobs))
-    wp, wn = _ws(ws)
-    with torch.cuda.device(logits.device):
-        _check(lib().rlhf_topk_logprobs(logits.data_ptr(), DTYPES[logits.dtype], sb, st, lengths.data_ptr(), B, T, V, k,
-                                        temperature, out.ids.data_ptr(), out.logprobs.data_ptr(), wp, wn,
-                                        _stream(logits)), "rlhf_topk_logprobs")
+    _call("rlhf_topk_logprobs", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st,
+          _arg(lengths, (B,), torch.int32, dev, "lengths"), B, T, V, k, temperature,
+          _arg(out.ids, (B, T, k), torch.int32, dev, "out.ids"),
+          _arg(out.logprobs, (B, T, k), _F32, dev, "out.logprobs"), *_ws(ws, dev))
     return out
 
 
@@ -469,10 +509,9 @@ class DistillOutputs:
     """Buffers written by distill_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, in_place: bool = False, want_row_loss: bool = True):
-        B, T = logits.shape[0], logits.shape[1]
-        self.loss = torch.empty(1, dtype=torch.float32, device=logits.device)
-        self.dlogits = logits if in_place else torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        self.row_loss = torch.empty((B, T), dtype=torch.float32, device=logits.device) if want_row_loss else None
+        self.loss = logits.new_empty(1, dtype=_F32)
+        self.dlogits = logits if in_place else _like(logits)
+        self.row_loss = logits.new_empty(logits.shape[:2], dtype=_F32) if want_row_loss else None
 
 
 def distill_loss_fwd_bwd(logits: torch.Tensor, topk_ids: torch.Tensor, topk_logprobs: torch.Tensor, lengths: torch.Tensor,
@@ -480,28 +519,23 @@ def distill_loss_fwd_bwd(logits: torch.Tensor, topk_ids: torch.Tensor, topk_logp
                          out: Optional[DistillOutputs] = None) -> DistillOutputs:
     """rlhf_distill_loss_fwd_bwd.  topk_ids (int32) and topk_logprobs (fp32) are [B,T,K] with equal strides and a contiguous
     last axis; `mode` is DISTILL_PLAIN, DISTILL_NORMALISED or DISTILL_TAIL."""
-    B, T, V, sb, st = _logits(logits, "logits")
-    _lengths(lengths, B)
+    B, T, V, sb, st, dev = _rows(logits)
     _dev(topk_ids, torch.int32, "topk_ids")
-    _dev(topk_logprobs, torch.float32, "topk_logprobs")
-    if topk_ids.dim() != 3 or tuple(topk_ids.shape[:2]) != (B, T) or topk_ids.shape != topk_logprobs.shape:
+    _dev(topk_logprobs, _F32, "topk_logprobs")
+    _same_device(topk_ids, dev, "topk_ids")
+    _same_device(topk_logprobs, dev, "topk_logprobs")
+    if topk_ids.dim() != 3 or topk_ids.shape[:2] != (B, T) or topk_ids.shape != topk_logprobs.shape:
         raise ValueError(f"topk_ids and topk_logprobs must be [{B},{T},K]")
     K = topk_ids.shape[2]
-    if topk_ids.stride() != topk_logprobs.stride() or (K > 1 and topk_ids.stride(2) != 1):
+    ksb, kst, ks = topk_ids.stride()
+    if topk_logprobs.stride() != (ksb, kst, ks) or (K > 1 and ks != 1):
         raise ValueError("topk_ids and topk_logprobs must have the same strides and a contiguous last axis")
     if out is None:
         out = DistillOutputs(logits)
-    dsb, dst = _dlogits(out.dlogits, logits)
-    loss = _vector(out.loss, 1, "out.loss")
-    row_ptr = _bt(out.row_loss, B, T, "out.row_loss").data_ptr() if out.row_loss is not None else None
-    _together(logits, ("topk_ids", topk_ids), ("topk_logprobs", topk_logprobs), ("lengths", lengths), ("ws", ws),
-              ("out.loss", out.loss), ("out.dlogits", out.dlogits), ("out.row_loss", out.row_loss))
-    wp, wn = _ws(ws)
-    with torch.cuda.device(logits.device):
-        _check(lib().rlhf_distill_loss_fwd_bwd(
-            logits.data_ptr(), DTYPES[logits.dtype], sb, st, topk_ids.data_ptr(), topk_logprobs.data_ptr(),
-            topk_ids.stride(0), topk_ids.stride(1), K, lengths.data_ptr(), B, T, V, mode, temperature, grad_scale,
-            loss, row_ptr, out.dlogits.data_ptr(), dsb, dst, wp, wn, _stream(logits)), "rlhf_distill_loss_fwd_bwd")
+    _call("rlhf_distill_loss_fwd_bwd", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st,
+          topk_ids.data_ptr(), topk_logprobs.data_ptr(), ksb, kst, K, _arg(lengths, (B,), torch.int32, dev, "lengths"),
+          B, T, V, mode, temperature, grad_scale, _arg(out.loss, (1,), _F32, dev, "out.loss"),
+          _opt(out.row_loss, (B, T), _F32, dev, "out.row_loss"), *_dlogits(out.dlogits, logits, dev), *_ws(ws, dev))
     return out
 
 
@@ -509,10 +543,9 @@ class PolicyKlOutputs:
     """Buffers written by policy_kl_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, in_place: bool = False, want_lp_new: bool = True):
-        B, T = logits.shape[0], logits.shape[1]
-        self.loss = torch.empty(2, dtype=torch.float32, device=logits.device)      # [loss_pg, loss_kl]
-        self.dlogits = logits if in_place else torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        self.lp_new = torch.empty((B, T), dtype=torch.float32, device=logits.device) if want_lp_new else None
+        self.loss = logits.new_empty(2, dtype=_F32)                                  # [loss_pg, loss_kl]
+        self.dlogits = logits if in_place else _like(logits)
+        self.lp_new = logits.new_empty(logits.shape[:2], dtype=_F32) if want_lp_new else None
 
 
 def policy_kl_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor, lp_old: torch.Tensor,
@@ -521,32 +554,23 @@ def policy_kl_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: tor
                            out: Optional[PolicyKlOutputs] = None) -> PolicyKlOutputs:
     """rlhf_policy_kl_loss_fwd_bwd.  `adv` is [B,T] (any strides) or [B], one advantage per sequence; `reduction` is
     MEAN_TOKENS or MEAN_SEQUENCES."""
-    B, T, V, sb, st = _logits(logits, "logits")
-    isb = _ids(ids, B, T)
-    _lengths(lengths, B)
-    _bt(lp_old, B, T, "lp_old")
-    ref_ptr = _bt(lp_ref, B, T, "lp_ref").data_ptr() if lp_ref is not None else None
-    _dev(adv, torch.float32, "adv")
-    if tuple(adv.shape) == (B, T):
+    B, T, V, sb, st, dev = _rows(logits)
+    _dev(adv, _F32, "adv")
+    _same_device(adv, dev, "adv")
+    if adv.shape == (B, T):
         asb, ast = adv.stride()
-    elif tuple(adv.shape) == (B,):
+    elif adv.shape == (B,):
         asb, ast = adv.stride(0), 0
     else:
         raise ValueError(f"adv must be [{B},{T}] or [{B}]")
     if out is None:
         out = PolicyKlOutputs(logits)
-    dsb, dst = _dlogits(out.dlogits, logits)
-    loss = _vector(out.loss, 2, "out.loss")
-    lp_new_ptr = _bt(out.lp_new, B, T, "out.lp_new").data_ptr() if out.lp_new is not None else None
-    _together(logits, ("ids", ids), ("lengths", lengths), ("lp_old", lp_old), ("lp_ref", lp_ref), ("adv", adv), ("ws", ws),
-              ("out.loss", out.loss), ("out.dlogits", out.dlogits), ("out.lp_new", out.lp_new))
-    wp, wn = _ws(ws)
-    with torch.cuda.device(logits.device):
-        _check(lib().rlhf_policy_kl_loss_fwd_bwd(
-            logits.data_ptr(), DTYPES[logits.dtype], sb, st, ids.data_ptr(), isb, lengths.data_ptr(),
-            lp_old.data_ptr(), ref_ptr, adv.data_ptr(), asb, ast, B, T, V, clip_low, clip_high, kl_coef,
-            reduction, grad_scale, loss, loss + 4, out.dlogits.data_ptr(), dsb, dst, lp_new_ptr,
-            wp, wn, _stream(logits)), "rlhf_policy_kl_loss_fwd_bwd")
+    loss = _arg(out.loss, (2,), _F32, dev, "out.loss")
+    _call("rlhf_policy_kl_loss_fwd_bwd", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st, *_ids_arg(ids, B, T, dev),
+          _arg(lengths, (B,), torch.int32, dev, "lengths"), _arg(lp_old, (B, T), _F32, dev, "lp_old"),
+          _opt(lp_ref, (B, T), _F32, dev, "lp_ref"), adv.data_ptr(), asb, ast, B, T, V, clip_low, clip_high, kl_coef,
+          reduction, grad_scale, loss, loss + 4, *_dlogits(out.dlogits, logits, dev),
+          _opt(out.lp_new, (B, T), _F32, dev, "out.lp_new"), *_ws(ws, dev))
     return out
 
 
@@ -554,11 +578,10 @@ class PreferenceOutputs:
     """Buffers written by preference_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, in_place: bool = False, want_lp_new: bool = True):
-        B, T = logits.shape[0], logits.shape[1]
-        self.loss = torch.empty(1, dtype=torch.float32, device=logits.device)
-        self.rewards = torch.empty(B, dtype=torch.float32, device=logits.device)    # beta * log ratio of every sequence
-        self.dlogits = logits if in_place else torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        self.lp_new = torch.empty((B, T), dtype=torch.float32, device=logits.device) if want_lp_new else None
+        self.loss = logits.new_empty(1, dtype=_F32)
+        self.rewards = logits.new_empty(logits.shape[0], dtype=_F32)                 # beta * log ratio of every sequence
+        self.dlogits = logits if in_place else _like(logits)
+        self.lp_new = logits.new_empty(logits.shape[:2], dtype=_F32) if want_lp_new else None
 
 
 def preference_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor,
@@ -567,22 +590,12 @@ def preference_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: to
                             out: Optional[PreferenceOutputs] = None) -> PreferenceOutputs:
     """rlhf_preference_loss_fwd_bwd: sequences 0..B/2-1 are the chosen, B/2..B-1 the rejected responses; `kind` is
     PREF_SIGMOID, PREF_HINGE or PREF_SQUARED."""
-    B, T, V, sb, st = _logits(logits, "logits")
-    isb = _ids(ids, B, T)
-    _lengths(lengths, B)
-    ref_ptr = _bt(lp_ref, B, T, "lp_ref").data_ptr() if lp_ref is not None else None
+    B, T, V, sb, st, dev = _rows(logits)
     if out is None:
         out = PreferenceOutputs(logits)
-    dsb, dst = _dlogits(out.dlogits, logits)
-    loss = _vector(out.loss, 1, "out.loss")
-    rewards = _vector(out.rewards, B, "out.rewards")
-    lp_new_ptr = _bt(out.lp_new, B, T, "out.lp_new").data_ptr() if out.lp_new is not None else None
-    _together(logits, ("ids", ids), ("lengths", lengths), ("lp_ref", lp_ref), ("ws", ws), ("out.loss", out.loss),
-              ("out.rewards", out.rewards), ("out.dlogits", out.dlogits), ("out.lp_new", out.lp_new))
-    wp, wn = _ws(ws)
-    with torch.cuda.device(logits.device):
-        _check(lib().rlhf_preference_loss_fwd_bwd(
-            logits.data_ptr(), DTYPES[logits.dtype], sb, st, ids.data_ptr(), isb, lengths.data_ptr(), ref_ptr,
-            B, T, V, kind, beta, margin, label_smoothing, int(length_mean), grad_scale, loss, rewards,
-            out.dlogits.data_ptr(), dsb, dst, lp_new_ptr, wp, wn, _stream(logits)), "rlhf_preference_loss_fwd_bwd")
+    _call("rlhf_preference_loss_fwd_bwd", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st, *_ids_arg(ids, B, T, dev),
+          _arg(lengths, (B,), torch.int32, dev, "lengths"), _opt(lp_ref, (B, T), _F32, dev, "lp_ref"), B, T, V, kind, beta,
+          margin, label_smoothing, int(length_mean), grad_scale, _arg(out.loss, (1,), _F32, dev, "out.loss"),
+          _arg(out.rewards, (B,), _F32, dev, "out.rewards"), *_dlogits(out.dlogits, logits, dev),
+          _opt(out.lp_new, (B, T), _F32, dev, "out.lp_new"), *_ws(ws, dev))
     return out

@@ -536,21 +536,26 @@ int launch_distill_rows(RowArgs& a, const DistillArgs& d, bool f16, const Device
 template <int NT, bool kF16>
 int launch_topk_as(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 {
-    if (int e = keep_max_carveout(topk_logprobs_kernel<NT, kF16>)) return e;
-    const long long blocks = (long long)dev.sm_count * std::max(1, 1024 / NT);
-    const int grid = (int)std::min<long long>((long long)ta.B * ta.T, blocks);
-    RLHF_CUDA(launch_kernel(topk_logprobs_kernel<NT, kF16>, grid, NT, 0, s, ta));
-    return launch_check("topk_logprobs_kernel");
+    auto kernel = topk_block_kernel<NT, kF16>;
+    // (no preference for shared memory: what the kernel does not take serves its loads in flight as L1.  With the largest
+    // carve-out V = 128256, K = 128 takes 267 instead of 189 us on 6 x 512 rows.)
+    const int grid = (int)std::min<long long>((long long)ta.B * ta.T, (long long)dev.sm_count * topk_blocks_per_sm(NT));
+    RLHF_CUDA(launch_kernel(kernel, grid, NT, 0, s, ta));
+    return launch_check("topk_block_kernel");
 }
 
-// Threads per row: 256 and four rows per SM, or 1024 where there are no more rows than SMs.
+// Threads per row.  1024 where there are no more rows than SMs and a row keeps them busy (one row of 50272: 13 us against
+// 16 us with 256).  Else by the row's length, measured on 4096 rows: V = 1000, K = 32: 68 us with 64 threads, 104 with 128,
+// 191 with 256; V = 8192, K = 32: 33, 35, 51; V = 32000, K = 64: 118, 78, 86; V = 50272, K = 256 (12 x 256 rows): 325, 158,
+// 166; V = 128256, K = 128: 451, 220, 191.
 template <bool kF16>
 int launch_topk(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 {
     if ((long long)ta.B * ta.T <= dev.sm_count && ta.V > 16384) return launch_topk_as<1024, kF16>(ta, dev, s);
+    if (ta.V <= 8192) return launch_topk_as<64, kF16>(ta, dev, s);
+    if (ta.V <= 65536) return launch_topk_as<128, kF16>(ta, dev, s);
     return launch_topk_as<256, kF16>(ta, dev, s);
 }
-
 
 // Launches the row kernel for an objective with one generated token per row.  Sets a.fused if that kernel also does
 // the finalisation (the losses; value loss and dvalues in step 4); otherwise it leaves per-token terms in a.row_loss

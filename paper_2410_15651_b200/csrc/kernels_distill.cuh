@@ -44,12 +44,6 @@ __device__ __forceinline__ int distill_find(const DistillTable& tab, int id)
     return -1;
 }
 
-__device__ __forceinline__ uint32_t vec_entry(const uint4& q, int i)
-{
-    const uint32_t w = (i >> 1) == 0 ? q.x : ((i >> 1) == 1 ? q.y : ((i >> 1) == 2 ? q.z : q.w));
-    return (i & 1) ? (w >> 16) : (w & 0xffffu);
-}
-
 template <bool kF16>
 __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRowArgs da)
 {

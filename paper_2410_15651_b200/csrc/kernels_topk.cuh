@@ -1,27 +1,31 @@
 // The K largest log-probs of every row of a logits tensor, for rows of any alignment.
 //
-// One block per row, rows dealt from a counter in the workspace.  The row is streamed once: every thread keeps an online
-// partition sum (running maximum and sum, fp32) and the maxima of eight groups of its vectors (vector j of a thread
-// belongs to group j mod 8).  The K-th largest of the 8 * threads group maxima is a lower bound of the K-th largest entry
-// -- K groups hold an entry at least that large -- and, the groups being many, a tight one: with G groups about
-// -G ln(1 - K/G) entries reach it (65 for K = 64, 2048 groups), so that only the groups above it, some K of them, are read
-// again (from L2) to collect the candidates, and the candidates are ranked by counting the larger ones.  Candidates are
-// compared as (value, lower index first), so the result does not depend on the order in which they were collected.
-// Rows with more candidates than the list holds (long runs of equal values, rows sorted against the groups) are selected
-// by bisection over the 16-bit values with repeated reads of the row, ties in index order.
+// A row is streamed once: every thread keeps an online partition sum (running maximum and sum, fp32) and the maxima of
+// groups of the entries that it sees.  The K-th largest of G group maxima is a lower bound of the K-th largest entry -- K
+// groups hold an entry at least that large -- and a tight one: of random entries about -G ln(1 - K/G) reach it (74 for
+// K = 64, G = 256).  Only the groups that reach it are read again, to collect the candidates.  Candidates are compared as
+// (value, lower index first), so the result does not depend on the order in which they were collected.
+//
+// One block per row, several blocks per SM, rows dealt from a counter in the workspace.
 //
 // Exponents are formed as (z - maximum) * log2(e) / temperature: the difference of two 16-bit values is exact or nearly so,
 // whatever their size.
 //
-// Bound: one read of the row from DRAM; per logit one ex2 and half a packed maximum.
+// Floor: one read of the row from DRAM (32 us for 2048 rows of 50272 in bf16 at 6.5 TB/s).  What bounds the kernel is
+// instruction issue: per row of 50272 and K = 64 some 9,000 warp instructions for the stream (one ex2 and half a packed
+// maximum per logit) and 8,000 for the selection, which the warps of a block share.  Measured (12 x 256 rows, 84 us) and dropped: a row per
+// warp (all rows of a batch are then in flight, L2 does not hold them, and what is read again comes from DRAM in sectors:
+// 120 us; with groups of whole lines 78 us, but 178 against 158 us at K = 256 and 226 against 191 us at V = 128256);
+// separate streaming and selecting warps (105 us: one warp selects for 25 us); rows through a ring of bulk copies (88 us).
 #pragma once
 #include "kernels_ring.cuh"
+#include <cuda_fp16.h>
 
 namespace rlhf {
 
 constexpr int kTopkMax = 256;
 constexpr int kTopkGroups = 8;          // per thread
-constexpr int kTopkCandidates = 2048;
+constexpr int kTopkCandidates = 1024;
 constexpr float kTopkFloor = -3.0e38f;  // maximum of a thread that has seen no entry
 
 struct TopkArgs {
@@ -37,6 +41,7 @@ struct TopkArgs {
     unsigned* row_counter;
 };
 
+// ---------------------------------------------------------------- order and candidates
 // Order of the 16-bit values as whole numbers: -0 and +0 equal, NaN above everything with its sign.
 __device__ __forceinline__ uint32_t order_key(uint32_t bits16)
 {
@@ -55,6 +60,7 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
     return r;
 }
 
+// ---------------------------------------------------------------- rows
 // A row as the 16-byte aligned span that holds it.
 struct RowSpan {
     const uint4* vecs;
@@ -81,6 +87,13 @@ __device__ __forceinline__ uint4 load_streaming(const uint4* p)
     return q;
 }
 
+// Entry i of a vector.
+__device__ __forceinline__ uint32_t vec_entry(const uint4& q, int i)
+{
+    const uint32_t w = (i >> 1) == 0 ? q.x : ((i >> 1) == 1 ? q.y : ((i >> 1) == 2 ? q.z : q.w));
+    return (i & 1) ? (w >> 16) : (w & 0xffffu);
+}
+
 // Vector v of the span, entries that are not the row's replaced by -inf.
 template <bool kF16>
 __device__ __forceinline__ uint4 span_vec(const RowSpan& r, uint32_t v)
@@ -91,6 +104,17 @@ __device__ __forceinline__ uint4 span_vec(const RowSpan& r, uint32_t v)
     return q;
 }
 
+// Barrier over the NT threads that work on a row; the second form also counts those with a predicate.
+template <int NT>
+__device__ __forceinline__ void row_sync() { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); }
+template <int NT>
+__device__ __forceinline__ int row_count(bool x)
+{
+    int n;
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.popc.u32 %0, 1, %2, q;\n\t}" : "=r"(n) : "r"((uint32_t)x), "n"(NT) : "memory");
+    return n;
+}
+
 // Sum of one unsigned per thread, for every thread; `scratch` holds two sets of NT/32 words, used alternately.
 template <int NT>
 __device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t* scratch, int& turn)
@@ -98,7 +122,7 @@ __device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t* scratch, int
     uint32_t* s = scratch + (turn ^= 1) * (NT / 32);
     v = __reduce_add_sync(0xffffffffu, v);
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
+    row_sync<NT>();
     uint32_t t = 0;
 #pragma unroll
     for (int w = 0; w < NT / 32; ++w) t += s[w];
@@ -110,20 +134,49 @@ __device__ __forceinline__ unsigned long long candidate(uint32_t key, uint32_t i
     return ((unsigned long long)key << 32) | (0xffffffffu - index);
 }
 
-// Appends the entries of vector v with a key of at least `least`.
+// Two lanes of 16 bits: all ones where a >= b (or a == b), as numbers (never for NaN).
+template <bool kF16, bool kEqual>
+__device__ __forceinline__ uint32_t mask2(uint32_t a, uint32_t b)
+{
+    if (kF16) return kEqual ? __heq2_mask(*(const __half2*)&a, *(const __half2*)&b) : __hge2_mask(*(const __half2*)&a, *(const __half2*)&b);
+    return kEqual ? __heq2_mask(*(const __nv_bfloat162*)&a, *(const __nv_bfloat162*)&b)
+                  : __hge2_mask(*(const __nv_bfloat162*)&a, *(const __nv_bfloat162*)&b);
+}
+
+// Bit e: entry e of the vector has a key of at least (kEqual: equal to) that of the value in both halves of `least2`.
+template <bool kF16, bool kEqual>
+__device__ __forceinline__ uint32_t entries_that_reach(const uint4& q, uint32_t least2)
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t hit = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t m = mask2<kF16, kEqual>(w[k], least2);
+        hit |= (m & (1u << (2 * k))) | ((m >> 16) & (2u << (2 * k)));
+    }
+    return hit;
+}
+__device__ __forceinline__ uint32_t both_halves(uint32_t key) { return key_bits(key) * 0x10001u; }
+
+// Appends the entries of vector v, whose bits are q, with a key of at least `least`.
+template <bool kF16>
+__device__ __forceinline__ void collect_entries(const RowSpan& r, const uint4& q, uint32_t v, uint32_t least, unsigned long long* cand, uint32_t* n_cand)
+{
+    uint32_t hit = entries_that_reach<kF16, false>(q, both_halves(least));
+    if (!hit) return;
+    uint32_t at = atomicAdd(n_cand, (uint32_t)__popc(hit));
+    while (hit) {
+        const int i = __ffs(hit) - 1;
+        hit &= hit - 1;
+        if (at < (uint32_t)kTopkCandidates) cand[at] = candidate(order_key(vec_entry(q, i)), v * 8u + (uint32_t)i - r.eoff);
+        ++at;
+    }
+}
+
 template <bool kF16>
 __device__ __forceinline__ void collect_vec(const RowSpan& r, uint32_t v, uint32_t least, unsigned long long* cand, uint32_t* n_cand)
 {
-    const uint4 q = span_vec<kF16>(r, v);
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t key = order_key((i & 1) ? (w[i >> 1] >> 16) : (w[i >> 1] & 0xffffu));
-        if (key >= least) {
-            const uint32_t at = atomicAdd(n_cand, 1u);
-            if (at < (uint32_t)kTopkCandidates) cand[at] = candidate(key, v * 8u + (uint32_t)i - r.eoff);
-        }
-    }
+    collect_entries<kF16>(r, span_vec<kF16>(r, v), v, least, cand, n_cand);
 }
 
 template <int NT, bool kF16>
@@ -131,10 +184,7 @@ __device__ __forceinline__ uint32_t count_at_least(const RowSpan& r, uint32_t le
 {
     uint32_t n = 0;
     for (uint32_t v = threadIdx.x; v < r.nvec; v += NT) {
-        const uint4 q = span_vec<kF16>(r, v);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) n += order_key((i & 1) ? (w[i >> 1] >> 16) : (w[i >> 1] & 0xffffu)) >= least ? 1u : 0u;
+        n += (uint32_t)__popc(entries_that_reach<kF16, false>(span_vec<kF16>(r, v), both_halves(least)));
     }
     return block_sum<NT>(n, scratch, turn);
 }
@@ -145,29 +195,23 @@ template <int NT, bool kF16>
 __device__ __noinline__ uint32_t topk_bisect(const RowSpan& r, uint32_t K, unsigned long long* cand, uint32_t* n_cand,
                                              uint32_t* scratch, int& turn)
 {
-    uint32_t lo = key_of_neg_inf<kF16>() + 1u, hi = 65536u;
+    uint32_t lo = key_of_neg_inf<kF16>() + 1u, hi = 65536u - key_of_neg_inf<kF16>() + 1u;   // above +inf
     const bool few = count_at_least<NT, kF16>(r, lo, scratch, turn) <= K;
     while (!few && hi - lo > 1u) {
         const uint32_t mid = (lo + hi) >> 1;
         if (count_at_least<NT, kF16>(r, mid, scratch, turn) >= K) lo = mid; else hi = mid;
     }
     if (threadIdx.x == 0) *n_cand = 0;
-    __syncthreads();
+    row_sync<NT>();
     for (uint32_t v = threadIdx.x; v < r.nvec; v += NT) collect_vec<kF16>(r, v, few ? lo : lo + 1u, cand, n_cand);
-    __syncthreads();
+    row_sync<NT>();
     uint32_t n = min(*n_cand, (uint32_t)kTopkCandidates);
     if (few) return n;
     // entries equal to `lo`, in index order
     for (uint32_t v0 = 0; v0 < r.nvec && n < K; v0 += NT) {
         const uint32_t v = v0 + threadIdx.x;
         uint32_t hit = 0;
-        if (v < r.nvec) {
-            const uint4 q = span_vec<kF16>(r, v);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (order_key((i & 1) ? (w[i >> 1] >> 16) : (w[i >> 1] & 0xffffu)) == lo) hit |= 1u << i;
-        }
+        if (v < r.nvec) hit = entries_that_reach<kF16, true>(span_vec<kF16>(r, v), both_halves(lo));
         const uint32_t mine = (uint32_t)__popc(hit);
         uint32_t upto = mine;                                    // inclusive prefix within the warp
 #pragma unroll
@@ -177,7 +221,7 @@ __device__ __noinline__ uint32_t topk_bisect(const RowSpan& r, uint32_t K, unsig
         }
         uint32_t* s = scratch + (turn ^= 1) * (NT / 32);
         if ((threadIdx.x & 31) == 31) s[threadIdx.x >> 5] = upto;
-        __syncthreads();
+        row_sync<NT>();
         uint32_t before = 0, all = 0;
         for (int w = 0; w < NT / 32; ++w) {
             if (w < (int)(threadIdx.x >> 5)) before += s[w];
@@ -192,40 +236,235 @@ __device__ __noinline__ uint32_t topk_bisect(const RowSpan& r, uint32_t K, unsig
             }
         n = min(K, n + all);
     }
-    __syncthreads();
+    row_sync<NT>();
     return n;
 }
 
-// NT threads per row; as many blocks per SM as registers allow, so that some stream while others select.
+// One thread's part of a row that NT threads stream: group maxima (two values each), running maximum and sum of
+// 2^((z - zm) * scale).  The vectors that lie inside the row belong to groups; the first and the last, which may hold
+// entries of neighbouring rows, are added to the sums of one thread each and belong to none.
 template <int NT, bool kF16>
-__global__ void __launch_bounds__(NT, NT >= 1024 ? 1 : 1024 / NT) topk_logprobs_kernel(TopkArgs p)
+__device__ __forceinline__ void stream_row(const RowSpan& r, int tid, float scale, uint32_t (&g2)[kTopkGroups], float& zm, float& s)
+{
+#pragma unroll
+    for (int u = 0; u < kTopkGroups; ++u) g2[u] = El<kF16>::kNegInf2;
+    zm = kTopkFloor;
+    s = 0.f;
+    auto add4 = [&](const uint4 (&q)[4], uint32_t m2) {
+        const float2 mf = El<kF16>::unpack2(m2);
+        const float zn = fmaxf(zm, fmaxf(mf.x, mf.y));
+        float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 x = __fmul2_rn(__fadd2_rn(El<kF16>::unpack2(w[k]), splat2(-zn)), splat2(scale));
+                acc[k & 1] = __fadd2_rn(acc[k & 1], make_float2(ex2(x.x), ex2(x.y)));
+            }
+        }
+        s = fmaf(s, ex2((zm - zn) * scale), (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y));
+        zm = zn;
+    };
+    const uint4 none = make_uint4(El<kF16>::kNegInf2, El<kF16>::kNegInf2, El<kF16>::kNegInf2, El<kF16>::kNegInf2);
+    auto vec_max = [&](const uint4& q) { return max2<kF16>(max2<kF16>(q.x, q.y), max2<kF16>(q.z, q.w)); };
+    const uint32_t last = r.nvec - 1;           // vectors 1 .. last-1 lie inside the row
+    uint32_t v0 = 1 + tid;
+    for (; v0 + (kTopkGroups - 1) * NT < last; v0 += kTopkGroups * NT) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint4 q[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[u] = load_streaming(r.vecs + v0 + (4 * h + u) * NT);
+            uint32_t vm[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                vm[u] = vec_max(q[u]);
+                g2[4 * h + u] = max2<kF16>(g2[4 * h + u], vm[u]);
+            }
+            add4(q, max2<kF16>(max2<kF16>(vm[0], vm[1]), max2<kF16>(vm[2], vm[3])));
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {               // the rest: fewer than eight vectors
+        if (v0 + 4 * h * NT < last) {
+            uint4 q[4];
+            uint32_t m2 = El<kF16>::kNegInf2;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t v = v0 + (4 * h + u) * NT;
+                q[u] = none;
+                if (v < last) q[u] = load_streaming(r.vecs + v);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t vm = vec_max(q[u]);
+                g2[4 * h + u] = max2<kF16>(g2[4 * h + u], vm);
+                m2 = max2<kF16>(m2, vm);
+            }
+            add4(q, m2);
+        }
+    }
+    if (tid == 0 || (tid == NT - 1 && last > 0)) {
+        const uint4 q[4] = {span_vec<kF16>(r, tid == 0 ? 0u : last), none, none, none};
+        add4(q, vec_max(q[0]));
+    }
+}
+
+// ---------------------------------------------------------------- a row per block
+// A thread's groups are eight: its vectors j with equal j mod 8.  Rows with more candidates than the list holds (long runs
+// of equal values, rows sorted against the groups) are selected by bisection over the 16-bit values with repeated reads of
+// the row.
+// NT threads per row; as many blocks per SM as registers allow, so that some stream while others select.
+// What the threads of a row share.
+template <int NT>
+struct TopkShared {
+    unsigned long long cand[kTopkCandidates];
+    uint16_t group[kTopkGroups * NT];
+    uint32_t scratch[2 * (NT / 32)];
+    float2 part[NT / 32];
+    uint32_t lo[NT / 32], hi[NT / 32];
+    uint32_t n[2];                      // qualifying groups, candidates: zero when a selection starts
+};
+
+// Selects the K best entries of a row from what its NT threads saw of it, and writes them.
+template <int NT, bool kF16>
+__device__ __forceinline__ void select_row(const TopkArgs& p, const RowSpan& r, TopkShared<NT>& sh, int tid,
+                                           const uint32_t (&g2)[kTopkGroups], float zm, float s, int& turn, int* ids, float* lps)
 {
     constexpr int kWarps = NT / 32;
-    __shared__ unsigned long long s_cand[kTopkCandidates];
-    __shared__ uint16_t s_group[kTopkGroups * NT];
-    __shared__ uint32_t s_scratch[2 * kWarps];
-    __shared__ float2 s_part[kWarps];
-    __shared__ uint32_t s_lo[kWarps], s_hi[kWarps];
-    __shared__ uint32_t s_n[2];                     // qualifying groups, candidates
+    const int warp = tid >> 5, lane = tid & 31;
+    const uint32_t empty = key_of_neg_inf<kF16>();
+    const uint32_t last = r.nvec - 1;                              // vectors 1 .. last-1 belong to groups
+    // ---- block totals: the row's maximum and sum; smallest and largest of the threads' maxima
+    uint32_t key[kTopkGroups], top = 0u;
+#pragma unroll
+    for (int u = 0; u < kTopkGroups; ++u) {
+        key[u] = max(order_key(g2[u] & 0xffffu), order_key(g2[u] >> 16));
+        if (key[u] <= empty) key[u] = 0;                       // nothing in it to select
+        top = max(top, key[u]);
+    }
+    float zw = zm;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) zw = fmaxf(zw, __shfl_xor_sync(0xffffffffu, zw, o));
+    float sw = s * ex2((zm - zw) * p.scale);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sw += __shfl_xor_sync(0xffffffffu, sw, o);
+    uint32_t lo = __reduce_min_sync(0xffffffffu, top), hi = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) { sh.part[warp] = make_float2(zw, sw); sh.lo[warp] = lo; sh.hi[warp] = hi; }
+    row_sync<NT>();
+    float zt = kTopkFloor, st = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { zt = fmaxf(zt, sh.part[w].x); lo = min(lo, sh.lo[w]); hi = max(hi, sh.hi[w]); }
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) st += sh.part[w].y * ex2((sh.part[w].x - zt) * p.scale);
+    const float l2 = log2f(st);
+
+    // ---- a bound that K groups reach
+    uint32_t end = hi + 1u;                                    // nothing reaches this
+    if (p.K <= NT / 2) {
+        // the K-th largest of the threads' maxima, by bisection: a thread's eight groups count as one, which costs a
+        // few more candidates (74 instead of 65 for K = 64 of 256) and an eighth of the comparisons
+        lo = max(lo, empty + 1u);
+        if (row_count<NT>(top >= lo) < p.K) lo = end = empty + 1u;   // fewer threads with an entry than K
+        while (end > lo + 1u) {
+            const uint32_t mid = (lo + end) >> 1;
+            if (row_count<NT>(top >= mid) >= p.K) lo = mid; else end = mid;
+        }
+    } else {
+        // the K-th largest of all group maxima, by trisection (two counts of at most 2^13 in one reduction)
+        lo = empty + 1u;
+        uint32_t n = 0;
+#pragma unroll
+        for (int u = 0; u < kTopkGroups; ++u) n += key[u] >= lo ? 1u : 0u;
+        if (block_sum<NT>(n, sh.scratch, turn) < (uint32_t)p.K) end = lo;
+        while (end > lo + 1u) {
+            const uint32_t d = end - lo, p1 = lo + max(1u, d / 3u), p2 = max(p1, lo + 2u * d / 3u);
+            n = 0;
+#pragma unroll
+            for (int u = 0; u < kTopkGroups; ++u) n += (key[u] >= p1 ? 1u : 0u) + (key[u] >= p2 ? 65536u : 0u);
+            n = block_sum<NT>(n, sh.scratch, turn);
+            if ((n >> 16) >= (uint32_t)p.K) lo = p2;
+            else if ((n & 0xffffu) >= (uint32_t)p.K) { lo = p1; end = p2; }      // p1 < p2 here: their counts differ
+            else end = p1;
+        }
+    }
+
+    // ---- the groups that reach it, and their entries that do; the two outer vectors always
+    {
+        uint32_t mine = 0;
+#pragma unroll
+        for (int u = 0; u < kTopkGroups; ++u) mine += key[u] >= lo ? 1u : 0u;
+        uint32_t at = mine ? atomicAdd(&sh.n[0], mine) : 0u;
+#pragma unroll
+        for (int u = 0; u < kTopkGroups; ++u)
+            if (key[u] >= lo) sh.group[at++] = (uint16_t)(u * NT + tid);
+    }
+    if (tid == 0 || (tid == NT - 1 && last > 0)) collect_vec<kF16>(r, tid == 0 ? 0u : last, lo, sh.cand, &sh.n[1]);
+    row_sync<NT>();
+    // (a group's vectors are dealt to a power of two of neighbouring threads)
+    const uint32_t rounds = max(1u, (last + kTopkGroups * NT - 1) / (kTopkGroups * NT)), log_rounds = 32 - __clz((int)(rounds - 1));
+    const uint32_t items = sh.n[0] << log_rounds;
+    for (uint32_t it = tid; it < items; it += 2 * NT) {
+        uint32_t v[2];
+        uint4 q[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                          // both in flight
+            const uint32_t x = it + h * NT;
+            v[h] = last;
+            if (x < items) v[h] = 1u + sh.group[x >> log_rounds] + (x & ((1u << log_rounds) - 1u)) * (kTopkGroups * NT);
+            if (v[h] < last) q[h] = load_streaming(r.vecs + v[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (v[h] < last) collect_entries<kF16>(r, q[h], v[h], lo, sh.cand, &sh.n[1]);
+    }
+    row_sync<NT>();
+    uint32_t n = sh.n[1];
+    if (n > (uint32_t)kTopkCandidates) n = topk_bisect<NT, kF16>(r, (uint32_t)p.K, sh.cand, &sh.n[1], sh.scratch, turn);
+
+    // ---- ranks: the number of larger candidates
+    for (uint32_t c = tid; c < n; c += NT) {
+        const unsigned long long mine = sh.cand[c];
+        uint32_t rank = 0;
+#pragma unroll 4
+        for (uint32_t o = 0; o < n; ++o) rank += sh.cand[o] > mine ? 1u : 0u;
+        if (rank < (uint32_t)p.K) {
+            const float z = El<kF16>::widen(key_bits((uint32_t)(mine >> 32)));
+            ids[rank] = (int)(0xffffffffu - (uint32_t)mine);
+            lps[rank] = kLn2 * fmaf(z - zt, p.scale, -l2);
+        }
+    }
+    for (uint32_t k = n + tid; k < (uint32_t)p.K; k += NT) {    // fewer entries than K
+        ids[k] = -1;
+        lps[k] = __uint_as_float(0xff800000u);
+    }
+}
+
+constexpr int topk_blocks_per_sm(int threads) { return threads >= 1024 ? 1 : 1024 / threads; }
+
+template <int NT, bool kF16>
+__global__ void __launch_bounds__(NT, topk_blocks_per_sm(NT)) topk_block_kernel(TopkArgs p)
+{
+    __shared__ TopkShared<NT> sh;
     __shared__ long long s_row[2];
     __shared__ long long s_cnt[33];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x;
     int turn = 0;
 
     pdl_wait_prior_grid();
     pdl_release_next_grid();
-    if (blockIdx.x == 0) block_count_valid(p.lengths, p.B, p.T, s_cnt, p.status);
     const long long total = (long long)p.B * p.T;
-    const uint32_t empty = key_of_neg_inf<kF16>();
-    if (tid == 0) s_row[0] = (long long)atomicAdd(p.row_counter, 1u);
+    const bool one_each = (long long)gridDim.x >= total;   // no counter: block i has row i
+    if (tid == 0) s_row[0] = one_each ? (long long)blockIdx.x : (long long)atomicAdd(p.row_counter, 1u);
 
     for (int i = 0;; ++i) {
         __syncthreads();                            // s_row[i & 1] is there; the previous row's shared data has been read
         const long long row = s_row[i & 1];
         if (row >= total) break;
         if (tid == 0) {
-            s_row[(i + 1) & 1] = (long long)atomicAdd(p.row_counter, 1u);   // the next row, in flight during this one
-            s_n[0] = s_n[1] = 0;
+            s_row[(i + 1) & 1] = one_each ? total : (long long)atomicAdd(p.row_counter, 1u);   // the next row, in flight during this one
+            sh.n[0] = sh.n[1] = 0;
         }
         const int b = (int)(row / p.T), t = (int)(row % p.T);
         int* ids = p.ids + row * p.K;
@@ -236,126 +475,15 @@ __global__ void __launch_bounds__(NT, NT >= 1024 ? 1 : 1024 / NT) topk_logprobs_
         }
         const RowSpan r = row_span(p.logits + (long long)b * p.stride_b + (long long)t * p.stride_t, p.V);
 
-        // ---- the stream: partition sum and group maxima
+        // ---- the stream
         uint32_t g2[kTopkGroups];
-#pragma unroll
-        for (int u = 0; u < kTopkGroups; ++u) g2[u] = El<kF16>::kNegInf2;
-        float zm = kTopkFloor, s = 0.f;             // running maximum and sum of 2^((z - zm) * scale)
-        for (uint32_t v0 = tid; v0 < r.nvec; v0 += kTopkGroups * NT) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint4 q[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t v = v0 + (4 * h + u) * NT;
-                    q[u] = make_uint4(El<kF16>::kNegInf2, El<kF16>::kNegInf2, El<kF16>::kNegInf2, El<kF16>::kNegInf2);
-                    if (v < r.nvec) q[u] = load_streaming(r.vecs + v);
-                }
-                uint32_t m2 = El<kF16>::kNegInf2;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t v = v0 + (4 * h + u) * NT;
-                    if (v == 0 || v == r.nvec - 1)
-                        q[u] = mask_vec_outside<kF16>(q[u], v == 0 ? (int)r.eoff : 0, v == r.nvec - 1 ? (int)r.tail : 8);
-                    const uint32_t vm = max2<kF16>(max2<kF16>(q[u].x, q[u].y), max2<kF16>(q[u].z, q[u].w));
-                    g2[4 * h + u] = max2<kF16>(g2[4 * h + u], vm);
-                    m2 = max2<kF16>(m2, vm);
-                }
-                const float2 mf = El<kF16>::unpack2(m2);
-                const float zn = fmaxf(zm, fmaxf(mf.x, mf.y));
-                float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float2 x = __fmul2_rn(__fadd2_rn(El<kF16>::unpack2(w[k]), splat2(-zn)), splat2(p.scale));
-                        acc[k & 1] = __fadd2_rn(acc[k & 1], make_float2(ex2(x.x), ex2(x.y)));
-                    }
-                }
-                s = fmaf(s, ex2((zm - zn) * p.scale), (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y));
-                zm = zn;
-            }
-        }
+        float zm, s;
+        stream_row<NT, kF16>(r, tid, p.scale, g2, zm, s);
 
-        // ---- block totals: the row's maximum and sum; smallest and largest group maximum
-        uint32_t key[kTopkGroups], lo = 65535u, hi = 0u;
-#pragma unroll
-        for (int u = 0; u < kTopkGroups; ++u) {
-            key[u] = max(order_key(g2[u] & 0xffffu), order_key(g2[u] >> 16));
-            if (key[u] <= empty) key[u] = 0;                       // nothing in it to select
-            hi = max(hi, key[u]);
-            lo = min(lo, key[u]);
-        }
-        float zw = zm;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) zw = fmaxf(zw, __shfl_xor_sync(0xffffffffu, zw, o));
-        float sw = s * ex2((zm - zw) * p.scale);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sw += __shfl_xor_sync(0xffffffffu, sw, o);
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        if (lane == 0) { s_part[warp] = make_float2(zw, sw); s_lo[warp] = lo; s_hi[warp] = hi; }
-        __syncthreads();
-        float zt = kTopkFloor, st = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) { zt = fmaxf(zt, s_part[w].x); lo = min(lo, s_lo[w]); hi = max(hi, s_hi[w]); }
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) st += s_part[w].y * ex2((s_part[w].x - zt) * p.scale);
-        const float l2 = log2f(st);
-
-        // ---- the K-th largest group maximum, by trisection (two counts of at most 2^14 in one reduction)
-        lo = max(lo, empty + 1u);                                  // every selectable entry reaches this
-        uint32_t end = hi + 1u;                                    // nothing reaches this
-        bool enough = true;
-        {
-            uint32_t n = 0;
-#pragma unroll
-            for (int u = 0; u < kTopkGroups; ++u) n += key[u] >= lo ? 1u : 0u;
-            enough = block_sum<NT>(n, s_scratch, turn) >= (uint32_t)p.K;
-        }
-        while (enough && end - lo > 1u) {
-            const uint32_t d = end - lo, p1 = lo + max(1u, d / 3u), p2 = max(p1, lo + 2u * d / 3u);
-            uint32_t n = 0;
-#pragma unroll
-            for (int u = 0; u < kTopkGroups; ++u) n += (key[u] >= p1 ? 1u : 0u) + (key[u] >= p2 ? 65536u : 0u);
-            n = block_sum<NT>(n, s_scratch, turn);
-            if ((n >> 16) >= (uint32_t)p.K) lo = p2;
-            else if ((n & 0xffffu) >= (uint32_t)p.K) { lo = p1; end = p2; }      // p1 < p2 here: their counts differ
-            else end = p1;
-        }
-
-        // ---- the groups that reach it, and their entries that do
-#pragma unroll
-        for (int u = 0; u < kTopkGroups; ++u)
-            if (key[u] >= lo) s_group[atomicAdd(&s_n[0], 1u)] = (uint16_t)(u * NT + tid);
-        __syncthreads();
-        const uint32_t rounds = (r.nvec + kTopkGroups * NT - 1) / (kTopkGroups * NT), items = s_n[0] * rounds;
-        for (uint32_t it = tid; it < items; it += NT) {
-            const uint32_t v = s_group[it / rounds] + (it % rounds) * (kTopkGroups * NT);
-            if (v < r.nvec) collect_vec<kF16>(r, v, lo, s_cand, &s_n[1]);
-        }
-        __syncthreads();
-        uint32_t n = s_n[1];
-        if (n > (uint32_t)kTopkCandidates) n = topk_bisect<NT, kF16>(r, (uint32_t)p.K, s_cand, &s_n[1], s_scratch, turn);
-
-        // ---- ranks: the number of larger candidates
-        for (uint32_t c = tid; c < n; c += NT) {
-            const unsigned long long mine = s_cand[c];
-            uint32_t rank = 0;
-            for (uint32_t o = 0; o < n; ++o) rank += s_cand[o] > mine ? 1u : 0u;
-            if (rank < (uint32_t)p.K) {
-                const float z = El<kF16>::widen(key_bits((uint32_t)(mine >> 32)));
-                ids[rank] = (int)(0xffffffffu - (uint32_t)mine);
-                lps[rank] = kLn2 * fmaf(z - zt, p.scale, -l2);
-            }
-        }
-        for (uint32_t k = n + tid; k < (uint32_t)p.K; k += NT) {    // fewer entries than K
-            ids[k] = -1;
-            lps[k] = __uint_as_float(0xff800000u);
-        }
+        select_row<NT, kF16>(p, r, sh, tid, g2, zm, s, turn, ids, lps);
     }
-    if (tid == 0) {
+    if (blockIdx.x == 0) block_count_valid(p.lengths, p.B, p.T, s_cnt, p.status);   // flags lengths out of range
+    if (tid == 0 && !one_each) {
         if (atomicAdd(p.ticket, 1u) == gridDim.x - 1) { *p.ticket = 0u; *p.row_counter = 0u; }
     }
 }

@@ -270,7 +270,10 @@ def check_topk(z, lengths, K, temperature):
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("B,T,V,K", [(1, 1, 1, 1), (2, 3, 7, 9), (1, 1, 50272, 20), (3, 5, 1000, 256), (3, 5, 1001, 1), (2, 9, 2047, 100),
                                      (3, 70, 8200, 33), (4, 60, 32000, 64), (2, 3, 50257, 50), (2, 200, 50257, 7),
-                                     (2, 3, 128256, 256), (3, 101, 128256, 128), (1, 2, 300001, 256)])
+                                     (2, 3, 128256, 256), (3, 101, 128256, 128), (1, 2, 300001, 256),
+                                     # enough rows for a row per warp
+                                     (8, 90, 1, 3), (8, 90, 7, 5), (8, 90, 1000, 256), (8, 90, 1001, 1), (6, 120, 8200, 100), (5, 160, 32000, 64),
+                                     (5, 160, 50257, 256), (3, 210, 128256, 128)])
 def test_topk_sizes(B, T, V, K, dtype):
     gen = torch.Generator(device=DEV).manual_seed(V + K)
     z, _ = ref.row_logits(B, T, V, dtype, gen, DEV, prompt=1 if V < 60000 else 0, pitch=3 if V % 2 else 0)
@@ -279,9 +282,10 @@ def test_topk_sizes(B, T, V, K, dtype):
     assert lib.poll_status(ws) == 0
 
 
-def test_topk_ties_runs_and_deleted_entries():
+@pytest.mark.parametrize("T", [2, 55])                       # a row per block, a row per warp
+def test_topk_ties_runs_and_deleted_entries(T):
     gen = torch.Generator(device=DEV).manual_seed(31)
-    B, T, V = 12, 2, 20003
+    B, V = 12, 20003
     for dtype in (BF, HF):
         z, _ = ref.row_logits(B, T, V, dtype, gen, DEV, pitch=2)
         z[0] = 0.0                                           # all entries equal
@@ -305,9 +309,10 @@ def test_topk_ties_runs_and_deleted_entries():
             check_topk(z, lengths, K, 1.0)
 
 
-def test_topk_lengths_out_of_range_and_non_finite_logits():
+@pytest.mark.parametrize("T", [3, 210])
+def test_topk_lengths_out_of_range_and_non_finite_logits(T):
     gen = torch.Generator(device=DEV).manual_seed(32)
-    B, T, V, K = 3, 3, 9000, 16
+    B, V, K = 3, 9000, 16
     z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
     lengths = torch.tensor([T + 4, -1, 2], dtype=torch.int32, device=DEV)
     _, ws = check_topk(z, lengths, K, 0.7)
