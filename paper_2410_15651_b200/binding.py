@@ -470,13 +470,21 @@ def _like(logits: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(logits, memory_format=torch.contiguous_format)
 
 
+def _raw_stream(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+# the same without the Stream object (0.1 us against 2.2 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
 def _call(name: str, dev: int, *args) -> None:
     """Calls the entry point with the device of its tensors current and that device's current stream."""
     if torch.cuda.current_device() == dev:
-        status = getattr(lib(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+        status = getattr(_lib or lib(), name)(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            status = getattr(lib(), name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+            status = getattr(_lib or lib(), name)(*args, _raw_stream(dev))
     if status != 0:
         raise RlhfError(status, name)
 
@@ -509,9 +517,10 @@ class DistillOutputs:
     """Buffers written by distill_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, in_place: bool = False, want_row_loss: bool = True):
+        B, T, _ = logits.shape
         self.loss = logits.new_empty(1, dtype=_F32)
         self.dlogits = logits if in_place else _like(logits)
-        self.row_loss = logits.new_empty(logits.shape[:2], dtype=_F32) if want_row_loss else None
+        self.row_loss = logits.new_empty((B, T), dtype=_F32) if want_row_loss else None
 
 
 def distill_loss_fwd_bwd(logits: torch.Tensor, topk_ids: torch.Tensor, topk_logprobs: torch.Tensor, lengths: torch.Tensor,
@@ -543,9 +552,10 @@ class PolicyKlOutputs:
     """Buffers written by policy_kl_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, in_place: bool = False, want_lp_new: bool = True):
+        B, T, _ = logits.shape
         self.loss = logits.new_empty(2, dtype=_F32)                                  # [loss_pg, loss_kl]
         self.dlogits = logits if in_place else _like(logits)
-        self.lp_new = logits.new_empty(logits.shape[:2], dtype=_F32) if want_lp_new else None
+        self.lp_new = logits.new_empty((B, T), dtype=_F32) if want_lp_new else None
 
 
 def policy_kl_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor, lp_old: torch.Tensor,
@@ -578,10 +588,11 @@ class PreferenceOutputs:
     """Buffers written by preference_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, in_place: bool = False, want_lp_new: bool = True):
+        B, T, _ = logits.shape
         self.loss = logits.new_empty(1, dtype=_F32)
-        self.rewards = logits.new_empty(logits.shape[0], dtype=_F32)                 # beta * log ratio of every sequence
+        self.rewards = logits.new_empty(B, dtype=_F32)                               # beta * log ratio of every sequence
         self.dlogits = logits if in_place else _like(logits)
-        self.lp_new = logits.new_empty(logits.shape[:2], dtype=_F32) if want_lp_new else None
+        self.lp_new = logits.new_empty((B, T), dtype=_F32) if want_lp_new else None
 
 
 def preference_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor,

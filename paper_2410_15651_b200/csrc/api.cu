@@ -557,6 +557,46 @@ int launch_topk(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
     return launch_topk_as<256, kF16>(ta, dev, s);
 }
 
+template <int NT, bool kF16>
+int launch_logprob_block_as(const BlockLpArgs& a, const DeviceInfo& dev, cudaStream_t s)
+{
+    const int grid = (int)std::min<long long>((long long)a.B * a.T, (long long)dev.sm_count * (1024 / NT));
+    RLHF_CUDA(launch_kernel(logprob_block_kernel<NT, kF16>, grid, NT, 0, s, a));
+    return launch_check("logprob_block_kernel");
+}
+
+// Log-probs for the objectives that form them in a launch of their own: a row per warp, or a row per block in batches of at
+// most eight rows per SM, which leave a device with a row per warp idle.  The preference loss with the one and the other,
+// 64 rows of 32000: 35 and 24 us; 256 rows of 50272: 48 and 37 us; 512: 61 and 50 us; 1024: 85 and 83 us.
+int launch_logprobs(const RowArgs& a, float* out_lp, bool f16, const DeviceInfo& dev, cudaStream_t s)
+{
+    const long long rows = (long long)a.B * a.T;
+    if (rows <= 8ll * dev.sm_count) {
+        BlockLpArgs b{};
+        b.logits = a.logits;
+        b.stride_b = a.stride_b;
+        b.stride_t = a.stride_t;
+        b.ids = a.ids;
+        b.ids_stride_b = a.ids_stride_b;
+        b.lengths = a.lengths;
+        b.B = a.B; b.T = a.T; b.V = a.V;
+        b.out_lp = out_lp;
+        b.status = a.status;
+        if (rows <= dev.sm_count && a.V > 16384)
+            return f16 ? launch_logprob_block_as<1024, true>(b, dev, s) : launch_logprob_block_as<1024, false>(b, dev, s);
+        return f16 ? launch_logprob_block_as<256, true>(b, dev, s) : launch_logprob_block_as<256, false>(b, dev, s);
+    }
+    WarpArgs wa{};
+    wa.row = a;
+    wa.row.out_lp = out_lp;
+    if (rows_16B(a.logits, a.stride_b, a.stride_t, a.V)) {
+        if (int e = launch_warp_logprob<false, false>(wa, f16, dev, s)) return e;
+    } else {
+        if (int e = launch_warp_logprob<false, true>(wa, f16, dev, s)) return e;
+    }
+    return launch_check("logprob_warp_kernel");
+}
+
 // Launches the row kernel for an objective with one generated token per row.  Sets a.fused if that kernel also does
 // the finalisation (the losses; value loss and dvalues in step 4); otherwise it leaves per-token terms in a.row_loss
 // (and a.row_kl).
@@ -1145,18 +1185,11 @@ int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long
     a.seq_factor = (const float*)(ws + kRowLossOffset + 4 * tokens);
 
     // log-probs of every token, the pairs, then the gradient rows with each sequence's factor known
-    WarpArgs wa{};
-    wa.row = a;
-    wa.row.out_lp = out_lp_new ? out_lp_new : (float*)(ws + kRowLossOffset);
-    if (rows_16B(logits, stride_b, stride_t, V)) {
-        if (int e = launch_warp_logprob<false, false>(wa, f16, dev, s)) return e;
-    } else {
-        if (int e = launch_warp_logprob<false, true>(wa, f16, dev, s)) return e;
-    }
-    if (int e = launch_check("logprob_warp_kernel")) return e;
+    float* lp = out_lp_new ? out_lp_new : (float*)(ws + kRowLossOffset);
+    if (int e = launch_logprobs(a, lp, f16, dev, s)) return e;
 
     PairArgs pa{};
-    pa.lp = wa.row.out_lp;
+    pa.lp = lp;
     pa.lp_ref = lp_ref;
     pa.ids = ids;
     pa.ids_stride_b = ids_stride_b;

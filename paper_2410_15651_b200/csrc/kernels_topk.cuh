@@ -488,4 +488,64 @@ __global__ void __launch_bounds__(NT, topk_blocks_per_sm(NT)) topk_block_kernel(
     }
 }
 
+// ---------------------------------------------------------------- log-probs of few rows
+// The log-prob of the generated token for batches that do not fill the device with a row per warp (logprob_warp_kernel): a
+// row per block, streamed as above, all of a row's loads in flight at once.  64 rows of 32000: 7 us against 20 us.
+struct BlockLpArgs {
+    const uint16_t* logits;
+    long long stride_b, stride_t;
+    const long long* ids;
+    long long ids_stride_b;
+    const int* lengths;
+    int B, T, V;
+    float* out_lp;
+    unsigned* status;
+};
+
+template <int NT, bool kF16>
+__global__ void __launch_bounds__(NT, 1024 / NT) logprob_block_kernel(BlockLpArgs p)
+{
+    __shared__ float2 s_part[2][NT / 32];
+    __shared__ long long s_cnt[33];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    pdl_wait_prior_grid();
+    pdl_release_next_grid();
+    const long long total = (long long)p.B * p.T;
+    int par = 0;
+    for (long long row = blockIdx.x; row < total; row += gridDim.x, par ^= 1) {
+        const int b = (int)(row / p.T), t = (int)(row % p.T);
+        if (t >= clamp_len(__ldg(p.lengths + b), p.T)) {
+            if (tid == 0) p.out_lp[row] = 0.f;
+            continue;
+        }
+        const uint16_t* z16 = p.logits + (long long)b * p.stride_b + (long long)t * p.stride_t;
+        float zy = 0.f;
+        bool bad_id = false;
+        if (tid == 0) {                                              // in flight during the stream
+            const long long y = __ldg(p.ids + (long long)b * p.ids_stride_b + t);
+            bad_id = y < 0 || y >= p.V;
+            if (bad_id) atomicOr(p.status, kErrIdRange);
+            else zy = El<kF16>::widen(__ldg(z16 + y));
+        }
+        uint32_t g2[kTopkGroups];
+        float zm, s;
+        stream_row<NT, kF16>(row_span(z16, p.V), tid, kLog2e, g2, zm, s);
+        float zw = zm;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) zw = fmaxf(zw, __shfl_xor_sync(0xffffffffu, zw, o));
+        float sw = s * ex2((zm - zw) * kLog2e);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sw += __shfl_xor_sync(0xffffffffu, sw, o);
+        if (lane == 0) s_part[par][warp] = make_float2(zw, sw);
+        __syncthreads();                                             // (the two sets of parts alternate)
+        if (tid == 0) {
+            float zt = kTopkFloor, st = 0.f;
+            for (int w = 0; w < NT / 32; ++w) zt = fmaxf(zt, s_part[par][w].x);
+            for (int w = 0; w < NT / 32; ++w) st += s_part[par][w].y * ex2((s_part[par][w].x - zt) * kLog2e);
+            p.out_lp[row] = bad_id ? 0.f : kLn2 * fmaf(zy - zt, kLog2e, -log2f(st));
+        }
+    }
+    if (blockIdx.x == 0) block_count_valid(p.lengths, p.B, p.T, s_cnt, p.status);   // flags lengths out of range
+}
+
 }  // namespace rlhf
