@@ -284,14 +284,16 @@ struct CringPlan {
     size_t smem_bytes = 0;
 };
 
-CringPlan plan_cring(unsigned row_bytes, const DeviceInfo& dev)
+// K: teacher entries per row, 0 for the objectives of one generated token.
+CringPlan plan_cring(unsigned row_bytes, const DeviceInfo& dev, int K = 0)
 {
     CringPlan pl;
     if (row_bytes % 16 != 0) return pl;
     const unsigned row_vecs = row_bytes / 16;
     const size_t chunk = cring_chunk_bytes(kCregWarps);
     int R = kCringMaxSlots;
-    while (R > 0 && cring_smem_bytes(kCregWarps, R) + 3072 > (size_t)dev.max_smem_optin) --R;
+    // (static shared memory apart; with margin)
+    while (R > 0 && cring_smem_bytes(kCregWarps, R, K) + (K > 0 ? 2688 : 3 * 1024) > (size_t)dev.max_smem_optin) --R;
     for (int c = 1; c <= 4; ++c) {
         const unsigned sv = (row_vecs + c - 1) / c;
         const int C = (int)(((size_t)sv * 16 + chunk - 1) / chunk);
@@ -306,17 +308,19 @@ CringPlan plan_cring(unsigned row_bytes, const DeviceInfo& dev)
         pl.tmem_cols = cols;
         pl.n_slots = R;
         pl.chunks = C;
-        pl.smem_bytes = cring_smem_bytes(kCregWarps, R);
+        pl.smem_bytes = cring_smem_bytes(kCregWarps, R, K);
         return pl;
     }
     return pl;
 }
 
-template <int C, bool kF16>
-int launch_cring(const RowArgs& a, const CringPlan& pl, const DeviceInfo& dev, cudaStream_t s)
+template <int C, bool kF16, bool kDistill = false>
+int launch_cring(const RowArgs& a, const CringPlan& pl, const DeviceInfo& dev, cudaStream_t s, const DistillArgs& dt = DistillArgs{})
 {
-    constexpr int NW = kCregWarps;
+    constexpr int NW = kCregWarps, kThreads = NW * 32 + (kDistill ? 96 : 32);
+    auto kernel = loss_cring_kernel<NW, C, kF16, kDistill>;
     CringArgs ca{};
+    ca.distill = dt;
     ca.row = a;
     ca.row_bytes = 2u * (unsigned)a.V;
     ca.slice_vecs = pl.slice_vecs;
@@ -324,8 +328,7 @@ int launch_cring(const RowArgs& a, const CringPlan& pl, const DeviceInfo& dev, c
     ca.n_slots = pl.n_slots;
     ca.chunks = pl.chunks;
     ca.row_counter = (unsigned*)((char*)a.status + 16);
-    RLHF_CUDA(cudaFuncSetAttribute(loss_cring_kernel<NW, C, kF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)pl.smem_bytes));
+    RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pl.smem_bytes));
     // clusters that the device holds at once (one block per SM); looked up once per device
     static std::mutex mu;
     static int cached[64] = {};
@@ -339,8 +342,8 @@ int launch_cring(const RowArgs& a, const CringPlan& pl, const DeviceInfo& dev, c
             int n = 0;
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
-            fill_launch_config(cfg, attr, dev.sm_count / C * C, NW * 32 + 32, pl.smem_bytes, C, nullptr);
-            RLHF_CUDA(cudaOccupancyMaxActiveClusters(&n, loss_cring_kernel<NW, C, kF16>, &cfg));
+            fill_launch_config(cfg, attr, dev.sm_count / C * C, kThreads, pl.smem_bytes, C, nullptr);
+            RLHF_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
             if (n < 1) n = 1;
             if (d >= 0 && d < 64) cached[d] = n;
             clusters = n;
@@ -350,7 +353,7 @@ int launch_cring(const RowArgs& a, const CringPlan& pl, const DeviceInfo& dev, c
     }
     const long long rows = (long long)a.B * a.T;
     const int grid = (int)std::min<long long>(rows, clusters) * C;
-    RLHF_CUDA(launch_kernel_cluster(loss_cring_kernel<NW, C, kF16>, grid, NW * 32 + 32, pl.smem_bytes, C, s, ca));
+    RLHF_CUDA(launch_kernel_cluster(kernel, grid, kThreads, pl.smem_bytes, C, s, ca));
     return RLHF_OK;
 }
 
@@ -505,6 +508,18 @@ int launch_distill_creg(const RowArgs& a, const DistillArgs& d, const CregPlan& 
     }
 }
 
+// Distillation rows on the chunk-ring kernel.
+template <bool kF16>
+int launch_distill_cring(const RowArgs& a, const DistillArgs& d, const CringPlan& pl, const DeviceInfo& dev, cudaStream_t s)
+{
+    switch (pl.cluster) {
+        case 1: return launch_cring<1, kF16, true>(a, pl, dev, s, d);
+        case 2: return launch_cring<2, kF16, true>(a, pl, dev, s, d);
+        case 3: return launch_cring<3, kF16, true>(a, pl, dev, s, d);
+        default: return launch_cring<4, kF16, true>(a, pl, dev, s, d);
+    }
+}
+
 // Launches the distillation row kernel; sets a.fused if it also forms the mean.
 int launch_distill_rows(RowArgs& a, const DistillArgs& d, bool f16, const DeviceInfo& dev, char* ws, cudaStream_t s)
 {
@@ -514,11 +529,17 @@ int launch_distill_rows(RowArgs& a, const DistillArgs& d, bool f16, const Device
     CregPlan pl;
     if (all_16B) pl = plan_creg(2u * (unsigned)a.V, dev, d.K);
     else if (same_offsets) pl = plan_creg_any(a.V, dev, d.K);
-    if (pl.cluster > 0 && dev.sm_count * 7 <= kMaxFusedBlocks) {
+    const CringPlan rp = all_16B ? plan_cring(2u * (unsigned)a.V, dev, d.K) : CringPlan{};
+    const bool cring = use_cring(pl, rp);
+    if ((cring || pl.cluster > 0) && dev.sm_count * 7 <= kMaxFusedBlocks) {
         a.fused = 1;
         a.ticket = (unsigned*)(ws + 4);
         a.partials = (double*)(ws + kPartialsOffset);
         int e;
+        if (cring) {
+            e = f16 ? launch_distill_cring<true>(a, d, rp, dev, s) : launch_distill_cring<false>(a, d, rp, dev, s);
+            return e ? e : launch_check("loss_cring_kernel<distill>");
+        }
         if (pl.tmem_cols != 0) e = f16 ? launch_distill_creg<true, true>(a, d, pl, !all_16B, dev, s) : launch_distill_creg<true, false>(a, d, pl, !all_16B, dev, s);
         else e = f16 ? launch_distill_creg<false, true>(a, d, pl, !all_16B, dev, s) : launch_distill_creg<false, false>(a, d, pl, !all_16B, dev, s);
         return e ? e : launch_check("loss_creg_kernel<distill>");

@@ -287,6 +287,134 @@ __device__ __forceinline__ void tmem_load8(uint32_t taddr, float2 (&v)[4])
 __device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// ---- what the target warps of the two on-chip-exponentials kernels do with a row's teacher entries (whole warp; lane l has
+// the entries l, l + 32, ...)
+constexpr int kPer = kDistillMax / 32;                       // entries per lane
+
+// Weights pk, positions in this block's slice of the row (or -1), sum of the weights P, sum of p log p H, and the weights'
+// sums over the slices of the cluster's blocks.  eoff: entries of the slice's first vector that precede the row.
+template <int kCluster>
+__device__ __forceinline__ void distill_weights(const RowArgs& p, const DistillArgs& dt, long long entries, uint32_t eoff,
+                                                uint32_t v0, uint32_t nvec, uint32_t slice_vecs, uint32_t crank, int lane,
+                                                int (&pos)[kPer], float (&pk)[kPer], double& P, double& H, float (&pr)[kCluster])
+{
+    float lt[kPer];
+    bool bad = false;
+    float lmax = kFloorM;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int k = lane + 32 * j;
+        pos[j] = -1;
+        lt[j] = __uint_as_float(0xff800000u);
+        if (k < dt.K) {
+            pos[j] = __ldg(dt.ids + entries + k);
+            lt[j] = __ldg(dt.logprobs + entries + k);
+            bad |= pos[j] < -1 || pos[j] >= p.V;
+            if (pos[j] < 0 || pos[j] >= p.V) { pos[j] = -1; lt[j] = __uint_as_float(0xff800000u); }
+            lmax = fmaxf(lmax, lt[j]);
+        }
+    }
+    if (__any_sync(0xffffffffu, bad) && lane == 0 && crank == 0) atomicOr(p.status, kErrIdRange);
+    P = 0.0;
+    if (dt.mode == kDistillNormalised) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) lmax = fmaxf(lmax, __shfl_xor_sync(0xffffffffu, lmax, o));
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        pk[j] = 0.f;
+        if (32 * j >= dt.K) continue;
+        // tail: 1 - sum p is what the mass outside is worth, so the sum is formed of terms in double precision
+        if (dt.mode == kDistillTail) { const double e = exp((double)lt[j]); P += e; pk[j] = (float)e; }
+        else { pk[j] = expf(dt.mode == kDistillNormalised ? lt[j] - lmax : lt[j]); P += (double)pk[j]; }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) P += __shfl_xor_sync(0xffffffffu, P, o);
+    if (dt.mode == kDistillNormalised) {
+        const float inv = P > 0.0 ? (float)(1.0 / P) : (P == P ? 0.f : (float)P), lse = lmax + (float)log(P);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) { pk[j] *= inv; lt[j] -= lse; }
+        P = P > 0.0 ? 1.0 : (P == P ? 0.0 : P);
+    }
+    H = 0.0;
+#pragma unroll
+    for (int c = 0; c < kCluster; ++c) pr[c] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (!(pk[j] == 0.f)) H += (double)pk[j] * (double)lt[j];
+        const uint32_t v = pos[j] < 0 ? 0xffffffffu : (eoff + (uint32_t)pos[j]) >> 3;
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c)
+            if (v - (uint32_t)c * slice_vecs < slice_vecs) pr[c] += pk[j];
+        // position in this block's buffer, or -1
+        pos[j] = v - v0 < nvec ? (int)(eoff + (uint32_t)pos[j] - v0 * 8u) : -1;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        H += __shfl_xor_sync(0xffffffffu, H, o);
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) pr[c] += __shfl_xor_sync(0xffffffffu, pr[c], o);
+    }
+}
+
+// The first of several equal entries takes the weight of all, added in the order of the list; the others are dropped.
+__device__ __forceinline__ void distill_merge(int K, int Kpad, int lane, int* tp, float* tw, int (&pos)[kPer], float (&pk)[kPer])
+{
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int k = lane + 32 * j, mine = pos[j];
+        if (mine < 0) continue;
+        for (int o = 0; o < k; ++o)
+            if (tp[o] == mine) { pos[j] = -1; break; }
+        if (pos[j] < 0) { pk[j] = 0.f; continue; }
+        for (int o = k + 1; o < K; ++o)
+            if (tp[o] == mine) pk[j] += tw[o];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; }
+}
+
+// Sums over the slice's entries against their own largest exponent, and what the consumers and the patch warp need.
+template <int kCluster>
+__device__ __forceinline__ void distill_publish(const DistillArgs& dt, float xscale, uint32_t crank, int lane, const int (&pos)[kPer],
+                                                const float (&pk)[kPer], const float (&z)[kPer], double P, double H,
+                                                const float (&pr)[kCluster], TargetInfo& target, LabelInfo& lab)
+{
+    float Mt = kFloorM;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (pos[j] >= 0) Mt = fmaxf(Mt, z[j] * xscale);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) Mt = fmaxf(Mt, __shfl_xor_sync(0xffffffffu, Mt, o));
+    float ey = 0.f, zy = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (pos[j] >= 0) {
+            const float x = fmaf(z[j], xscale, -Mt);
+            ey += ex2(x);
+            if (!(pk[j] == 0.f)) zy = fmaf(pk[j], x, zy);
+        }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        ey += __shfl_xor_sync(0xffffffffu, ey, o);
+        zy += __shfl_xor_sync(0xffffffffu, zy, o);
+    }
+    if (lane == 0) {
+        TargetInfo ti;
+        ti.H = H;
+        ti.P = (float)P;
+        ti.p0 = dt.mode == kDistillTail ? (float)(1.0 - P > 0.0 ? 1.0 - P : 0.0) : 0.f;
+        ti.W = dt.mode == kDistillTail ? (float)(P > 1.0 ? P : 1.0) : (float)P;
+        if (!(P == P)) ti.W = ti.P;
+        for (int c = 0; c < 4; ++c) ti.pr[c] = c < kCluster ? pr[c < kCluster ? c : 0] : 0.f;
+        target = ti;
+        lab = LabelInfo{zy, ey, Mt, ti.pr[crank]};
+    }
+}
+
 // ---------------------------------------------------------------- the kernel
 // kTmem: a thread's vectors beyond the first kRegVecsTmem keep their exponentials in tensor memory; otherwise a
 // thread has at most kRegVecsOnly vectors and registers hold all of them.  kF16: logits and gradient are IEEE
@@ -529,7 +657,6 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
 
     if (kDistill && warp == NW + 1) {
         // ------------------------------------------------------------ target warp
-        constexpr int kPer = kDistillMax / 32;                       // entries per lane
         for (int i = 0; !aborted; ++i) {
             const int buf = i % NB;
             mbar_wait(announced(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
@@ -541,66 +668,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
                 if (lane == 0) mbar_arrive(ready(buf));
                 break;
             }
-            // the entries' weights
             int pos[kPer];
-            float pk[kPer], lt[kPer];
-            bool bad = false;
-            float lmax = kFloorM;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const int k = lane + 32 * j;
-                pos[j] = -1;
-                lt[j] = __uint_as_float(0xff800000u);
-                if (k < dt.K) {
-                    pos[j] = __ldg(dt.ids + entries + k);
-                    lt[j] = __ldg(dt.logprobs + entries + k);
-                    bad |= pos[j] < -1 || pos[j] >= p.V;
-                    if (pos[j] < 0 || pos[j] >= p.V) { pos[j] = -1; lt[j] = __uint_as_float(0xff800000u); }
-                    lmax = fmaxf(lmax, lt[j]);
-                }
-            }
-            if (__any_sync(0xffffffffu, bad) && lane == 0 && crank == 0) atomicOr(p.status, kErrIdRange);
-            double P = 0.0;
-            if (dt.mode == kDistillNormalised) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) lmax = fmaxf(lmax, __shfl_xor_sync(0xffffffffu, lmax, o));
-            }
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                pk[j] = 0.f;
-                if (32 * j >= dt.K) continue;
-                // tail: 1 - sum p is what the mass outside is worth, so the sum is formed of terms in double precision
-                if (dt.mode == kDistillTail) { const double e = exp((double)lt[j]); P += e; pk[j] = (float)e; }
-                else { pk[j] = expf(dt.mode == kDistillNormalised ? lt[j] - lmax : lt[j]); P += (double)pk[j]; }
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) P += __shfl_xor_sync(0xffffffffu, P, o);
-            if (dt.mode == kDistillNormalised) {
-                const float inv = P > 0.0 ? (float)(1.0 / P) : (P == P ? 0.f : (float)P), lse = lmax + (float)log(P);
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) { pk[j] *= inv; lt[j] -= lse; }
-                P = P > 0.0 ? 1.0 : (P == P ? 0.0 : P);
-            }
-            double H = 0.0;
-            float pr[kCluster];
-#pragma unroll
-            for (int c = 0; c < kCluster; ++c) pr[c] = 0.f;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                if (!(pk[j] == 0.f)) H += (double)pk[j] * (double)lt[j];
-                const uint32_t v = pos[j] < 0 ? 0xffffffffu : (eoff + (uint32_t)pos[j]) >> 3;
-#pragma unroll
-                for (int c = 0; c < kCluster; ++c)
-                    if (v - (uint32_t)c * ca.slice_vecs < ca.slice_vecs) pr[c] += pk[j];
-                // position in this block's buffer, or -1
-                pos[j] = v - v0 < nvec ? (int)(eoff + (uint32_t)pos[j] - v0 * 8u) : -1;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                H += __shfl_xor_sync(0xffffffffu, H, o);
-#pragma unroll
-                for (int c = 0; c < kCluster; ++c) pr[c] += __shfl_xor_sync(0xffffffffu, pr[c], o);
-            }
+            float pk[kPer], pr[kCluster];
+            double P, H;
+            distill_weights<kCluster>(p, dt, entries, eoff, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
             // the logits leave the buffer.  Every entry leaves its number in its place and looks whether it is still
             // there: if not, the same entry is named twice.
             mbar_wait(landed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
@@ -626,54 +697,8 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
                 if (pos[j] >= 0) row16[pos[j]] = (uint16_t)El<kF16>::kNegInf;
                 if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; tz[lane + 32 * j] = z[j]; }
             }
-            if (__any_sync(0xffffffffu, twice)) {
-                // the first of several equal entries takes the weight of all, added in the order of the list
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const int k = lane + 32 * j, mine = pos[j];
-                    if (mine < 0) continue;
-                    for (int o = 0; o < k; ++o)
-                        if (tp[o] == mine) { pos[j] = -1; break; }
-                    if (pos[j] < 0) { pk[j] = 0.f; continue; }
-                    for (int o = k + 1; o < dt.K; ++o)
-                        if (tp[o] == mine) pk[j] += tw[o];
-                }
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; }
-            }
-            float Mt = kFloorM;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (pos[j] >= 0) Mt = fmaxf(Mt, z[j] * xscale);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) Mt = fmaxf(Mt, __shfl_xor_sync(0xffffffffu, Mt, o));
-            float ey = 0.f, zy = 0.f;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (pos[j] >= 0) {
-                    const float x = fmaf(z[j], xscale, -Mt);
-                    ey += ex2(x);
-                    if (!(pk[j] == 0.f)) zy = fmaf(pk[j], x, zy);
-                }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                ey += __shfl_xor_sync(0xffffffffu, ey, o);
-                zy += __shfl_xor_sync(0xffffffffu, zy, o);
-            }
-            if (lane == 0) {
-                TargetInfo ti;
-                ti.H = H;
-                ti.P = (float)P;
-                ti.p0 = dt.mode == kDistillTail ? (float)(1.0 - P > 0.0 ? 1.0 - P : 0.0) : 0.f;
-                ti.W = dt.mode == kDistillTail ? (float)(P > 1.0 ? P : 1.0) : (float)P;
-                if (!(P == P)) ti.W = ti.P;
-                for (int c = 0; c < 4; ++c) ti.pr[c] = c < kCluster ? pr[c < kCluster ? c : 0] : 0.f;
-                s_target[buf] = ti;
-                s_tlab[buf] = LabelInfo{zy, ey, Mt, s_target[buf].pr[crank]};
-            }
+            if (__any_sync(0xffffffffu, twice)) distill_merge(dt.K, Kpad, lane, tp, tw, pos, pk);
+            distill_publish<kCluster>(dt, xscale, crank, lane, pos, pk, z, P, H, pr, s_target[buf], s_tlab[buf]);
             __syncwarp();
             if (lane == 0) mbar_arrive(ready(buf));
         }

@@ -16,6 +16,11 @@
 // reduction, cluster exchange), and write chunk after chunk in pass 2, handing each chunk back as soon as a
 // warp is done with it.  The chunks of a slice stay in their slots from pass 1 to pass 2.
 //
+// kDistill: distillation from a teacher's entries, with a target and a patch warp as in kernels_creg.cuh.  The target warp
+// takes the entries' logits out chunk by chunk as the chunks land ("ready" per slot), the patch warp writes the entries'
+// gradients chunk by chunk as the consumers finish them ("patched" per slot, which the producer waits for).  What they hand
+// on for a row lies in one of four sets, freed by the patch warp.
+//
 // Rows are dealt as in kernels_creg.cuh: single blocks take them from the counter in the workspace (a padded
 // row is zero-filled on the spot), clusters statically.  Waits are bounded; the tensor-memory columns are
 // released by the warp that took them.
@@ -30,6 +35,7 @@ constexpr int kCringU = 2;                    // vectors per consumer thread and
 constexpr int kCringZeroBytes = 8192;         // zeroed buffer that feeds the bulk zero-fill of padded rows
 constexpr int kCringMaxSlots = 13;
 constexpr int kCringRows = 8;                 // row infos in flight (a power of two)
+constexpr int kCringTargets = 4;              // kDistill: rows whose entries are held (a power of two)
 
 struct CringArgs {
     RowArgs row;
@@ -39,12 +45,15 @@ struct CringArgs {
     int n_slots;             // R
     int chunks;              // chunks of the longest slice, at most R - 1
     unsigned* row_counter;   // workspace word, zero between calls: next row to hand out (kCluster == 1)
+    DistillArgs distill;     // kDistill
 };
 
 inline size_t cring_chunk_bytes(int consumer_warps) { return (size_t)consumer_warps * 32 * 16 * kCringU; }
-inline size_t cring_smem_bytes(int consumer_warps, int n_slots)
+// K: teacher entries per row (0: not distillation).
+inline size_t cring_smem_bytes(int consumer_warps, int n_slots, int K = 0)
 {
-    return (size_t)n_slots * cring_chunk_bytes(consumer_warps) + kCringZeroBytes + 256;
+    return (size_t)n_slots * cring_chunk_bytes(consumer_warps) + (K > 0 ? kDistillZeroBytes : kCringZeroBytes) + 256 +
+           12 * (size_t)distill_pad(K) * kCringTargets;
 }
 
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
@@ -66,13 +75,14 @@ __device__ __forceinline__ void bulk_wait_read_upto(uint32_t n)
     else asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
 }
 
-template <int NW, int kCluster, bool kF16>
-__global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs ca)
+template <int NW, int kCluster, bool kF16, bool kDistill = false>
+__global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_kernel(CringArgs ca)
 {
     constexpr int kRegVecs = kRegVecsTmem;                   // the first two chunks' exponentials stay in registers
     static_assert(kRegVecs == 2 * kCringU, "two chunks in registers");
     constexpr int kCons = NW * 32;
-    constexpr int kThreads = kCons + 32;
+    constexpr int kThreads = kCons + (kDistill ? 96 : 32);
+    constexpr int kZeroBytesHere = kDistill ? kDistillZeroBytes : kCringZeroBytes;
     constexpr uint32_t kChunk = (uint32_t)kCons * 16u * kCringU;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ long long s_cnt[33];
@@ -86,8 +96,15 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
     __shared__ __align__(16) float4 s_xchg[2][kCluster];     // per row parity: (M, s, ey, zy) of every block of the cluster
     __shared__ __align__(8) unsigned long long s_xbar[2];
     __shared__ uint32_t s_tmem_base;
+    // kDistill: barriers ready / patched of every slot, announced of every row info, told / spare of every set of entries
+    __shared__ __align__(8) unsigned long long s_dbar[kDistill ? 2 * kCringMaxSlots + kCringRows + 2 * kCringTargets : 1];
+    __shared__ TargetInfo s_target[kDistill ? kCringTargets : 1];
+    __shared__ LabelInfo s_tlab[kDistill ? kCringTargets : 1];
+    __shared__ float4 s_total[kDistill ? kCringTargets : 1];
 
     const RowArgs& p = ca.row;
+    const DistillArgs& dt = ca.distill;
+    const float xscale = kDistill ? dt.scale : kLog2e;       // logit -> base-2 exponent
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int R = ca.n_slots;
     const uint32_t crank = kCluster > 1 ? cluster_ctarank() : 0u;
@@ -101,10 +118,20 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
 
     const uint32_t ring_addr = smem_u32(smem);
     unsigned char* zero_buf = smem + (size_t)R * kChunk;
-    const uint32_t bar_addr = smem_u32(zero_buf + kCringZeroBytes);
+    const uint32_t bar_addr = smem_u32(zero_buf + kZeroBytesHere);
     auto full = [&](int s) { return bar_addr + 8u * s; };
     auto done = [&](int s) { return bar_addr + 8u * (kCringMaxSlots + s); };
     const uint32_t xbar_addr = smem_u32(s_xbar);
+    const uint32_t dbar = smem_u32(s_dbar);
+    auto ready = [&](int slot) { return dbar + 8u * slot; };
+    auto patched = [&](int slot) { return dbar + 8u * (kCringMaxSlots + slot); };
+    auto announced = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + (i & (kCringRows - 1))); };
+    auto told = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + kCringRows + (i & (kCringTargets - 1))); };
+    auto spare = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + kCringRows + kCringTargets + (i & (kCringTargets - 1))); };
+    auto finished = [&](int slot) { return kDistill ? patched(slot) : done(slot); };
+    const int Kpad = kDistill ? (dt.K + 31) / 32 * 32 : 0;
+    // a row's teacher entries: position in the slice (or -1), weight, logit
+    auto t_pos = [&](int i) { return (int*)(zero_buf + kZeroBytesHere + 256) + 3 * (i & (kCringTargets - 1)) * Kpad; };
     static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     static_assert(2 * kCringMaxSlots * 8 <= 256, "the slots' mbarriers take the 256 bytes after the zero buffer");
 
@@ -112,13 +139,22 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
         for (int s = 0; s < R; ++s) {
             mbar_init(full(s), 1);
             mbar_init(done(s), NW);
+            if (kDistill) {
+                mbar_init(ready(s), 1);
+                mbar_init(patched(s), 1);
+            }
+        }
+        for (int i = 0; kDistill && i < kCringRows; ++i) mbar_init(announced(i), 1);
+        for (int i = 0; kDistill && i < kCringTargets; ++i) {
+            mbar_init(told(i), 1);
+            mbar_init(spare(i), 1);
         }
         mbar_init(xbar_addr, 1);
         mbar_init(xbar_addr + 8u, 1);
         fence_mbar_init();
     }
     if (warp == 0) tmem_alloc(smem_u32(&s_tmem_base), ca.tmem_cols);
-    for (int i = tid; i < kCringZeroBytes / 16; i += kThreads) ((uint4*)zero_buf)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < kZeroBytesHere / 16; i += kThreads) ((uint4*)zero_buf)[i] = make_uint4(0, 0, 0, 0);
     fence_async_smem();
     tmem_fence_before_sync();
     __syncthreads();
@@ -148,8 +184,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
             uint32_t sseq[4] = {0, 0, 0, 0};  // seq of the store of chunk d, at d & 3, for the last four chunks stored
             auto zero_fill_row = [&](int b, int t) {
                 unsigned char* drow = (unsigned char*)(p.dlogits + (long long)b * p.dl_stride_b + (long long)t * p.dl_stride_t) + slice_off;
-                for (uint32_t off = 0; off < slice_bytes; off += kCringZeroBytes)
-                    bulk_store(drow + off, smem_u32(zero_buf), min((uint32_t)kCringZeroBytes, slice_bytes - off));
+                for (uint32_t off = 0; off < slice_bytes; off += kZeroBytesHere)
+                    bulk_store(drow + off, smem_u32(zero_buf), min((uint32_t)kZeroBytesHere, slice_bytes - off));
                 bulk_commit();
                 ++seq;
             };
@@ -176,12 +212,12 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 const long long need = g - R;
                 if (need < 0) return;
                 while (d_idx <= need && !aborted) {
-                    mbar_wait(done(d_slot), d_ph, p.status, aborted, p.wait_limit_ns);
+                    mbar_wait(finished(d_slot), d_ph, p.status, aborted, p.wait_limit_ns);
                     if (!aborted) store_next();
                 }
                 if (aborted) return;
                 // chunks that are done already go out too, so that their stores overlap this one's
-                while (d_idx <= need + 2 && d_idx < g && mbar_test(done(d_slot), d_ph)) store_next();
+                while (d_idx <= need + 2 && d_idx < g && mbar_test(finished(d_slot), d_ph)) store_next();
                 bulk_wait_read_upto(min(seq - sseq[need & 3], 3u));
             };
             // The rows: single blocks take the next row of the row-major list of all rows from a counter (a padded row
@@ -214,8 +250,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 }
                 if (a.ok) {
                     const long long f = (long long)a.b * p.T + a.t;
-                    a.y = __ldg(p.ids + (long long)a.b * p.ids_stride_b + a.t);
-                    a.sc = load_row_scalars(p, a.b, a.t, f);
+                    a.y = kDistill ? 0 : __ldg(p.ids + (long long)a.b * p.ids_stride_b + a.t);
+                    if (!kDistill) a.sc = load_row_scalars(p, a.b, a.t, f);
                 }
                 return a;
             };
@@ -236,7 +272,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 ri.dl_offset = (long long)b * p.dl_stride_b + (long long)t * p.dl_stride_t;
                 ri.bad_id = (a.y < 0 || a.y >= p.V) ? 1 : 0;
                 ri.y = ri.bad_id ? 0 : (int)a.y;
-                ri.sc = a.sc;
+                if (!kDistill) ri.sc = a.sc;
+                ri.entries = kDistill ? (long long)b * dt.stride_b + (long long)t * dt.stride_t : 0;
                 ri.mis = 0;
                 ri.pad = 0;
                 if (ri.bad_id && crank == 0) atomicOr(p.status, kErrIdRange);
@@ -244,7 +281,10 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 for (int c = 0; c < C && !aborted; ++c, ++g) {
                     ensure_free(g);
                     if (aborted) break;
-                    if (c == 0) s_row[i & (kCringRows - 1)] = ri;       // published by the arrival below
+                    if (c == 0) {
+                        s_row[i & (kCringRows - 1)] = ri;               // published by the arrivals below
+                        if (kDistill) mbar_arrive(announced(i));
+                    }
                     const uint32_t bytes = c == C - 1 ? last_bytes : kChunk;
                     mbar_arrive_expect_tx(full(l_slot), bytes);
                     bulk_load(ring_addr + (uint32_t)l_slot * kChunk, row + (size_t)c * kChunk, bytes, full(l_slot));
@@ -261,16 +301,138 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 ensure_free(g);
                 if (!aborted) {
                     s_row[i & (kCringRows - 1)].flat = -1;
+                    if (kDistill) mbar_arrive(announced(i));
                     mbar_arrive_expect_tx(full(l_slot), 0);
                 }
             }
             while (d_idx < g && !aborted) {
-                mbar_wait(done(d_slot), d_ph, p.status, aborted, p.wait_limit_ns);
+                mbar_wait(finished(d_slot), d_ph, p.status, aborted, p.wait_limit_ns);
                 if (!aborted) store_next();
             }
             bulk_wait_all();
         }
         if (kCluster > 1) cluster_sync_unaligned();                     // no block leaves while a peer may still write to it
+        return;
+    }
+
+    constexpr int kChunkEntries = (int)(kChunk / 2);
+    if (kDistill && warp == NW + 1) {
+        // ------------------------------------------------------------ target warp
+        int slot = 0;
+        uint32_t ph = 0;
+        for (int i = 0; !aborted && nvec > 0; ++i) {
+            mbar_wait(announced(i), (uint32_t)(i / kCringRows) & 1u, p.status, aborted, p.wait_limit_ns);
+            // the set's previous row has been patched (nothing to wait for in the first turn)
+            mbar_wait(spare(i), ((uint32_t)(i / kCringTargets) & 1u) ^ 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+            if (aborted) break;
+            const RowInfo& ri = s_row[i & (kCringRows - 1)];
+            if (ri.flat < 0) break;
+            int pos[kPer];
+            float pk[kPer], pr[kCluster], z[kPer];
+            double P, H;
+            distill_weights<kCluster>(p, dt, ri.entries, 0u, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
+            int* tp = t_pos(i);
+            float *tw = (float*)tp + Kpad, *tz = (float*)tp + 2 * Kpad;
+            // the logits leave the chunks; every entry leaves its number in its place and looks whether it is still there:
+            // if not, the same entry is named twice
+            bool twice = false;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) z[j] = 0.f;
+            for (int c = 0; c < C; ++c) {
+                mbar_wait(full(slot), ph, p.status, aborted, p.wait_limit_ns);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted) break;
+                uint16_t* chunk16 = (uint16_t*)(smem + (size_t)slot * kChunk);
+                bool any = false;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) any |= pos[j] >= 0 && pos[j] / kChunkEntries == c;
+                if (__any_sync(0xffffffffu, any)) {
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c) z[j] = El<kF16>::widen(chunk16[pos[j] % kChunkEntries]);
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)(lane + 32 * j);
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c)
+                            twice |= chunk16[pos[j] % kChunkEntries] != (uint16_t)(lane + 32 * j);
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)El<kF16>::kNegInf;
+                    __syncwarp();
+                }
+                if (lane == 0) mbar_arrive(ready(slot));
+                if (++slot == R) { slot = 0; ph ^= 1u; }
+            }
+            if (aborted) break;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; tz[lane + 32 * j] = z[j]; }
+            if (__any_sync(0xffffffffu, twice)) distill_merge(dt.K, Kpad, lane, tp, tw, pos, pk);
+            distill_publish<kCluster>(dt, xscale, crank, lane, pos, pk, z, P, H, pr, s_target[i & (kCringTargets - 1)],
+                                      s_tlab[i & (kCringTargets - 1)]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(told(i));
+        }
+        return;
+    }
+
+    if (kDistill && warp == NW + 2) {
+        // ------------------------------------------------------------ patch warp
+        const float row_scale = N > 0 ? p.grad_scale * dt.tau / (float)N : 0.f;
+        int slot = 0;
+        uint32_t ph = 0;
+        for (int i = 0; !aborted && nvec > 0; ++i) {
+            mbar_wait(done(slot), ph, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+            if (aborted) break;
+            const long long flat = s_row[i & (kCringRows - 1)].flat;
+            if (flat < 0) break;
+            const float4 tot = s_total[i & (kCringTargets - 1)];     // M, mass outside, mass of the entries, sum p (x - M)
+            const TargetInfo ti = s_target[i & (kCringTargets - 1)];
+            const float l2 = log2f(tot.y + tot.z);
+            const int* tp = t_pos(i);
+            int pos[kPer];
+            uint32_t value[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int k = lane + 32 * j;
+                pos[j] = k < dt.K ? tp[k] : -1;
+                value[j] = 0;
+                if (pos[j] >= 0) {
+                    const float q = ex2(fmaf(((const float*)tp)[2 * Kpad + k], xscale, -tot.x) - l2);
+                    value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -((const float*)tp)[Kpad + k]), 0.f) & 0xffffu;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(spare(i));                    // the set has been read
+            for (int c = 0; c < C; ++c) {
+                if (c > 0) mbar_wait(done(slot), ph, p.status, aborted, p.wait_limit_ns);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted) break;
+                uint16_t* chunk16 = (uint16_t*)(smem + (size_t)slot * kChunk);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)value[j];
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(patched(slot));
+                if (++slot == R) { slot = 0; ph ^= 1u; }
+            }
+            if (aborted) break;
+            if (lane == 0 && crank == 0) {
+                const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot.w, tot.y, tot.z));
+                p.row_loss[flat] = L;
+                if (p.out_lp_new) p.out_lp_new[flat] = L;
+            }
+        }
+        __threadfence();
+        asm volatile("bar.sync 2, %0;" ::"n"(kCons + 32) : "memory");   // the row losses are written
         return;
     }
 
@@ -299,22 +461,26 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
         aborted = __any_sync(0xffffffffu, aborted);                 // a warp gives up as a whole
         RowInfo ri = s_row[i & (kCringRows - 1)];
         if (aborted) { ri.y = 0; ri.bad_id = 1; ri.flat = 0; }      // stale row info: touch nothing
-        if (ri.flat < 0) break;                                      // the producer has no more rows (the same for every thread)
+        if (ri.flat < 0) {                                           // the producer has no more rows (the same for every thread)
+            if (kDistill && lane == 0) mbar_arrive(done(s0));        // tells the patch warp
+            break;
+        }
 
         // where the generated token sits: vector ylocal of this slice (if < nvec), entry yj
         const uint32_t ylocal = ((uint32_t)ri.y >> 3) - v0;
         const int yj = ri.y & 7;
-        const bool label_here = ylocal < nvec;
+        const bool label_here = !kDistill && ylocal < nvec;
         const bool owner = label_here && (ylocal % kCons) == (uint32_t)tid;
         const int jy = owner ? (int)(ylocal / kCons) : -1;
 
         // The reference exponent: the scaled maximum of the slice's first vector, which every thread reads,
         // without the generated token's entry.
         float Mref;
+        if (kDistill) mbar_wait(ready(s0), ph0, p.status, aborted, p.wait_limit_ns);
         {
             uint4 q0 = *(const uint4*)(smem + (size_t)s0 * kChunk);
             if (label_here && ylocal == 0) q0 = mask_vec_entry<kF16>(q0, yj);
-            Mref = max8_scaled<kF16>(q0);
+            Mref = max8_scaled<kF16>(q0, xscale);
         }
         // This thread's vector j, the generated token's entry taken out (it becomes -inf, a term of 0), so that
         // the sums below are sums over the other entries and 1 - p_y comes without cancellation.
@@ -335,7 +501,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const float2 x = __ffma2_rn(El<kF16>::unpack2(w[h]), splat2(kLog2e), splat2(negM));
+                const float2 x = __ffma2_rn(El<kF16>::unpack2(w[h]), splat2(xscale), splat2(negM));
                 ev[h] = make_float2(ex2(x.x), ex2(x.y));
             }
         };
@@ -348,6 +514,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 mbar_wait(full(slot_of(c)), phase_of(c), p.status, aborted, p.wait_limit_ns);
+                if (kDistill) mbar_wait(ready(slot_of(c)), phase_of(c), p.status, aborted, p.wait_limit_ns);
                 const unsigned char* chunk = smem + (size_t)slot_of(c) * kChunk;
 #pragma unroll
                 for (int u = 0; u < kCringU; ++u) {
@@ -361,6 +528,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
             }
             auto to_tmem = [&](auto last, int c) {
                 mbar_wait(full(slot_of(c)), phase_of(c), p.status, aborted, p.wait_limit_ns);
+                if (kDistill) mbar_wait(ready(slot_of(c)), phase_of(c), p.status, aborted, p.wait_limit_ns);
                 const unsigned char* chunk = smem + (size_t)slot_of(c) * kChunk;
 #pragma unroll
                 for (int u = 0; u < kCringU; ++u) {
@@ -394,15 +562,17 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 for (int c = 0; c < C; ++c)
                     for (int u = 0; u < kCringU; ++u)
                         if (valid(c * kCringU + u))
-                            m = fmaxf(m, max8_scaled<kF16>(((const uint4*)(smem + (size_t)slot_of(c) * kChunk))[u * kCons + tid]));
+                            m = fmaxf(m, max8_scaled<kF16>(((const uint4*)(smem + (size_t)slot_of(c) * kChunk))[u * kCons + tid], xscale));
                 M = m;
             }
         }
+        if (kDistill) mbar_wait(told(i), (uint32_t)(i / kCringTargets) & 1u, p.status, aborted, p.wait_limit_ns);
         aborted = __any_sync(0xffffffffu, aborted);
         if (!valid(0) && !owner) { M = Mref; vs = 0.f; }
         const bool diverged = M != Mref;
 
-        if (label_here ? owner : tid == 0)
+        const int ts = i & (kCringTargets - 1);                      // kDistill: the row's set of entries
+        if (!kDistill && (label_here ? owner : tid == 0))
             s_lab[par] = label_here ? LabelInfo{zy, ex2(fmaf(zy, kLog2e, -M)), M, 0.f} : LabelInfo{0.f, 0.f, kFloorM, 0.f};
         float ws = vs;
 #pragma unroll
@@ -412,13 +582,21 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
         if (!consumer_barrier_or<NW>(diverged || aborted)) {
             tot.M = Mref;
             tot.s = sum_warp_sums<NW>(s_sum[par]);
-            tot.ey = s_lab[par].ey;
+            if (kDistill) {
+                const LabelInfo li = s_tlab[ts];
+                tot.M = fmaxf(Mref, li.M);
+                tot.s *= ex2(Mref - tot.M);
+                tot.ey = li.ey * ex2(li.M - tot.M);
+            } else {
+                tot.ey = s_lab[par].ey;
+            }
         } else {
             // a wait that ran out somewhere in the block ends the block's work here, for all its threads alike
             if (consumer_barrier_or<NW>(aborted)) { aborted = true; break; }
-            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], &s_lab[par], warp, lane);
+            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], kDistill ? &s_tlab[ts] : &s_lab[par], warp, lane);
         }
-        float zy_row = s_lab[par].zy;
+        // the generated token's logit; kDistill: sum over the slice's teacher entries of p (x - M), M the total's reference
+        float zy_row = kDistill ? fmaf(s_tlab[ts].pad, s_tlab[ts].M - tot.M, s_tlab[ts].zy) : s_lab[par].zy;
 
         if (kCluster > 1) {
             // every block of the cluster sends its slice's (M, s, ey, zy) to every block, itself included
@@ -443,7 +621,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
                 const float sc = ex2(part.x - Mx);
                 sx = fmaf(part.y, sc, sx);
                 eyx = fmaf(part.z, sc, eyx);
-                zx += part.w;
+                zx += kDistill ? fmaf(s_target[ts].pr[r], part.x - Mx, part.w) : part.w;
             }
             tot = Acc{Mx, sx, eyx};
             zy_row = zx;
@@ -451,8 +629,13 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
         RowResult r = row_finish_fast(tot, zy_row);
 
         float loss = 0.f, kl = 0.f, g = 0.f;
-        if (!ri.bad_id) row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
-        if (tid == 0 && crank == 0 && !aborted) {
+        if (kDistill) {
+            g = -(scale_over_N * dt.tau) * distill_factor(s_target[ts], tot.s, r.one_m_py);
+            if (tid == 0) s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+        } else if (!ri.bad_id) {
+            row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
+        }
+        if (!kDistill && tid == 0 && crank == 0 && !aborted) {
             if (p.row_loss) p.row_loss[ri.flat] = loss;
             if (p.row_kl) p.row_kl[ri.flat] = kl;
             if (p.out_lp_new) p.out_lp_new[ri.flat] = ri.bad_id ? 0.f : r.lp;
@@ -517,6 +700,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, 1) loss_cring_kernel(CringArgs c
     // The two losses.  Every block leaves its share of the value loss in the workspace; the block that finishes last
     // adds the per-token policy terms (and KL terms, where the objective has them) of the whole batch (all its consumer
     // threads, fixed shares, fixed tree) and the blocks' value-loss shares in block order.
+    if (kDistill) asm volatile("bar.sync 2, %0;" ::"n"(kCons + 32) : "memory");   // the patch warp has written the row losses
     if (p.fused) {
         if (tid == 0) {
             p.partials[2 * blockIdx.x] = 0.0;
