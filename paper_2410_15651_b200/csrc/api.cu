@@ -232,7 +232,7 @@ int creg_resident_clusters(const CregPlan& pl, const DeviceInfo& dev, int& out)
         int n = 0;
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
-        fill_launch_config(cfg, attr, dev.sm_count / C * C, NW * 32 + (kDistill ? 96 : 32), pl.smem_bytes, C, nullptr);
+        fill_launch_config(cfg, attr, dev.sm_count / C * C, NW * 32 + (kDistill ? 128 : 32), pl.smem_bytes, C, nullptr);
         RLHF_CUDA(cudaOccupancyMaxActiveClusters(&n, loss_creg_kernel<NW, C, kTmem, kF16, kAny, kDistill>, &cfg));
         if (n < 1) n = 1;
         if (d < 0 || d >= 64) { out = n; return RLHF_OK; }
@@ -260,7 +260,7 @@ int launch_creg(const RowArgs& a, const CregPlan& pl, const DeviceInfo& dev, cud
     if (int e = creg_resident_clusters<NW, C, kTmem, kF16, kAny, kDistill>(pl, dev, clusters)) return e;
     const long long rows = (long long)a.B * a.T;
     const int grid = (int)std::min<long long>(rows, clusters) * C;
-    RLHF_CUDA(launch_kernel_cluster(kernel, grid, NW * 32 + (kDistill ? 96 : 32), pl.smem_bytes, C, s, ca));
+    RLHF_CUDA(launch_kernel_cluster(kernel, grid, NW * 32 + (kDistill ? 128 : 32), pl.smem_bytes, C, s, ca));
     return RLHF_OK;
 }
 
@@ -317,7 +317,7 @@ CringPlan plan_cring(unsigned row_bytes, const DeviceInfo& dev, int K = 0)
 template <int C, bool kF16, bool kDistill = false>
 int launch_cring(const RowArgs& a, const CringPlan& pl, const DeviceInfo& dev, cudaStream_t s, const DistillArgs& dt = DistillArgs{})
 {
-    constexpr int NW = kCregWarps, kThreads = NW * 32 + (kDistill ? 96 : 32);
+    constexpr int NW = kCregWarps, kThreads = NW * 32 + (kDistill ? 128 : 32);
     auto kernel = loss_cring_kernel<NW, C, kF16, kDistill>;
     CringArgs ca{};
     ca.distill = dt;
@@ -610,6 +610,7 @@ int launch_logprobs(const RowArgs& a, float* out_lp, bool f16, const DeviceInfo&
     WarpArgs wa{};
     wa.row = a;
     wa.row.out_lp = out_lp;
+    wa.relative = 1;
     if (rows_16B(a.logits, a.stride_b, a.stride_t, a.V)) {
         if (int e = launch_warp_logprob<false, false>(wa, f16, dev, s)) return e;
     } else {

@@ -42,8 +42,8 @@
 // have passed a block barrier at the end of the kernel.
 //
 // kDistill: the row's loss is distillation from up to 256 teacher entries instead of an objective of one generated
-// token.  Two more warps serve it.  The target warp turns the entries of a row into weights while the row is still on
-// its way, then takes the logits of those entries out of the buffer (they become -inf, as the generated token's does
+// token.  Three more warps serve it.  Two target warps, in turn, turn the entries of a row into weights while the row is
+// still on its way, then take the logits of those entries out of the buffer (they become -inf, as the generated token's does
 // above, so that the sum over the other entries -- the student's mass outside the teacher's entries -- comes without
 // cancellation).  The consumers' two passes are as above, with one factor for all entries that are not the teacher's.
 // The patch warp then writes the gradients of the teacher's entries into the finished buffer and forms the row's loss,
@@ -136,14 +136,22 @@ __device__ __forceinline__ float distill_factor(const TargetInfo& ti, float s, f
     return ti.p0 > 0.f && s > 0.f ? ti.W - ti.p0 / q0 : ti.P;
 }
 
+// log2 of a positive fp32 number to 2^-24: the exponent exactly, the mantissa's logarithm (below 1) in fp32.
+__device__ __forceinline__ double log2_split(float v)
+{
+    int e;
+    const float m = frexpf(v, &e);                           // in [1/2, 1)
+    return (double)e + (double)log2f(m);
+}
+
 // Loss of a row.  With x the scaled logits and M a reference, zy = sum_k p_k (x_k - M); s and ey are the sums of 2^(x-M)
 // over the other and over the teacher's entries.
-__device__ inline double distill_loss(const TargetInfo& ti, float zy, float s, float ey)
+__device__ __forceinline__ double distill_loss(const TargetInfo& ti, float zy, float s, float ey)
 {
     constexpr double ln2 = 0.6931471805599453;
-    const double l2 = log2((double)s + (double)ey);
+    const double l2 = log2_split(s + ey);
     double L = ti.H - ln2 * ((double)zy - (double)ti.P * l2);
-    if (ti.p0 > 0.f && s > 0.f) L += (double)ti.p0 * (log((double)ti.p0) - ln2 * (log2((double)s) - l2));
+    if (ti.p0 > 0.f && s > 0.f) L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (log2_split(s) - l2));
     return L;
 }
 
@@ -306,7 +314,7 @@ __device__ __forceinline__ void distill_weights(const RowArgs& p, const DistillA
         const int k = lane + 32 * j;
         pos[j] = -1;
         lt[j] = __uint_as_float(0xff800000u);
-        if (k < dt.K) {
+        if (32 * j < dt.K && k < dt.K) {
             pos[j] = __ldg(dt.ids + entries + k);
             lt[j] = __ldg(dt.logprobs + entries + k);
             bad |= pos[j] < -1 || pos[j] >= p.V;
@@ -333,7 +341,8 @@ __device__ __forceinline__ void distill_weights(const RowArgs& p, const DistillA
     if (dt.mode == kDistillNormalised) {
         const float inv = P > 0.0 ? (float)(1.0 / P) : (P == P ? 0.f : (float)P), lse = lmax + (float)log(P);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) { pk[j] *= inv; lt[j] -= lse; }
+        for (int j = 0; j < kPer; ++j)
+            if (32 * j < dt.K) { pk[j] *= inv; lt[j] -= lse; }
         P = P > 0.0 ? 1.0 : (P == P ? 0.0 : P);
     }
     H = 0.0;
@@ -341,6 +350,7 @@ __device__ __forceinline__ void distill_weights(const RowArgs& p, const DistillA
     for (int c = 0; c < kCluster; ++c) pr[c] = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
+        if (32 * j >= dt.K) continue;
         if (!(pk[j] == 0.f)) H += (double)pk[j] * (double)lt[j];
         const uint32_t v = pos[j] < 0 ? 0xffffffffu : (eoff + (uint32_t)pos[j]) >> 3;
 #pragma unroll
@@ -386,13 +396,13 @@ __device__ __forceinline__ void distill_publish(const DistillArgs& dt, float xsc
     float Mt = kFloorM;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (pos[j] >= 0) Mt = fmaxf(Mt, z[j] * xscale);
+        if (32 * j < dt.K && pos[j] >= 0) Mt = fmaxf(Mt, z[j] * xscale);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Mt = fmaxf(Mt, __shfl_xor_sync(0xffffffffu, Mt, o));
     float ey = 0.f, zy = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (pos[j] >= 0) {
+        if (32 * j < dt.K && pos[j] >= 0) {
             const float x = fmaf(z[j], xscale, -Mt);
             ey += ex2(x);
             if (!(pk[j] == 0.f)) zy = fmaf(pk[j], x, zy);
@@ -425,12 +435,12 @@ __device__ __forceinline__ void distill_publish(const DistillArgs& dt, float xsc
 // ends by 2-byte stores.
 // kDistill: see the head of the file.
 template <int NW, int kCluster, bool kTmem, bool kF16, bool kAny = false, bool kDistill = false>
-__global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_kernel(CregArgs ca)
+__global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_kernel(CregArgs ca)
 {
     static_assert(!kAny || kCluster == 1, "rows off 16-byte boundaries are not split over a cluster");
     constexpr int kRegVecs = kTmem ? kRegVecsTmem : kRegVecsOnly;
     constexpr int kCons = NW * 32;
-    constexpr int kThreads = kCons + (kDistill ? 96 : 32);
+    constexpr int kThreads = kCons + (kDistill ? 128 : 32);
     constexpr int kZeroBytesHere = kDistill ? kDistillZeroBytes : kCregZeroBytes;
     constexpr uint32_t kPiece = RLHF_CREG_PIECE;  // size of one bulk copy
     extern __shared__ __align__(128) unsigned char smem[];
@@ -649,15 +659,19 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
                 }
             }
             for (int j = i + 1 >= NB ? i + 1 - NB : 0; j < i && !aborted; ++j) drain(j);
+            if (kDistill && !aborted) {                                // the other target warp waits for the row after the last
+                s_row[(i + 1) % NB].flat = -1;
+                mbar_arrive(announced((i + 1) % NB));
+            }
             bulk_wait_all();
             if (kCluster > 1) cluster_sync_unaligned();                 // no block leaves while a peer may still write to it
         }
         return;
     }
 
-    if (kDistill && warp == NW + 1) {
-        // ------------------------------------------------------------ target warp
-        for (int i = 0; !aborted; ++i) {
+    if (kDistill && (warp == NW + 1 || warp == NW + 2)) {
+        // ------------------------------------------------------------ target warps: one for every other row
+        for (int i = warp - (NW + 1); !aborted; i += 2) {
             const int buf = i % NB;
             mbar_wait(announced(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
@@ -682,20 +696,25 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
             float *tw = t_p(buf), *tz = t_z(buf);
             float z[kPer];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) z[j] = pos[j] >= 0 ? El<kF16>::widen(row16[pos[j]]) : 0.f;
+            for (int j = 0; j < kPer; ++j) {
+                z[j] = 0.f;
+                if (32 * j < dt.K && pos[j] >= 0) z[j] = El<kF16>::widen(row16[pos[j]]);
+            }
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
-                if (pos[j] >= 0) row16[pos[j]] = (uint16_t)(lane + 32 * j);
+                if (32 * j < dt.K && pos[j] >= 0) row16[pos[j]] = (uint16_t)(lane + 32 * j);
             __syncwarp();
             bool twice = false;
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) twice |= pos[j] >= 0 && row16[pos[j]] != (uint16_t)(lane + 32 * j);
+            for (int j = 0; j < kPer; ++j)
+                if (32 * j < dt.K && pos[j] >= 0) twice |= row16[pos[j]] != (uint16_t)(lane + 32 * j);
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
+                if (32 * j >= dt.K) break;
                 if (pos[j] >= 0) row16[pos[j]] = (uint16_t)El<kF16>::kNegInf;
-                if (32 * j < Kpad) { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; tz[lane + 32 * j] = z[j]; }
+                { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; tz[lane + 32 * j] = z[j]; }
             }
             if (__any_sync(0xffffffffu, twice)) distill_merge(dt.K, Kpad, lane, tp, tw, pos, pk);
             distill_publish<kCluster>(dt, xscale, crank, lane, pos, pk, z, P, H, pr, s_target[buf], s_tlab[buf]);
@@ -705,7 +724,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
         return;
     }
 
-    if (kDistill && warp == NW + 2) {
+    if (kDistill && warp == NW + 3) {
         // ------------------------------------------------------------ patch warp
         const float row_scale = N > 0 ? p.grad_scale * dt.tau / (float)N : 0.f;
         for (int i = 0; !aborted; ++i) {
@@ -932,13 +951,26 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
             g = -(scale_over_N * dt.tau) * distill_factor(s_target[buf], tot.s, r.one_m_py);
             if (tid == 0) s_total[buf] = make_float4(tot.M, tot.s, tot.ey, zy_row);
         } else if (!ri.bad_id) {
-            row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
+            if (p.objective == kObjPolicyKl) g = policy_gradient(p, ri.sc, policy_term<true>(p, ri.sc, tot, zy_row), scale_over_N);
+            else row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
         }
-        if (!kDistill && tid == 0 && crank == 0 && !aborted) {
+        if (!kDistill && p.objective != kObjPolicyKl && tid == 0 && crank == 0 && !aborted) {
             if (p.row_loss) p.row_loss[ri.flat] = loss;
-            if (p.row_kl) p.row_kl[ri.flat] = kl;
             if (p.out_lp_new) p.out_lp_new[ri.flat] = ri.bad_id ? 0.f : r.lp;
         }
+        // the policy loss with KL: its terms are formed by one thread, when the block has its gradient
+        auto write_terms = [&]() {
+            if (kDistill || p.objective != kObjPolicyKl || tid != 0 || crank != 0 || aborted) return;
+            float lp = 0.f;
+            if (!ri.bad_id) {
+                const PolicyTerm q = policy_term<false>(p, ri.sc, tot, zy_row);
+                policy_loss_terms(p, ri.sc, q, loss, kl);
+                lp = q.lp;
+            }
+            p.row_loss[ri.flat] = loss;
+            p.row_kl[ri.flat] = kl;
+            if (p.out_lp_new) p.out_lp_new[ri.flat] = lp;
+        };
 
         // ---- pass 2: gradient = exponential * (-g / sum), written over the logits in the buffer
         uint4* dst = (uint4*)rowbuf + tid;
@@ -973,6 +1005,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_creg_k
         fence_async_smem();                                         // this thread's writes, before the bulk store reads them
         __syncwarp();
         if (lane == 0) mbar_arrive(computed(buf));
+        write_terms();
     }
     // The two losses.  Every block leaves its share of the value loss in the workspace; the block that finishes last
     // adds the per-token policy terms (and KL terms, where the objective has them) of the whole batch (all its consumer

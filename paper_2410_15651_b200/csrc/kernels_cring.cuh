@@ -16,7 +16,7 @@
 // reduction, cluster exchange), and write chunk after chunk in pass 2, handing each chunk back as soon as a
 // warp is done with it.  The chunks of a slice stay in their slots from pass 1 to pass 2.
 //
-// kDistill: distillation from a teacher's entries, with a target and a patch warp as in kernels_creg.cuh.  The target warp
+// kDistill: distillation from a teacher's entries, with two target warps and a patch warp as in kernels_creg.cuh.  A target warp
 // takes the entries' logits out chunk by chunk as the chunks land ("ready" per slot), the patch warp writes the entries'
 // gradients chunk by chunk as the consumers finish them ("patched" per slot, which the producer waits for).  What they hand
 // on for a row lies in one of four sets, freed by the patch warp.
@@ -76,12 +76,12 @@ __device__ __forceinline__ void bulk_wait_read_upto(uint32_t n)
 }
 
 template <int NW, int kCluster, bool kF16, bool kDistill = false>
-__global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_kernel(CringArgs ca)
+__global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring_kernel(CringArgs ca)
 {
     constexpr int kRegVecs = kRegVecsTmem;                   // the first two chunks' exponentials stay in registers
     static_assert(kRegVecs == 2 * kCringU, "two chunks in registers");
     constexpr int kCons = NW * 32;
-    constexpr int kThreads = kCons + (kDistill ? 96 : 32);
+    constexpr int kThreads = kCons + (kDistill ? 128 : 32);
     constexpr int kZeroBytesHere = kDistill ? kDistillZeroBytes : kCringZeroBytes;
     constexpr uint32_t kChunk = (uint32_t)kCons * 16u * kCringU;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -301,7 +301,11 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
                 ensure_free(g);
                 if (!aborted) {
                     s_row[i & (kCringRows - 1)].flat = -1;
-                    if (kDistill) mbar_arrive(announced(i));
+                    if (kDistill) {
+                        mbar_arrive(announced(i));
+                        s_row[(i + 1) & (kCringRows - 1)].flat = -1;    // the other target warp waits for the row after the last
+                        mbar_arrive(announced(i + 1));
+                    }
                     mbar_arrive_expect_tx(full(l_slot), 0);
                 }
             }
@@ -316,11 +320,9 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
     }
 
     constexpr int kChunkEntries = (int)(kChunk / 2);
-    if (kDistill && warp == NW + 1) {
-        // ------------------------------------------------------------ target warp
-        int slot = 0;
-        uint32_t ph = 0;
-        for (int i = 0; !aborted && nvec > 0; ++i) {
+    if (kDistill && (warp == NW + 1 || warp == NW + 2)) {
+        // ------------------------------------------------------------ target warps: one for every other row
+        for (int i = warp - (NW + 1); !aborted && nvec > 0; i += 2) {
             mbar_wait(announced(i), (uint32_t)(i / kCringRows) & 1u, p.status, aborted, p.wait_limit_ns);
             // the set's previous row has been patched (nothing to wait for in the first turn)
             mbar_wait(spare(i), ((uint32_t)(i / kCringTargets) & 1u) ^ 1u, p.status, aborted, p.wait_limit_ns);
@@ -339,6 +341,9 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
             bool twice = false;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) z[j] = 0.f;
+            const long long g0 = (long long)i * C;                   // the row's first chunk
+            int slot = (int)(g0 % R);
+            uint32_t ph = (uint32_t)(g0 / R) & 1u;
             for (int c = 0; c < C; ++c) {
                 mbar_wait(full(slot), ph, p.status, aborted, p.wait_limit_ns);
                 aborted = __any_sync(0xffffffffu, aborted);
@@ -346,24 +351,25 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
                 uint16_t* chunk16 = (uint16_t*)(smem + (size_t)slot * kChunk);
                 bool any = false;
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) any |= pos[j] >= 0 && pos[j] / kChunkEntries == c;
+                for (int j = 0; j < kPer; ++j)
+                    if (32 * j < dt.K) any |= pos[j] >= 0 && pos[j] / kChunkEntries == c;
                 if (__any_sync(0xffffffffu, any)) {
 #pragma unroll
                     for (int j = 0; j < kPer; ++j)
-                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c) z[j] = El<kF16>::widen(chunk16[pos[j] % kChunkEntries]);
+                        if (32 * j < dt.K && pos[j] >= 0 && pos[j] / kChunkEntries == c) z[j] = El<kF16>::widen(chunk16[pos[j] % kChunkEntries]);
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < kPer; ++j)
-                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)(lane + 32 * j);
+                        if (32 * j < dt.K && pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)(lane + 32 * j);
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < kPer; ++j)
-                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c)
+                        if (32 * j < dt.K && pos[j] >= 0 && pos[j] / kChunkEntries == c)
                             twice |= chunk16[pos[j] % kChunkEntries] != (uint16_t)(lane + 32 * j);
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < kPer; ++j)
-                        if (pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)El<kF16>::kNegInf;
+                        if (32 * j < dt.K && pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)El<kF16>::kNegInf;
                     __syncwarp();
                 }
                 if (lane == 0) mbar_arrive(ready(slot));
@@ -382,7 +388,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
         return;
     }
 
-    if (kDistill && warp == NW + 2) {
+    if (kDistill && warp == NW + 3) {
         // ------------------------------------------------------------ patch warp
         const float row_scale = N > 0 ? p.grad_scale * dt.tau / (float)N : 0.f;
         int slot = 0;
@@ -402,9 +408,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const int k = lane + 32 * j;
-                pos[j] = k < dt.K ? tp[k] : -1;
+                pos[j] = -1;
                 value[j] = 0;
-                if (pos[j] >= 0) {
+                if (32 * j < dt.K && k < dt.K) pos[j] = tp[k];
+                if (32 * j < dt.K && pos[j] >= 0) {
                     const float q = ex2(fmaf(((const float*)tp)[2 * Kpad + k], xscale, -tot.x) - l2);
                     value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -((const float*)tp)[Kpad + k]), 0.f) & 0xffffu;
                 }
@@ -418,7 +425,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
                 uint16_t* chunk16 = (uint16_t*)(smem + (size_t)slot * kChunk);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
-                    if (pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)value[j];
+                    if (32 * j < dt.K && pos[j] >= 0 && pos[j] / kChunkEntries == c) chunk16[pos[j] % kChunkEntries] = (uint16_t)value[j];
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(patched(slot));
@@ -633,13 +640,26 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
             g = -(scale_over_N * dt.tau) * distill_factor(s_target[ts], tot.s, r.one_m_py);
             if (tid == 0) s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
         } else if (!ri.bad_id) {
-            row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
+            if (p.objective == kObjPolicyKl) g = policy_gradient(p, ri.sc, policy_term<true>(p, ri.sc, tot, zy_row), scale_over_N);
+            else row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
         }
-        if (!kDistill && tid == 0 && crank == 0 && !aborted) {
+        if (!kDistill && p.objective != kObjPolicyKl && tid == 0 && crank == 0 && !aborted) {
             if (p.row_loss) p.row_loss[ri.flat] = loss;
-            if (p.row_kl) p.row_kl[ri.flat] = kl;
             if (p.out_lp_new) p.out_lp_new[ri.flat] = ri.bad_id ? 0.f : r.lp;
         }
+        // the policy loss with KL: its terms are formed by one thread, when the block has its gradient
+        auto write_terms = [&]() {
+            if (kDistill || p.objective != kObjPolicyKl || tid != 0 || crank != 0 || aborted) return;
+            float lp = 0.f;
+            if (!ri.bad_id) {
+                const PolicyTerm q = policy_term<false>(p, ri.sc, tot, zy_row);
+                policy_loss_terms(p, ri.sc, q, loss, kl);
+                lp = q.lp;
+            }
+            p.row_loss[ri.flat] = loss;
+            p.row_kl[ri.flat] = kl;
+            if (p.out_lp_new) p.out_lp_new[ri.flat] = lp;
+        };
 
         // ---- pass 2: gradient = exponential * (-g / sum), written over the logits chunk by chunk; every chunk
         // goes back to the producer as soon as this warp is done with it
@@ -694,6 +714,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 96 : 32), 1) loss_cring_
             for (int c = 2; c < C - 1; ++c) from_tmem(std::false_type{}, c);
             from_tmem(std::true_type{}, C - 1);
         }
+        write_terms();
         s0 += C;
         if (s0 >= R) { s0 -= R; ph0 ^= 1u; }
     }

@@ -100,8 +100,39 @@ __device__ __forceinline__ float lp_relative(const Acc& a, float zy)
     return kLn2 * (fmaf(zy, kLog2e, -a.M) - log2f(a.s + a.ey));
 }
 
-// Loss terms of one token and g = d(grad_scale * total loss) / d(log-prob).  `scale` is grad_scale over the number of
-// tokens (or of non-empty sequences).  lp is replaced by the value the objective is formed with.
+// A token of kObjPolicyKl.  A whole block waits for the gradient once per row, so that it forms it by a short chain on the
+// hardware's ex2 and lg2 (kFast; relative error about 2^-22, as in row_finish_fast); 1 - exp(d) loses its relative accuracy
+// at small d, where it is small beside the policy part.  The loss terms are formed by one thread, without the shortcuts.
+struct PolicyTerm {
+    float lp, unclipped, clipped;
+    bool free;                  // the unclipped branch is active
+};
+template <bool kFast>
+__device__ __forceinline__ PolicyTerm policy_term(const RowArgs& p, const RowScalars& s, const Acc& tot, float zy)
+{
+    PolicyTerm q;
+    q.lp = kFast ? kLn2 * (fmaf(zy, kLog2e, -tot.M) - lg2(tot.s + tot.ey)) : lp_relative(tot, zy);
+    const float rho = kFast ? ex2((q.lp - s.lp_old) * kLog2e) : expf(q.lp - s.lp_old);
+    q.unclipped = -s.adv * rho;
+    q.clipped = -s.adv * fminf(fmaxf(rho, p.ratio_lo), p.ratio_hi);
+    q.free = !(q.unclipped < q.clipped);                              // NaN stays in
+    return q;
+}
+// g = d(grad_scale * total loss) / d(log-prob).  `scale` is grad_scale over the number of tokens (or of non-empty sequences).
+__device__ __forceinline__ float policy_gradient(const RowArgs& p, const RowScalars& s, const PolicyTerm& q, float scale)
+{
+    const float d_pg = q.free ? q.unclipped : 0.f;
+    const float d_kl = p.lp_ref ? p.kl_coef * (1.f - ex2((s.lp_ref - q.lp) * kLog2e)) : 0.f;
+    return scale * s.w * (d_pg + d_kl);
+}
+// The token's terms in the two losses.
+__device__ __forceinline__ void policy_loss_terms(const RowArgs& p, const RowScalars& s, const PolicyTerm& q, float& loss, float& kl)
+{
+    loss = s.w * (q.free ? q.unclipped : q.clipped);
+    kl = p.lp_ref ? s.w * exp_excess(s.lp_ref - q.lp) : 0.f;
+}
+
+// Loss terms of one token and its g.  lp is replaced by the value the objective is formed with.
 template <bool kFast>
 __device__ __forceinline__ void row_objective(const RowArgs& p, const RowScalars& s, const Acc& tot, float zy, float& lp,
                                               float scale, float& loss, float& kl, float& g)
@@ -110,20 +141,10 @@ __device__ __forceinline__ void row_objective(const RowArgs& p, const RowScalars
     if (p.objective == kObjPpo) {
         ppo_token<kFast>(lp, s.lp_old, s.adv, p.clip_eps, scale, loss, g);
     } else if (p.objective == kObjPolicyKl) {
-        lp = lp_relative(tot, zy);
-        const float rho = expf(lp - s.lp_old);
-        const float unclipped = -s.adv * rho;
-        const float clipped = -s.adv * fminf(fmaxf(rho, p.ratio_lo), p.ratio_hi);
-        float d_pg = 0.f, d_kl = 0.f;
-        if (unclipped >= clipped) { loss = unclipped; d_pg = unclipped; } else loss = clipped;
-        if (!(unclipped == unclipped)) loss = d_pg = unclipped;           // NaN stays NaN
-        if (p.lp_ref) {
-            const float d = s.lp_ref - lp;
-            kl = s.w * exp_excess(d);
-            d_kl = -p.kl_coef * expm1f(d);
-        }
-        loss *= s.w;
-        g = scale * s.w * (d_pg + d_kl);
+        const PolicyTerm q = policy_term<kFast>(p, s, tot, zy);
+        lp = q.lp;
+        g = policy_gradient(p, s, q, scale);
+        policy_loss_terms(p, s, q, loss, kl);
     } else {
         loss = 0.f;
         g = s.adv;

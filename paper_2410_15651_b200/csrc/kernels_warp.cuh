@@ -42,6 +42,7 @@ struct WarpArgs {
     float* out_lp2;
     // kEnt: entropy of the softmax of every valid row of the (first) tensor, 0 at padded positions
     float* out_entropy;
+    int relative;           // form the log-prob as lp_relative does (sums of it are wanted)
 };
 
 // ---- sums that also carry what the entropy needs.  Beside (M, s, ey) of Acc a thread keeps
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(WPB * 32, 1) logprob_warp_kernel(WarpArgs wa)
         if (lane == 0 && !aborted) {
             const RowResult r = row_finish(Acc{M, s, ey}, zy);
             float* out = (kDual && k >= N1) ? wa.out_lp2 : p.out_lp;
-            out[flat] = bad_id ? 0.f : r.lp;
+            out[flat] = bad_id ? 0.f : (wa.relative ? lp_relative(Acc{M, s, ey}, zy) : r.lp);
             if (kEnt && !(kDual && k >= N1)) {
                 // H = ln2 * (log2 S - (sum_v e_v (x_v - M)) / S),  S = s + ey; the generated token's term joins the sum here
                 const float S = s + ey;
