@@ -397,8 +397,9 @@ __device__ __forceinline__ void distill_publish(const DistillArgs& dt, float xsc
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
         if (32 * j < dt.K && pos[j] >= 0) Mt = fmaxf(Mt, z[j] * xscale);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) Mt = fmaxf(Mt, __shfl_xor_sync(0xffffffffu, Mt, o));
+    // (the largest by the warp-wide integer maximum: the bits of a float, negative ones complemented, order as the floats do)
+    const int bits = __float_as_int(Mt), top = __reduce_max_sync(0xffffffffu, bits ^ ((bits >> 31) & 0x7fffffff));
+    Mt = __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
     float ey = 0.f, zy = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
@@ -457,9 +458,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     static_assert(kCregMaxBufs * 16 <= 64, "the mbarriers of the buffers take the 64 bytes after the zero buffer");
     __shared__ uint32_t s_tmem_base;
-    // kDistill: barriers announced / ready / patched of every buffer, and what target warp, consumers and patch warp hand on
+    // kDistill: barriers announced / ready / patched / told / totals of every buffer, and what target warps, consumers and
+    // patch warp hand on
     constexpr int kBufsHere = kDistill ? kCregMaxBufs : 1;
-    __shared__ __align__(8) unsigned long long s_dbar[3 * kBufsHere];
+    __shared__ __align__(8) unsigned long long s_dbar[5 * kBufsHere];
     __shared__ TargetInfo s_target[kBufsHere];
     __shared__ LabelInfo s_tlab[kBufsHere];
     __shared__ float4 s_total[kBufsHere];
@@ -486,6 +488,8 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     auto announced = [&](int buf) { return smem_u32(s_dbar) + 8u * buf; };               // the row's info is there
     auto ready = [&](int buf) { return smem_u32(s_dbar) + 8u * (kBufsHere + buf); };     // teacher entries taken out
     auto patched = [&](int buf) { return smem_u32(s_dbar) + 8u * (2 * kBufsHere + buf); };
+    auto told = [&](int buf) { return smem_u32(s_dbar) + 8u * (3 * kBufsHere + buf); };         // the entries' sums are there
+    auto totals = [&](int buf) { return smem_u32(s_dbar) + 8u * (4 * kBufsHere + buf); };       // the row's are
     const int Kpad = kDistill ? (dt.K + 31) / 32 * 32 : 0;
     // teacher entries of a buffer: position in it (or -1), weight, logit
     auto t_pos = [&](int buf) { return (int*)(zero_buf + kZeroBytesHere + 64) + 3 * buf * Kpad; };
@@ -500,6 +504,8 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 mbar_init(announced(b), 1);
                 mbar_init(ready(b), 1);
                 mbar_init(patched(b), 1);
+                mbar_init(told(b), 1);
+                mbar_init(totals(b), 1);
             }
         }
         mbar_init(xbar_addr, 1);
@@ -716,10 +722,12 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 if (pos[j] >= 0) row16[pos[j]] = (uint16_t)El<kF16>::kNegInf;
                 { tp[lane + 32 * j] = pos[j]; tw[lane + 32 * j] = pk[j]; tz[lane + 32 * j] = z[j]; }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ready(buf));
             if (__any_sync(0xffffffffu, twice)) distill_merge(dt.K, Kpad, lane, tp, tw, pos, pk);
             distill_publish<kCluster>(dt, xscale, crank, lane, pos, pk, z, P, H, pr, s_target[buf], s_tlab[buf]);
             __syncwarp();
-            if (lane == 0) mbar_arrive(ready(buf));
+            if (lane == 0) mbar_arrive(told(buf));
         }
         return;
     }
@@ -729,23 +737,35 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         const float row_scale = N > 0 ? p.grad_scale * dt.tau / (float)N : 0.f;
         for (int i = 0; !aborted; ++i) {
             const int buf = i % NB;
-            mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            mbar_wait(totals(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
             const long long flat = s_row[buf].flat;
             if (flat < 0) break;
+            // the gradients of the entries, while the consumers write the others
             const float4 tot = s_total[buf];                         // M, mass outside, mass of the entries, sum p (x - M)
             const TargetInfo ti = s_target[buf];
             const float l2 = log2f(tot.y + tot.z);
-            uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
-            const int* tp = t_pos(buf);
-            const float *tw = t_p(buf), *tz = t_z(buf);
-            for (int k = lane; k < dt.K; k += 32) {
-                const int at = tp[k];
-                if (at < 0) continue;
-                const float q = ex2(fmaf(tz[k], xscale, -tot.x) - l2);
-                row16[at] = (uint16_t)(El<kF16>::pack2(row_scale * fmaf(ti.W, q, -tw[k]), 0.f) & 0xffffu);
+            int pos[kPer];
+            uint32_t value[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int k = lane + 32 * j;
+                pos[j] = -1;
+                value[j] = 0;
+                if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(buf)[k];
+                if (32 * j < dt.K && pos[j] >= 0) {
+                    const float q = ex2(fmaf(t_z(buf)[k], xscale, -tot.x) - l2);
+                    value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -t_p(buf)[k]), 0.f) & 0xffffu;
+                }
             }
+            mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+            if (aborted) break;
+            uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (32 * j < dt.K && pos[j] >= 0) row16[pos[j]] = (uint16_t)value[j];
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -785,7 +805,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         RowInfo ri = s_row[buf];
         if (aborted) { ri.y = 0; ri.bad_id = 1; ri.flat = 0; }      // stale row info: touch nothing
         if (ri.flat < 0) {                                           // the producer has no more rows (the same for every thread)
-            if (kDistill && lane == 0) mbar_arrive(computed(buf));   // tells the patch warp
+            if (kDistill && tid == 0) mbar_arrive(totals(buf));      // tells the patch warp
             break;
         }
         unsigned char* rowbuf = smem + (size_t)buf * ca.buf_stride;
@@ -889,6 +909,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         }
         if (cnt == 0 && !owner) { M = Mref; vs = 0.f; }
         const bool diverged = M != Mref;
+        if (kDistill) {
+            mbar_wait(told(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
+        }
 
         if (!kDistill && (label_here ? owner : tid == 0))
             s_lab[par] = label_here ? LabelInfo{zy, ex2(fmaf(zy, kLog2e, -M)), M, 0.f} : LabelInfo{0.f, 0.f, kFloorM, 0.f};
@@ -949,7 +973,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         float loss = 0.f, kl = 0.f, g = 0.f;
         if (kDistill) {
             g = -(scale_over_N * dt.tau) * distill_factor(s_target[buf], tot.s, r.one_m_py);
-            if (tid == 0) s_total[buf] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+            if (tid == 0) {
+                s_total[buf] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                mbar_arrive(totals(buf));
+            }
         } else if (!ri.bad_id) {
             if (p.objective == kObjPolicyKl) g = policy_gradient(p, ri.sc, policy_term<true>(p, ri.sc, tot, zy_row), scale_over_N);
             else row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);

@@ -96,8 +96,9 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
     __shared__ __align__(16) float4 s_xchg[2][kCluster];     // per row parity: (M, s, ey, zy) of every block of the cluster
     __shared__ __align__(8) unsigned long long s_xbar[2];
     __shared__ uint32_t s_tmem_base;
-    // kDistill: barriers ready / patched of every slot, announced of every row info, told / spare of every set of entries
-    __shared__ __align__(8) unsigned long long s_dbar[kDistill ? 2 * kCringMaxSlots + kCringRows + 2 * kCringTargets : 1];
+    // kDistill: barriers ready / patched of every slot, announced of every row info, told / spare / totals of every set of
+    // entries
+    __shared__ __align__(8) unsigned long long s_dbar[kDistill ? 2 * kCringMaxSlots + kCringRows + 3 * kCringTargets : 1];
     __shared__ TargetInfo s_target[kDistill ? kCringTargets : 1];
     __shared__ LabelInfo s_tlab[kDistill ? kCringTargets : 1];
     __shared__ float4 s_total[kDistill ? kCringTargets : 1];
@@ -128,6 +129,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
     auto announced = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + (i & (kCringRows - 1))); };
     auto told = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + kCringRows + (i & (kCringTargets - 1))); };
     auto spare = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + kCringRows + kCringTargets + (i & (kCringTargets - 1))); };
+    auto totals = [&](int i) { return dbar + 8u * (2 * kCringMaxSlots + kCringRows + 2 * kCringTargets + (i & (kCringTargets - 1))); };
     auto finished = [&](int slot) { return kDistill ? patched(slot) : done(slot); };
     const int Kpad = kDistill ? (dt.K + 31) / 32 * 32 : 0;
     // a row's teacher entries: position in the slice (or -1), weight, logit
@@ -148,6 +150,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
         for (int i = 0; kDistill && i < kCringTargets; ++i) {
             mbar_init(told(i), 1);
             mbar_init(spare(i), 1);
+            mbar_init(totals(i), 1);
         }
         mbar_init(xbar_addr, 1);
         mbar_init(xbar_addr + 8u, 1);
@@ -394,7 +397,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
         int slot = 0;
         uint32_t ph = 0;
         for (int i = 0; !aborted && nvec > 0; ++i) {
-            mbar_wait(done(slot), ph, p.status, aborted, p.wait_limit_ns);
+            mbar_wait(totals(i), (uint32_t)(i / kCringTargets) & 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
             const long long flat = s_row[i & (kCringRows - 1)].flat;
@@ -419,7 +422,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
             __syncwarp();
             if (lane == 0) mbar_arrive(spare(i));                    // the set has been read
             for (int c = 0; c < C; ++c) {
-                if (c > 0) mbar_wait(done(slot), ph, p.status, aborted, p.wait_limit_ns);
+                mbar_wait(done(slot), ph, p.status, aborted, p.wait_limit_ns);
                 aborted = __any_sync(0xffffffffu, aborted);
                 if (aborted) break;
                 uint16_t* chunk16 = (uint16_t*)(smem + (size_t)slot * kChunk);
@@ -469,7 +472,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
         RowInfo ri = s_row[i & (kCringRows - 1)];
         if (aborted) { ri.y = 0; ri.bad_id = 1; ri.flat = 0; }      // stale row info: touch nothing
         if (ri.flat < 0) {                                           // the producer has no more rows (the same for every thread)
-            if (kDistill && lane == 0) mbar_arrive(done(s0));        // tells the patch warp
+            if (kDistill && tid == 0) mbar_arrive(totals(i));        // tells the patch warp
             break;
         }
 
@@ -638,7 +641,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
         float loss = 0.f, kl = 0.f, g = 0.f;
         if (kDistill) {
             g = -(scale_over_N * dt.tau) * distill_factor(s_target[ts], tot.s, r.one_m_py);
-            if (tid == 0) s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+            if (tid == 0) {
+                s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                mbar_arrive(totals(i));
+            }
         } else if (!ri.bad_id) {
             if (p.objective == kObjPolicyKl) g = policy_gradient(p, ri.sc, policy_term<true>(p, ri.sc, tot, zy_row), scale_over_N);
             else row_objective<true>(p, ri.sc, tot, zy_row, r.lp, scale_over_N, loss, kl, g);
