@@ -42,8 +42,8 @@
 // have passed a block barrier at the end of the kernel.
 //
 // kDistill: the row's loss is distillation from up to 256 teacher entries instead of an objective of one generated
-// token.  Three more warps serve it.  Two target warps, in turn, turn the entries of a row into weights while the row is
-// still on its way, then take the logits of those entries out of the buffer (they become -inf, as the generated token's does
+// token.  Three more warps serve it.  Two target warps, in turn, turn the entries of a row into weights before the row has
+// landed, then take the logits of those entries out of the buffer (they become -inf, as the generated token's does
 // above, so that the sum over the other entries -- the student's mass outside the teacher's entries -- comes without
 // cancellation).  The consumers' two passes are as above, with one factor for all entries that are not the teacher's.
 // The patch warp then writes the gradients of the teacher's entries into the finished buffer and forms the row's loss,
@@ -62,7 +62,6 @@ struct RowInfo {
     int y;                  // generated token (0 if it was out of range)
     int bad_id;
     RowScalars sc;
-    long long entries;      // kDistill: element offset of the row's teacher entries
     unsigned mis;           // bytes between the 16-byte boundary below the row's first logit and that logit
     unsigned pad;
 };
@@ -112,6 +111,8 @@ constexpr int kCregZeroBytes = 16384;  // zeroed buffer that feeds the bulk zero
 
 constexpr int kDistillMax = 256;       // teacher entries per row
 constexpr int kDistillZeroBytes = 4096;
+constexpr int kDistillSets = 4;         // rows whose entries are held (a power of two)
+constexpr int kDistillRows = 8;         // rows announced to the target warps (a power of two)
 constexpr int kDistillPlain = 0, kDistillNormalised = 1, kDistillTail = 2;
 
 struct DistillArgs {
@@ -120,6 +121,12 @@ struct DistillArgs {
     long long stride_b, stride_t;
     int K, mode;
     float tau, scale;        // temperature, log2(e) / temperature
+};
+
+// A row, as it is announced to the target warps when the producer learns of it, two rows before it is loaded.
+struct TargetRow {
+    long long entries;       // element offset of its teacher entries, or -1: no more rows
+    unsigned eoff;           // entries of its first vector that precede it
 };
 
 // What the target warp knows of a row's teacher entries.
@@ -175,11 +182,11 @@ inline size_t creg_buf_stride(unsigned slice_vecs, int consumer_warps)
     return (slice_vecs + per_round - 1) / per_round * per_round * 16;
 }
 constexpr int kCregMaxBufs = 3;
-// K: teacher entries per row (0: not distillation), for each of which a buffer carries position, weight and logit.
+// K: teacher entries per row (0: not distillation), for each of which a set holds position, weight and logit.
 inline int distill_pad(int K) { return (K + 31) / 32 * 32; }
 inline size_t creg_smem_bytes(unsigned slice_vecs, int consumer_warps, int n_buf, int K = 0)
 {
-    return (size_t)n_buf * (creg_buf_stride(slice_vecs, consumer_warps) + 12 * (size_t)distill_pad(K)) +
+    return (size_t)n_buf * creg_buf_stride(slice_vecs, consumer_warps) + 12 * (size_t)distill_pad(K) * kDistillSets +
            (K > 0 ? kDistillZeroBytes : kCregZeroBytes) + 64;
 }
 // Columns of tensor memory that a block needs for slices of `slice_vecs` vectors: each warp stores 8 columns per
@@ -458,13 +465,14 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     static_assert(kCregMaxBufs * 16 <= 64, "the mbarriers of the buffers take the 64 bytes after the zero buffer");
     __shared__ uint32_t s_tmem_base;
-    // kDistill: barriers announced / ready / patched / told / totals of every buffer, and what target warps, consumers and
-    // patch warp hand on
-    constexpr int kBufsHere = kDistill ? kCregMaxBufs : 1;
-    __shared__ __align__(8) unsigned long long s_dbar[5 * kBufsHere];
-    __shared__ TargetInfo s_target[kBufsHere];
-    __shared__ LabelInfo s_tlab[kBufsHere];
-    __shared__ float4 s_total[kBufsHere];
+    // kDistill: barriers ready / patched of every buffer, announced of every row that the target warps learn of, told / spare
+    // / totals of every set of entries, and what target warps, consumers and patch warp hand on
+    constexpr int kBufsHere = kDistill ? kCregMaxBufs : 1, kSetsHere = kDistill ? kDistillSets : 1;
+    __shared__ __align__(8) unsigned long long s_dbar[kDistill ? 2 * kBufsHere + kDistillRows + 3 * kDistillSets : 1];
+    __shared__ TargetRow s_trow[kDistill ? kDistillRows : 1];
+    __shared__ TargetInfo s_target[kSetsHere];
+    __shared__ LabelInfo s_tlab[kSetsHere];
+    __shared__ float4 s_total[kSetsHere];
 
     const RowArgs& p = ca.row;
     const DistillArgs& dt = ca.distill;
@@ -485,28 +493,35 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     auto landed = [&](int buf) { return bar_addr + 8u * buf; };
     auto computed = [&](int buf) { return bar_addr + 8u * (kCregMaxBufs + buf); };
     const uint32_t xbar_addr = smem_u32(s_xbar);
-    auto announced = [&](int buf) { return smem_u32(s_dbar) + 8u * buf; };               // the row's info is there
-    auto ready = [&](int buf) { return smem_u32(s_dbar) + 8u * (kBufsHere + buf); };     // teacher entries taken out
-    auto patched = [&](int buf) { return smem_u32(s_dbar) + 8u * (2 * kBufsHere + buf); };
-    auto told = [&](int buf) { return smem_u32(s_dbar) + 8u * (3 * kBufsHere + buf); };         // the entries' sums are there
-    auto totals = [&](int buf) { return smem_u32(s_dbar) + 8u * (4 * kBufsHere + buf); };       // the row's are
+    const uint32_t dbar = smem_u32(s_dbar);
+    auto ready = [&](int buf) { return dbar + 8u * buf; };                          // teacher entries taken out
+    auto patched = [&](int buf) { return dbar + 8u * (kBufsHere + buf); };
+    auto announced = [&](int i) { return dbar + 8u * (2 * kBufsHere + (i & (kDistillRows - 1))); };
+    const uint32_t sbar = dbar + 8u * (2 * kBufsHere + kDistillRows);
+    auto told = [&](int i) { return sbar + 8u * (i & (kDistillSets - 1)); };                          // the entries' sums are there
+    auto totals = [&](int i) { return sbar + 8u * (kDistillSets + (i & (kDistillSets - 1))); };       // the row's are
+    auto spare = [&](int i) { return sbar + 8u * (2 * kDistillSets + (i & (kDistillSets - 1))); };    // the set has been read
+    auto set_phase = [&](int i) { return (uint32_t)(i / kDistillSets) & 1u; };
     const int Kpad = kDistill ? (dt.K + 31) / 32 * 32 : 0;
-    // teacher entries of a buffer: position in it (or -1), weight, logit
-    auto t_pos = [&](int buf) { return (int*)(zero_buf + kZeroBytesHere + 64) + 3 * buf * Kpad; };
-    auto t_p = [&](int buf) { return (float*)t_pos(buf) + Kpad; };
-    auto t_z = [&](int buf) { return (float*)t_pos(buf) + 2 * Kpad; };
+    // teacher entries of a row: position in the buffer (or -1), weight, logit
+    auto t_pos = [&](int i) { return (int*)(zero_buf + kZeroBytesHere + 64) + 3 * (i & (kDistillSets - 1)) * Kpad; };
+    auto t_p = [&](int i) { return (float*)t_pos(i) + Kpad; };
+    auto t_z = [&](int i) { return (float*)t_pos(i) + 2 * Kpad; };
 
     if (tid == 0) {
         for (int b = 0; b < NB; ++b) {
             mbar_init(landed(b), 1);
             mbar_init(computed(b), NW);
             if (kDistill) {
-                mbar_init(announced(b), 1);
                 mbar_init(ready(b), 1);
                 mbar_init(patched(b), 1);
-                mbar_init(told(b), 1);
-                mbar_init(totals(b), 1);
             }
+        }
+        for (int i = 0; kDistill && i < kDistillRows; ++i) mbar_init(announced(i), 1);
+        for (int i = 0; kDistill && i < kDistillSets; ++i) {
+            mbar_init(told(i), 1);
+            mbar_init(totals(i), 1);
+            mbar_init(spare(i), 1);
         }
         mbar_init(xbar_addr, 1);
         mbar_init(xbar_addr + 8u, 1);
@@ -619,12 +634,26 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 }
                 return a;
             };
+            // the target warps learn of a row as soon as the producer does
+            auto announce = [&](int j, const Ahead& a) {
+                if (!kDistill) return;
+                TargetRow tr{-1, 0u};
+                if (a.ok) {
+                    tr.entries = (long long)a.b * dt.stride_b + (long long)a.t * dt.stride_t;
+                    if (kAny) tr.eoff = (unsigned)((uintptr_t)(p.logits + (long long)a.b * p.stride_b + (long long)a.t * p.stride_t) & 15u) >> 1;
+                }
+                s_trow[j & (kDistillRows - 1)] = tr;
+                mbar_arrive(announced(j));
+            };
             Ahead a0 = fetch(), a1 = fetch();
+            announce(0, a0);
+            announce(1, a1);
             int i = 0;
             for (; !aborted; ++i) {
                 const Ahead a = a0;
                 a0 = a1;
                 a1 = fetch();
+                announce(i + 2, a1);
                 if (!a.ok) break;
                 const unsigned char* row = (const unsigned char*)(p.logits + (long long)a.b * p.stride_b + (long long)a.t * p.stride_t) + slice_off;
                 RowInfo ri;
@@ -633,7 +662,6 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 ri.bad_id = (a.y < 0 || a.y >= p.V) ? 1 : 0;
                 ri.y = ri.bad_id ? 0 : (int)a.y;
                 if (!kDistill) ri.sc = a.sc;
-                ri.entries = kDistill ? (long long)a.b * dt.stride_b + (long long)a.t * dt.stride_t : 0;
                 ri.mis = kAny ? (unsigned)((uintptr_t)row & 15u) : 0u;
                 ri.pad = 0;
                 if (ri.bad_id && crank == 0) atomicOr(p.status, kErrIdRange);
@@ -641,7 +669,6 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 if (i >= NB) drain(i - NB);                              // the buffer's previous slice goes out first
                 if (aborted) break;
                 s_row[buf] = ri;
-                if (kDistill) mbar_arrive(announced(buf));
                 const uint32_t dst = buf_addr + (uint32_t)buf * ca.buf_stride;
                 // kAny: the aligned span around the row (it stays inside the 16-byte blocks that hold the row's ends)
                 const uint32_t load_bytes = kAny ? ((ri.mis + ca.row_bytes + 15u) & ~15u) : slice_bytes;
@@ -660,15 +687,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 if (i >= NB) drain(i - NB);
                 if (!aborted) {
                     s_row[buf].flat = -1;
-                    if (kDistill) mbar_arrive(announced(buf));
                     mbar_arrive_expect_tx(landed(buf), 0);
                 }
             }
             for (int j = i + 1 >= NB ? i + 1 - NB : 0; j < i && !aborted; ++j) drain(j);
-            if (kDistill && !aborted) {                                // the other target warp waits for the row after the last
-                s_row[(i + 1) % NB].flat = -1;
-                mbar_arrive(announced((i + 1) % NB));
-            }
             bulk_wait_all();
             if (kCluster > 1) cluster_sync_unaligned();                 // no block leaves while a peer may still write to it
         }
@@ -679,27 +701,25 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         // ------------------------------------------------------------ target warps: one for every other row
         for (int i = warp - (NW + 1); !aborted; i += 2) {
             const int buf = i % NB;
-            mbar_wait(announced(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            mbar_wait(announced(i), (uint32_t)(i / kDistillRows) & 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
-            const long long entries = s_row[buf].entries;
-            const uint32_t eoff = kAny ? (s_row[buf].mis >> 1) : 0u;
-            if (s_row[buf].flat < 0) {
-                if (lane == 0) mbar_arrive(ready(buf));
-                break;
-            }
+            const TargetRow tr = s_trow[i & (kDistillRows - 1)];
+            if (tr.entries < 0) break;
             int pos[kPer];
             float pk[kPer], pr[kCluster];
             double P, H;
-            distill_weights<kCluster>(p, dt, entries, eoff, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
+            distill_weights<kCluster>(p, dt, tr.entries, tr.eoff, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
             // the logits leave the buffer.  Every entry leaves its number in its place and looks whether it is still
             // there: if not, the same entry is named twice.
             mbar_wait(landed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            // the set's previous row has been patched (nothing to wait for in the first turn)
+            mbar_wait(spare(i), set_phase(i) ^ 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
             uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
-            int* tp = t_pos(buf);
-            float *tw = t_p(buf), *tz = t_z(buf);
+            int* tp = t_pos(i);
+            float *tw = t_p(i), *tz = t_z(i);
             float z[kPer];
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
@@ -725,9 +745,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
             __syncwarp();
             if (lane == 0) mbar_arrive(ready(buf));
             if (__any_sync(0xffffffffu, twice)) distill_merge(dt.K, Kpad, lane, tp, tw, pos, pk);
-            distill_publish<kCluster>(dt, xscale, crank, lane, pos, pk, z, P, H, pr, s_target[buf], s_tlab[buf]);
+            distill_publish<kCluster>(dt, xscale, crank, lane, pos, pk, z, P, H, pr, s_target[i & (kDistillSets - 1)],
+                                      s_tlab[i & (kDistillSets - 1)]);
             __syncwarp();
-            if (lane == 0) mbar_arrive(told(buf));
+            if (lane == 0) mbar_arrive(told(i));
         }
         return;
     }
@@ -737,14 +758,14 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         const float row_scale = N > 0 ? p.grad_scale * dt.tau / (float)N : 0.f;
         for (int i = 0; !aborted; ++i) {
             const int buf = i % NB;
-            mbar_wait(totals(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            mbar_wait(totals(i), set_phase(i), p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
             const long long flat = s_row[buf].flat;
             if (flat < 0) break;
             // the gradients of the entries, while the consumers write the others
-            const float4 tot = s_total[buf];                         // M, mass outside, mass of the entries, sum p (x - M)
-            const TargetInfo ti = s_target[buf];
+            const float4 tot = s_total[i & (kDistillSets - 1)];      // M, mass outside, mass of the entries, sum p (x - M)
+            const TargetInfo ti = s_target[i & (kDistillSets - 1)];
             const float l2 = log2f(tot.y + tot.z);
             int pos[kPer];
             uint32_t value[kPer];
@@ -753,12 +774,14 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 const int k = lane + 32 * j;
                 pos[j] = -1;
                 value[j] = 0;
-                if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(buf)[k];
+                if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(i)[k];
                 if (32 * j < dt.K && pos[j] >= 0) {
-                    const float q = ex2(fmaf(t_z(buf)[k], xscale, -tot.x) - l2);
-                    value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -t_p(buf)[k]), 0.f) & 0xffffu;
+                    const float q = ex2(fmaf(t_z(i)[k], xscale, -tot.x) - l2);
+                    value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -t_p(i)[k]), 0.f) & 0xffffu;
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(spare(i));                    // the set has been read
             mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
@@ -800,13 +823,16 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         const int buf = i % NB, par = i & 1;
         const uint32_t use = (uint32_t)(i >> 1) & 1u;                // of the exchange barrier, which alternates by row
         mbar_wait(landed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
-        if (kDistill) mbar_wait(ready(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
         aborted = __any_sync(0xffffffffu, aborted);                 // a warp gives up as a whole
         RowInfo ri = s_row[buf];
         if (aborted) { ri.y = 0; ri.bad_id = 1; ri.flat = 0; }      // stale row info: touch nothing
         if (ri.flat < 0) {                                           // the producer has no more rows (the same for every thread)
-            if (kDistill && tid == 0) mbar_arrive(totals(buf));      // tells the patch warp
+            if (kDistill && tid == 0) mbar_arrive(totals(i));        // tells the patch warp
             break;
+        }
+        if (kDistill) {
+            mbar_wait(ready(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
         }
         unsigned char* rowbuf = smem + (size_t)buf * ca.buf_stride;
         const uint4* src = (const uint4*)rowbuf + tid;
@@ -909,8 +935,9 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         }
         if (cnt == 0 && !owner) { M = Mref; vs = 0.f; }
         const bool diverged = M != Mref;
+        const int ts = i & (kDistillSets - 1);                       // kDistill: the row's set of entries
         if (kDistill) {
-            mbar_wait(told(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+            mbar_wait(told(i), set_phase(i), p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
         }
 
@@ -925,7 +952,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
             tot.M = Mref;
             tot.s = sum_warp_sums<NW>(s_sum[par]);
             if (kDistill) {
-                const LabelInfo li = s_tlab[buf];
+                const LabelInfo li = s_tlab[ts];
                 tot.M = fmaxf(Mref, li.M);
                 tot.s *= ex2(Mref - tot.M);
                 tot.ey = li.ey * ex2(li.M - tot.M);
@@ -935,10 +962,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         } else {
             // a wait that ran out somewhere in the block ends the block's work here, for all its threads alike
             if (consumer_barrier_or<NW>(aborted)) { aborted = true; break; }
-            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], kDistill ? &s_tlab[buf] : &s_lab[par], warp, lane);
+            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], kDistill ? &s_tlab[ts] : &s_lab[par], warp, lane);
         }
         // the generated token's logit; kDistill: sum over the slice's teacher entries of p (x - M), M the total's reference
-        float zy_row = kDistill ? fmaf(s_tlab[buf].pad, s_tlab[buf].M - tot.M, s_tlab[buf].zy) : s_lab[par].zy;
+        float zy_row = kDistill ? fmaf(s_tlab[ts].pad, s_tlab[ts].M - tot.M, s_tlab[ts].zy) : s_lab[par].zy;
 
         if (kCluster > 1) {
             // every block of the cluster sends its slice's (M, s, ey, zy) to every block, itself included
@@ -963,7 +990,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 const float sc = ex2(part.x - Mx);
                 sx = fmaf(part.y, sc, sx);
                 eyx = fmaf(part.z, sc, eyx);
-                zx += kDistill ? fmaf(s_target[buf].pr[r], part.x - Mx, part.w) : part.w;
+                zx += kDistill ? fmaf(s_target[ts].pr[r], part.x - Mx, part.w) : part.w;
             }
             tot = Acc{Mx, sx, eyx};
             zy_row = zx;
@@ -972,10 +999,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
 
         float loss = 0.f, kl = 0.f, g = 0.f;
         if (kDistill) {
-            g = -(scale_over_N * dt.tau) * distill_factor(s_target[buf], tot.s, r.one_m_py);
+            g = -(scale_over_N * dt.tau) * distill_factor(s_target[ts], tot.s, r.one_m_py);
             if (tid == 0) {
-                s_total[buf] = make_float4(tot.M, tot.s, tot.ey, zy_row);
-                mbar_arrive(totals(buf));
+                s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                mbar_arrive(totals(i));
             }
         } else if (!ri.bad_id) {
             if (p.objective == kObjPolicyKl) g = policy_gradient(p, ri.sc, policy_term<true>(p, ri.sc, tot, zy_row), scale_over_N);

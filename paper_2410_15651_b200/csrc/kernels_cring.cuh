@@ -35,7 +35,7 @@ constexpr int kCringU = 2;                    // vectors per consumer thread and
 constexpr int kCringZeroBytes = 8192;         // zeroed buffer that feeds the bulk zero-fill of padded rows
 constexpr int kCringMaxSlots = 13;
 constexpr int kCringRows = 8;                 // row infos in flight (a power of two)
-constexpr int kCringTargets = 4;              // kDistill: rows whose entries are held (a power of two)
+constexpr int kCringTargets = kDistillSets;   // kDistill: rows whose entries are held
 
 struct CringArgs {
     RowArgs row;
@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
     // kDistill: barriers ready / patched of every slot, announced of every row info, told / spare / totals of every set of
     // entries
     __shared__ __align__(8) unsigned long long s_dbar[kDistill ? 2 * kCringMaxSlots + kCringRows + 3 * kCringTargets : 1];
+    __shared__ TargetRow s_trow[kDistill ? kCringRows : 1];
     __shared__ TargetInfo s_target[kDistill ? kCringTargets : 1];
     __shared__ LabelInfo s_tlab[kDistill ? kCringTargets : 1];
     __shared__ float4 s_total[kDistill ? kCringTargets : 1];
@@ -258,7 +259,15 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 }
                 return a;
             };
+            // the target warps learn of a row as soon as the producer does
+            auto announce = [&](int j, const Ahead& a) {
+                if (!kDistill) return;
+                s_trow[j & (kCringRows - 1)] = TargetRow{a.ok ? (long long)a.b * dt.stride_b + (long long)a.t * dt.stride_t : -1, 0u};
+                mbar_arrive(announced(j));
+            };
             Ahead a0 = fetch(), a1 = fetch();
+            announce(0, a0);
+            announce(1, a1);
             // load side
             long long g = 0;
             int l_slot = 0;
@@ -267,6 +276,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 const Ahead a = a0;
                 a0 = a1;
                 a1 = fetch();
+                announce(i + 2, a1);
                 if (!a.ok) break;
                 const int b = a.b, t = a.t;
                 const long long flat = (long long)b * p.T + t;
@@ -276,7 +286,6 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 ri.bad_id = (a.y < 0 || a.y >= p.V) ? 1 : 0;
                 ri.y = ri.bad_id ? 0 : (int)a.y;
                 if (!kDistill) ri.sc = a.sc;
-                ri.entries = kDistill ? (long long)b * dt.stride_b + (long long)t * dt.stride_t : 0;
                 ri.mis = 0;
                 ri.pad = 0;
                 if (ri.bad_id && crank == 0) atomicOr(p.status, kErrIdRange);
@@ -284,10 +293,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 for (int c = 0; c < C && !aborted; ++c, ++g) {
                     ensure_free(g);
                     if (aborted) break;
-                    if (c == 0) {
-                        s_row[i & (kCringRows - 1)] = ri;               // published by the arrivals below
-                        if (kDistill) mbar_arrive(announced(i));
-                    }
+                    if (c == 0) s_row[i & (kCringRows - 1)] = ri;       // published by the arrival below
                     const uint32_t bytes = c == C - 1 ? last_bytes : kChunk;
                     mbar_arrive_expect_tx(full(l_slot), bytes);
                     bulk_load(ring_addr + (uint32_t)l_slot * kChunk, row + (size_t)c * kChunk, bytes, full(l_slot));
@@ -304,11 +310,6 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 ensure_free(g);
                 if (!aborted) {
                     s_row[i & (kCringRows - 1)].flat = -1;
-                    if (kDistill) {
-                        mbar_arrive(announced(i));
-                        s_row[(i + 1) & (kCringRows - 1)].flat = -1;    // the other target warp waits for the row after the last
-                        mbar_arrive(announced(i + 1));
-                    }
                     mbar_arrive_expect_tx(full(l_slot), 0);
                 }
             }
@@ -327,16 +328,14 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
         // ------------------------------------------------------------ target warps: one for every other row
         for (int i = warp - (NW + 1); !aborted && nvec > 0; i += 2) {
             mbar_wait(announced(i), (uint32_t)(i / kCringRows) & 1u, p.status, aborted, p.wait_limit_ns);
-            // the set's previous row has been patched (nothing to wait for in the first turn)
-            mbar_wait(spare(i), ((uint32_t)(i / kCringTargets) & 1u) ^ 1u, p.status, aborted, p.wait_limit_ns);
             aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
-            const RowInfo& ri = s_row[i & (kCringRows - 1)];
-            if (ri.flat < 0) break;
+            const TargetRow tr = s_trow[i & (kCringRows - 1)];
+            if (tr.entries < 0) break;
             int pos[kPer];
             float pk[kPer], pr[kCluster], z[kPer];
             double P, H;
-            distill_weights<kCluster>(p, dt, ri.entries, 0u, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
+            distill_weights<kCluster>(p, dt, tr.entries, 0u, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
             int* tp = t_pos(i);
             float *tw = (float*)tp + Kpad, *tz = (float*)tp + 2 * Kpad;
             // the logits leave the chunks; every entry leaves its number in its place and looks whether it is still there:
@@ -378,6 +377,9 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 if (lane == 0) mbar_arrive(ready(slot));
                 if (++slot == R) { slot = 0; ph ^= 1u; }
             }
+            // the set's previous row has been patched (nothing to wait for in the first turn)
+            mbar_wait(spare(i), ((uint32_t)(i / kCringTargets) & 1u) ^ 1u, p.status, aborted, p.wait_limit_ns);
+            aborted = __any_sync(0xffffffffu, aborted);
             if (aborted) break;
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
