@@ -433,6 +433,193 @@ __device__ __forceinline__ void distill_publish(const DistillArgs& dt, float xsc
     }
 }
 
+// The same for few entries (kDistillFew at most), with loops that are not unrolled and entries that stay in shared memory.
+// With a copy of every step per entry of a lane, most of them jumped over, the helping warps' code drives the consumers' out of
+// the instruction cache: V = 32000, K = 64 took 209 us against 166 us of the objective with one token, and the warps waited for
+// instructions 3.5 of 13.5 cycles per issue; it takes 169 us like this.  With many entries the unrolled steps are faster (K =
+// 256: 194 against 258 us).
+constexpr int kDistillFew = 64;
+
+struct EntrySet {
+    int* pos;                // position in the block's slice, or -1
+    float* p;                // weight
+    float* z;                // logit (log-prob until the row has landed)
+    int K;
+};
+
+// Weights, positions, the sums of p and of p log p, and the weights' sums over the slices of the cluster's blocks.
+// eoff: entries of the slice's first vector that precede the row.
+template <int kCluster>
+__device__ __forceinline__ void distill_weights_few(const RowArgs& p, const DistillArgs& dt, long long entries, uint32_t eoff,
+                                                uint32_t v0, uint32_t nvec, uint32_t slice_vecs, uint32_t crank, int lane,
+                                                const EntrySet& es, double& P, double& H, float (&pr)[kCluster])
+{
+    bool bad = false;
+    float lmax = kFloorM;
+#pragma unroll 2
+    for (int k = lane; k < es.K; k += 32) {
+        int id = __ldg(dt.ids + entries + k);
+        float lt = __ldg(dt.logprobs + entries + k);
+        bad |= id < -1 || id >= p.V;
+        if (id < 0 || id >= p.V) { id = -1; lt = __uint_as_float(0xff800000u); }
+        lmax = fmaxf(lmax, lt);
+        es.pos[k] = id;
+        es.z[k] = lt;
+    }
+    if (__any_sync(0xffffffffu, bad) && lane == 0 && crank == 0) atomicOr(p.status, kErrIdRange);
+    if (dt.mode == kDistillNormalised) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) lmax = fmaxf(lmax, __shfl_xor_sync(0xffffffffu, lmax, o));
+    } else {
+        lmax = 0.f;
+    }
+    P = 0.0;
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32) {
+        // tail: 1 - sum p is what the mass outside is worth, so the sum is formed of terms in double precision
+        float e;
+        if (dt.mode == kDistillTail) { const double x = exp((double)es.z[k]); P += x; e = (float)x; }
+        else { e = expf(es.z[k] - lmax); P += (double)e; }
+        es.p[k] = e;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) P += __shfl_xor_sync(0xffffffffu, P, o);
+    float scale = 1.f, lse = 0.f;
+    if (dt.mode == kDistillNormalised) {
+        scale = P > 0.0 ? (float)(1.0 / P) : (P == P ? 0.f : (float)P);
+        lse = lmax + (float)log(P);
+        P = P > 0.0 ? 1.0 : (P == P ? 0.0 : P);
+    }
+    H = 0.0;
+#pragma unroll
+    for (int c = 0; c < kCluster; ++c) pr[c] = 0.f;
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32) {
+        const float w = es.p[k] * scale;
+        es.p[k] = w;
+        if (!(w == 0.f)) H += (double)w * (double)(es.z[k] - lse);
+        const int id = es.pos[k];
+        const uint32_t v = id < 0 ? 0xffffffffu : (eoff + (uint32_t)id) >> 3;
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c)
+            if (v - (uint32_t)c * slice_vecs < slice_vecs) pr[c] += w;
+        es.pos[k] = v - v0 < nvec ? (int)(eoff + (uint32_t)id - v0 * 8u) : -1;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        H += __shfl_xor_sync(0xffffffffu, H, o);
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) pr[c] += __shfl_xor_sync(0xffffffffu, pr[c], o);
+    }
+}
+
+// Takes the entries' logits out of the row: they become -inf.  Every entry leaves its number in its place and looks whether it
+// is still there: if not, the same entry is named twice.
+template <bool kF16>
+__device__ __forceinline__ bool distill_take_few(const EntrySet& es, uint16_t* row16, int lane)
+{
+    bool twice = false;
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) es.z[k] = El<kF16>::widen(row16[es.pos[k]]);
+    __syncwarp();
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) row16[es.pos[k]] = (uint16_t)k;
+    __syncwarp();
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) twice |= row16[es.pos[k]] != (uint16_t)k;
+    __syncwarp();
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) row16[es.pos[k]] = (uint16_t)El<kF16>::kNegInf;
+    __syncwarp();
+    return twice;
+}
+
+// The first of several equal entries takes the weight of all, added in the order of the list; the others are dropped.
+__device__ __noinline__ void distill_merge_few(const EntrySet es, int lane)
+{
+    __syncwarp();
+    // a lane's new weights and positions wait until every lane has read the old ones: one entry per lane at a time
+    for (int k0 = 0; k0 < es.K; k0 += 32) {
+        const int k = k0 + lane, mine = k < es.K ? es.pos[k] : -1;
+        bool later = false;
+        float w = k < es.K ? es.p[k] : 0.f;
+        if (mine >= 0) {
+            for (int o = 0; o < k; ++o) later |= es.pos[o] == mine;
+            for (int o = k + 1; o < es.K && !later; ++o)
+                if (es.pos[o] == mine) w += es.p[o];
+        }
+        __syncwarp();
+        if (mine >= 0 && !later) es.p[k] = w;                // (read by no entry before it, and dropped ones after it are not)
+        __syncwarp();
+    }
+    for (int k0 = es.K - 1 - (es.K - 1) % 32; k0 >= 0; k0 -= 32) {
+        const int k = k0 + lane, mine = k < es.K ? es.pos[k] : -1;
+        bool later = false;
+        if (mine >= 0)
+            for (int o = 0; o < k; ++o) later |= es.pos[o] == mine;
+        __syncwarp();
+        if (later) { es.pos[k] = -1; es.p[k] = 0.f; }
+        __syncwarp();
+    }
+}
+
+// Sums over the slice's entries against their own largest exponent, and what the consumers and the patch warp need.
+template <int kCluster>
+__device__ __forceinline__ void distill_publish_few(const DistillArgs& dt, float xscale, uint32_t crank, int lane, const EntrySet& es,
+                                                double P, double H, const float (&pr)[kCluster], TargetInfo& target, LabelInfo& lab)
+{
+    float Mt = kFloorM;
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) Mt = fmaxf(Mt, es.z[k] * xscale);
+    // (the largest by the warp-wide integer maximum: the bits of a float, negative ones complemented, order as the floats do)
+    const int bits = __float_as_int(Mt), top = __reduce_max_sync(0xffffffffu, bits ^ ((bits >> 31) & 0x7fffffff));
+    Mt = __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
+    float ey = 0.f, zy = 0.f;
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) {
+            const float x = fmaf(es.z[k], xscale, -Mt);
+            ey += ex2(x);
+            if (!(es.p[k] == 0.f)) zy = fmaf(es.p[k], x, zy);
+        }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        ey += __shfl_xor_sync(0xffffffffu, ey, o);
+        zy += __shfl_xor_sync(0xffffffffu, zy, o);
+    }
+    if (lane == 0) {
+        target.H = H;
+        target.P = (float)P;
+        target.p0 = dt.mode == kDistillTail ? (float)(1.0 - P > 0.0 ? 1.0 - P : 0.0) : 0.f;
+        target.W = !(P == P) ? (float)P : (dt.mode == kDistillTail ? (float)(P > 1.0 ? P : 1.0) : (float)P);
+        float mine = pr[0];
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) {
+            target.pr[c] = pr[c];
+            if ((uint32_t)c == crank) mine = pr[c];
+        }
+        lab = LabelInfo{zy, ey, Mt, mine};
+    }
+}
+
+// The gradients of the entries, as 16-bit patterns in the place of the weights.
+template <bool kF16>
+__device__ __forceinline__ void distill_values_few(const EntrySet& es, const float4& tot, const TargetInfo& ti, float xscale,
+                                               float row_scale, int lane)
+{
+    const float l2 = log2f(tot.y + tot.z);
+#pragma unroll 1
+    for (int k = lane; k < es.K; k += 32)
+        if (es.pos[k] >= 0) {
+            const float q = ex2(fmaf(es.z[k], xscale, -tot.x) - l2);
+            es.p[k] = __uint_as_float(El<kF16>::pack2(row_scale * fmaf(ti.W, q, -es.p[k]), 0.f) & 0xffffu);
+        }
+}
 // ---------------------------------------------------------------- the kernel
 // kTmem: a thread's vectors beyond the first kRegVecsTmem keep their exponentials in tensor memory; otherwise a
 // thread has at most kRegVecsOnly vectors and registers hold all of them.  kF16: logits and gradient are IEEE
@@ -507,6 +694,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     auto t_pos = [&](int i) { return (int*)(zero_buf + kZeroBytesHere + 64) + 3 * (i & (kDistillSets - 1)) * Kpad; };
     auto t_p = [&](int i) { return (float*)t_pos(i) + Kpad; };
     auto t_z = [&](int i) { return (float*)t_pos(i) + 2 * Kpad; };
+    const bool few = kDistill && dt.K <= kDistillFew;
 
     if (tid == 0) {
         for (int b = 0; b < NB; ++b) {
@@ -706,9 +894,29 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
             if (aborted) break;
             const TargetRow tr = s_trow[i & (kDistillRows - 1)];
             if (tr.entries < 0) break;
-            int pos[kPer];
-            float pk[kPer], pr[kCluster];
+            float pr[kCluster];
             double P, H;
+            if (few) {
+                const EntrySet es{t_pos(i), t_p(i), t_z(i), dt.K};
+                // the set's previous row has been patched (nothing to wait for in the first turn)
+                mbar_wait(spare(i), set_phase(i) ^ 1u, p.status, aborted, p.wait_limit_ns);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted) break;
+                distill_weights_few<kCluster>(p, dt, tr.entries, tr.eoff, v0, nvec, ca.slice_vecs, crank, lane, es, P, H, pr);
+                mbar_wait(landed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted) break;
+                const bool again = distill_take_few<kF16>(es, (uint16_t*)(smem + (size_t)buf * ca.buf_stride), lane);
+                if (lane == 0) mbar_arrive(ready(buf));
+                if (__any_sync(0xffffffffu, again)) distill_merge_few(es, lane);
+                distill_publish_few<kCluster>(dt, xscale, crank, lane, es, P, H, pr, s_target[i & (kDistillSets - 1)],
+                                              s_tlab[i & (kDistillSets - 1)]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(told(i));
+                continue;
+            }
+            int pos[kPer];
+            float pk[kPer];
             distill_weights<kCluster>(p, dt, tr.entries, tr.eoff, v0, nvec, ca.slice_vecs, crank, lane, pos, pk, P, H, pr);
             // the logits leave the buffer.  Every entry leaves its number in its place and looks whether it is still
             // there: if not, the same entry is named twice.
@@ -766,29 +974,43 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
             // the gradients of the entries, while the consumers write the others
             const float4 tot = s_total[i & (kDistillSets - 1)];      // M, mass outside, mass of the entries, sum p (x - M)
             const TargetInfo ti = s_target[i & (kDistillSets - 1)];
-            const float l2 = log2f(tot.y + tot.z);
-            int pos[kPer];
-            uint32_t value[kPer];
+            if (few) {
+                const EntrySet es{t_pos(i), t_p(i), t_z(i), dt.K};
+                distill_values_few<kF16>(es, tot, ti, xscale, row_scale, lane);
+                mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted) break;
+                uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
+#pragma unroll 1
+                for (int k = lane; k < dt.K; k += 32)
+                    if (es.pos[k] >= 0) row16[es.pos[k]] = (uint16_t)__float_as_uint(es.p[k]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(spare(i));                // the set has been read
+            } else {
+                const float l2 = log2f(tot.y + tot.z);
+                int pos[kPer];
+                uint32_t value[kPer];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const int k = lane + 32 * j;
-                pos[j] = -1;
-                value[j] = 0;
-                if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(i)[k];
-                if (32 * j < dt.K && pos[j] >= 0) {
-                    const float q = ex2(fmaf(t_z(i)[k], xscale, -tot.x) - l2);
-                    value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -t_p(i)[k]), 0.f) & 0xffffu;
+                for (int j = 0; j < kPer; ++j) {
+                    const int k = lane + 32 * j;
+                    pos[j] = -1;
+                    value[j] = 0;
+                    if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(i)[k];
+                    if (32 * j < dt.K && pos[j] >= 0) {
+                        const float q = ex2(fmaf(t_z(i)[k], xscale, -tot.x) - l2);
+                        value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -t_p(i)[k]), 0.f) & 0xffffu;
+                    }
                 }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(spare(i));                    // the set has been read
-            mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
-            aborted = __any_sync(0xffffffffu, aborted);
-            if (aborted) break;
-            uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(spare(i));                    // the set has been read
+                mbar_wait(computed(buf), (uint32_t)(i / NB) & 1u, p.status, aborted, p.wait_limit_ns);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted) break;
+                uint16_t* row16 = (uint16_t*)(smem + (size_t)buf * ca.buf_stride);
 #pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (32 * j < dt.K && pos[j] >= 0) row16[pos[j]] = (uint16_t)value[j];
+                for (int j = 0; j < kPer; ++j)
+                    if (32 * j < dt.K && pos[j] >= 0) row16[pos[j]] = (uint16_t)value[j];
+            }
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
