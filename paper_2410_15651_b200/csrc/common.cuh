@@ -262,6 +262,14 @@ __device__ inline long long block_count_valid(const int* __restrict__ lengths, i
     return scratch[32];
 }
 
+// log2 of a positive fp32 number to 2^-24: the exponent exactly, the mantissa's logarithm (below 1) in fp32.
+__device__ __forceinline__ double log2_split(float v)
+{
+    int e;
+    const float m = frexpf(v, &e);                           // in [1/2, 1)
+    return (double)e + (double)log2f(m);
+}
+
 // Number of sequences with at least one valid token, by the whole block (same scratch and barriers as above).
 __device__ inline long long block_count_nonempty(const int* __restrict__ lengths, int B, long long* scratch)
 {

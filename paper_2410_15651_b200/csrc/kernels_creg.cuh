@@ -143,14 +143,6 @@ __device__ __forceinline__ float distill_factor(const TargetInfo& ti, float s, f
     return ti.p0 > 0.f && s > 0.f ? ti.W - ti.p0 / q0 : ti.P;
 }
 
-// log2 of a positive fp32 number to 2^-24: the exponent exactly, the mantissa's logarithm (below 1) in fp32.
-__device__ __forceinline__ double log2_split(float v)
-{
-    int e;
-    const float m = frexpf(v, &e);                           // in [1/2, 1)
-    return (double)e + (double)log2f(m);
-}
-
 // Loss of a row.  With x the scaled logits and M a reference, zy = sum_k p_k (x_k - M); s and ey are the sums of 2^(x-M)
 // over the other and over the teacher's entries.
 __device__ __forceinline__ double distill_loss(const TargetInfo& ti, float zy, float s, float ey)

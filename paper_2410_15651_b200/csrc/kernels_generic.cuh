@@ -92,12 +92,12 @@ __device__ __forceinline__ float exp_excess(float d)
     return s * d * d;
 }
 
-// The row's log-prob from its partition sum, for the objectives beside step 4: the difference x_y - M is rounded once
-// and log2 of the sum is small, so the result is good to a few units in its own last place (row_finish forms lse first,
-// whose last place is that of the largest logit).
+// The row's log-prob from its partition sum, for the objectives beside step 4, rounded once: the terms are combined in double
+// precision, so that what remains is the sum's own error (row_finish forms lse first, whose last place is that of the largest
+// logit).  For one thread of a row.
 __device__ __forceinline__ float lp_relative(const Acc& a, float zy)
 {
-    return kLn2 * (fmaf(zy, kLog2e, -a.M) - log2f(a.s + a.ey));
+    return (float)(0.6931471805599453 * ((double)zy * (double)kLog2e - (double)a.M - log2_split(a.s + a.ey)));
 }
 
 // A token of kObjPolicyKl.  A whole block waits for the gradient once per row, so that it forms it by a short chain on the

@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_block_kernel(BlockLpArg
             float zt = kTopkFloor, st = 0.f;
             for (int w = 0; w < NT / 32; ++w) zt = fmaxf(zt, s_part[par][w].x);
             for (int w = 0; w < NT / 32; ++w) st += s_part[par][w].y * ex2((s_part[par][w].x - zt) * kLog2e);
-            p.out_lp[row] = bad_id ? 0.f : kLn2 * fmaf(zy - zt, kLog2e, -log2f(st));
+            p.out_lp[row] = bad_id ? 0.f : (float)(0.6931471805599453 * ((double)(zy - zt) * (double)kLog2e - log2_split(st)));
         }
     }
     if (blockIdx.x == 0) block_count_valid(p.lengths, p.B, p.T, s_cnt, p.status);   // flags lengths out of range
