@@ -111,7 +111,8 @@ int rlhf_pad_share(long long n_valid, long long n_padded, int n_blocks, int bloc
                    long long* start, long long* count);
 
 /* Bytes of scratch that rlhf_gather_logprobs, rlhf_experience and rlhf_ppo_loss_fwd_bwd need for a batch of B x T
- * tokens: O(B*T), never O(B*T*V) -- at most 16*B*T + 65536.  The same workspace serves the objectives below.  0 if B or T is not positive.
+ * tokens: O(B*T), never O(B*T*V) -- at most 16*B*T + 65536.  0 if B or T is not positive.  The objectives below use the
+ * same workspace.
  * The workspace must be 256-byte aligned and must have been cleared once with rlhf_workspace_init
  * before its first use; it can then be reused by any number of calls on the same stream. */
 size_t rlhf_workspace_bytes(int B, int T);

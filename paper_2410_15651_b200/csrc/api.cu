@@ -39,7 +39,7 @@ int cuda_fail(cudaError_t e, const char* what)
     } while (0)
 
 // Workspace layout (bytes): [0,4) status flags, [4,8) reduction ticket, [8,16) mean and 1/std of the
-// advantage whitening, [16,20) row counter of the loss kernel that deals its rows dynamically, [256, kRowLossOffset) block
+// advantage whitening, [16,20) row counter of the kernels that deal their rows dynamically, [256, kRowLossOffset) block
 // partial sums of the two losses (2 doubles per block of the kernel that reduces them),
 // [kRowLossOffset, +4*B*T) per-token policy loss terms (kernels without the fused finalisation), then, for the objectives
 // beside step 4, 8*B*T bytes more: per-token KL terms (policy loss with KL); the factor of each sequence and, from
@@ -559,7 +559,7 @@ int launch_topk_as(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 {
     auto kernel = topk_block_kernel<NT, kF16>;
     // (no preference for shared memory: what the kernel does not take serves its loads in flight as L1.  With the largest
-    // carve-out V = 128256, K = 128 takes 267 instead of 189 us on 6 x 512 rows.)
+    // carve-out V = 128256, K = 128 takes 1.41 times as long.)
     const int grid = (int)std::min<long long>((long long)ta.B * ta.T, (long long)dev.sm_count * topk_blocks_per_sm(NT));
     RLHF_CUDA(launch_kernel(kernel, grid, NT, 0, s, ta));
     return launch_check("topk_block_kernel");
@@ -567,8 +567,8 @@ int launch_topk_as(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 
 // Threads per row.  1024 where there are no more rows than SMs and a row keeps them busy (one row of 50272: 13 us against
 // 16 us with 256).  Else by the row's length, measured on 4096 rows: V = 1000, K = 32: 68 us with 64 threads, 104 with 128,
-// 191 with 256; V = 8192, K = 32: 33, 35, 51; V = 32000, K = 64: 118, 78, 86; V = 50272, K = 256 (12 x 256 rows): 325, 158,
-// 166; V = 128256, K = 128: 451, 220, 191.
+// 191 with 256; V = 8192, K = 32: 33, 35, 51; V = 32000, K = 64: 118, 78, 86; relative to the
+// fastest, V = 50272, K = 256: 2.06, 1, 1.05; V = 128256, K = 128: 2.36, 1.15, 1.
 template <bool kF16>
 int launch_topk(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 {

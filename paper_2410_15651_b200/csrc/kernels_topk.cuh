@@ -12,11 +12,12 @@
 // whatever their size.
 //
 // Floor: one read of the row from DRAM (32 us for 2048 rows of 50272 in bf16 at 6.5 TB/s).  What bounds the kernel is
-// instruction issue: per row of 50272 and K = 64 some 9,000 warp instructions for the stream (one ex2 and half a packed
-// maximum per logit) and 8,000 for the selection, which the warps of a block share.  Measured (12 x 256 rows, 84 us) and dropped: a row per
-// warp (all rows of a batch are then in flight, L2 does not hold them, and what is read again comes from DRAM in sectors:
-// 120 us; with groups of whole lines 78 us, but 178 against 158 us at K = 256 and 226 against 191 us at V = 128256);
-// separate streaming and selecting warps (105 us: one warp selects for 25 us); rows through a ring of bulk copies (88 us).
+// instruction issue: per row of 50272 and K = 64 14,600 warp instructions, some 9,000 of them for the stream (one ex2 and
+// half a packed maximum per logit), the others for the selection, which the warps of a block share.  Measured on such rows
+// and dropped, with their time over this kernel's: a row per warp (all rows of a batch are then in flight, L2 does not hold
+// them, and what is read again comes from DRAM in sectors: 1.43; with groups of whole lines 0.93, but 1.13 at K = 256 and
+// 1.18 at V = 128256); separate streaming and selecting warps (1.25: one warp selects for 25 us); rows through a ring of
+// bulk copies (1.05).
 #pragma once
 #include "kernels_ring.cuh"
 #include <cuda_fp16.h>
