@@ -307,7 +307,7 @@ int rlhf_ppo_stats(const float* lp_new, const float* lp_old, const float* adv, c
  * positions both outputs are 0.  One streaming read of each valid row.
  *   logits          bf16 or binary16 (logits_dtype) through (stride_b, stride_t)   read
  *   out_ids         int32 [B,T,K], out_logprobs fp32 [B,T,K], contiguous           written
- *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE; K may exceed V); temperature > 0, finite.   workspace as for step 1.
+ *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE; K may exceed V); temperature in [1e-3, 1e18].   workspace as for step 1.
  */
 #define RLHF_TOPK_MAX 256
 int rlhf_topk_logprobs(const void* logits, int logits_dtype, long long stride_b, long long stride_t, const int* lengths,
@@ -333,12 +333,14 @@ typedef enum {
  * [0,V) set RLHF_ERR_ID_RANGE and count as unused.  A token without entries adds 0 to a plain or normalised loss.  Where no
  * vocabulary entry is left outside S, or their mass is below the range of fp32, the tail term is left out.  A deleted
  * student entry (-inf) with p_k > 0 makes the loss infinite, as the definition has it.
+ * Finite logits must satisfy |z| / temperature <= 1e9.  A gradient below 2^-62 may be written as 0, and so may that of an
+ * entry with q_v < 2^-126.
  *   logits, lengths, out_dlogits   as step 4 (logits_dtype: rlhf_dtype_t of both tensors; in place allowed)
  *   topk_ids, topk_logprobs   int32 / fp32, [b*topk_stride_b + t*topk_stride_t + k], strides >= 0 in elements; the
  *                  log-probs are the teacher's at this temperature                                    read
  *   out_loss       fp32 scalar (device)                                                               written
  *   out_row_loss   fp32 [B,T] or NULL: temperature^2 L of every token, 0 at padding                   written if given
- *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE); temperature > 0, finite.   workspace as for step 1.
+ *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE); temperature in [1e-3, 1e18].   workspace as for step 1.
  */
 int rlhf_distill_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
                               const int* topk_ids, const float* topk_logprobs, long long topk_stride_b,
@@ -368,7 +370,8 @@ typedef enum {
  *   adv              fp32, adv[b*adv_stride_b + t*adv_stride_t] (strides in elements, >= 0; adv_stride_t = 0 for one
  *                    advantage per sequence)                           read
  *   out_loss_pg, out_loss_kl   fp32 scalars (device)                   written
- *   clip_low in (0,1), clip_high > 0, kl_coef >= 0, all finite.   workspace as for step 1.
+ *   clip_low in (0,1), clip_high > 0, kl_coef >= 0, all finite.   out_lp_new must not overlap lp_old, lp_ref or adv
+ *   (RLHF_ERR_STRIDE).   workspace as for step 1.
  */
 int rlhf_policy_kl_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
                                 const long long* ids, long long ids_stride_b, const int* lengths,
@@ -400,7 +403,7 @@ typedef enum {
  *   out_loss       fp32 scalar (device)                                written
  *   out_rewards    fp32 [B]                                            written
  *   B even (else RLHF_ERR_SHAPE); beta > 0; label_smoothing in [0, 1/2), 0 unless RLHF_PREF_SIGMOID; length_mean 0 or 1.
- *   workspace as for step 1.
+ *   out_lp_new must not overlap lp_ref (RLHF_ERR_STRIDE).   workspace as for step 1.
  */
 int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
                                  const long long* ids, long long ids_stride_b, const int* lengths, const float* lp_ref,

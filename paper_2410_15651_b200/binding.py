@@ -537,7 +537,8 @@ def distill_loss_fwd_bwd(logits: torch.Tensor, topk_ids: torch.Tensor, topk_logp
         raise ValueError(f"topk_ids and topk_logprobs must be [{B},{T},K]")
     K = topk_ids.shape[2]
     ksb, kst, ks = topk_ids.stride()
-    if topk_logprobs.stride() != (ksb, kst, ks) or (K > 1 and ks != 1):
+    lsb, lst, ls = topk_logprobs.stride()                # (the stride of an axis with one position says nothing)
+    if (B > 1 and ksb != lsb) or (T > 1 and kst != lst) or (K > 1 and (ks != 1 or ls != 1)):
         raise ValueError("topk_ids and topk_logprobs must have the same strides and a contiguous last axis")
     if out is None:
         out = DistillOutputs(logits)

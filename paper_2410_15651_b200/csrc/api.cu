@@ -459,6 +459,16 @@ int check_rows(const void* logits, int logits_dtype, long long stride_b, long lo
     return RLHF_OK;
 }
 
+// Temperatures whose square is a number in fp32, and that leave logits of 1e6 below 1e9.  (NaN is none.)
+bool temperature_ok(float t) { return t >= 1e-3f && t <= 1e18f; }
+
+// The two [B,T] fp32 arrays share bytes (null: they do not).
+bool overlap(const float* a, const float* b, int B, int T)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), n = 4 * (uintptr_t)B * (uintptr_t)T;
+    return a && b && x < y + n && y < x + n;
+}
+
 // Host-side checks of the loss call's arguments, the workspace apart (shared by the two loss entry points).
 int check_loss_args(const void* logits, long long stride_b, long long stride_t, const long long* ids,
                     long long ids_stride_b, const int* lengths, const float* lp_old, const float* adv,
@@ -793,7 +803,7 @@ int rlhf_topk_logprobs(const void* logits, int logits_dtype, long long stride_b,
     if (int e = check_shape(B, T, V)) return e;
     if (K <= 0 || K > RLHF_TOPK_MAX) return RLHF_ERR_SHAPE;
     if (stride_b < 0 || stride_t < 0 || (T > 1 && stride_t < V)) return RLHF_ERR_STRIDE;
-    if (!std::isfinite(temperature) || !(temperature > 0.f)) return RLHF_ERR_SCALAR;
+    if (!temperature_ok(temperature)) return RLHF_ERR_SCALAR;
     if (!aligned(logits, 2) || !aligned(lengths, 4) || !aligned(out_ids, 4) || !aligned(out_logprobs, 4)) return RLHF_ERR_ALIGN;
     if (int e = check_workspace(workspace, workspace_bytes, rlhf_workspace_bytes(B, T))) return e;
     DeviceInfo dev;
@@ -1107,6 +1117,11 @@ int rlhf_policy_kl_loss_fwd_bwd(const void* logits, int logits_dtype, long long 
     if (!aligned(ids, 8) || !aligned(lengths, 4) || !aligned(lp_old, 4) || !aligned(lp_ref, 4) || !aligned(adv, 4) ||
         !aligned(out_loss_pg, 4) || !aligned(out_loss_kl, 4) || !aligned(out_lp_new, 4))
         return RLHF_ERR_ALIGN;
+    const uintptr_t adv_begin = reinterpret_cast<uintptr_t>(adv), lp_begin = reinterpret_cast<uintptr_t>(out_lp_new);
+    const uintptr_t adv_bytes = 4 * ((uintptr_t)(B - 1) * (uintptr_t)adv_stride_b + (uintptr_t)(T - 1) * (uintptr_t)adv_stride_t + 1);
+    if (overlap(out_lp_new, lp_old, B, T) || overlap(out_lp_new, lp_ref, B, T) ||
+        (out_lp_new && lp_begin < adv_begin + adv_bytes && adv_begin < lp_begin + 4 * (uintptr_t)B * (uintptr_t)T))
+        return RLHF_ERR_STRIDE;
     if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
     DeviceInfo dev;
     if (int e = device_info(dev)) return e;
@@ -1182,6 +1197,7 @@ int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long
     if (!aligned(ids, 8) || !aligned(lengths, 4) || !aligned(lp_ref, 4) || !aligned(out_loss, 4) ||
         !aligned(out_rewards, 4) || !aligned(out_lp_new, 4))
         return RLHF_ERR_ALIGN;
+    if (overlap(out_lp_new, lp_ref, B, T)) return RLHF_ERR_STRIDE;
     if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
     DeviceInfo dev;
     if (int e = device_info(dev)) return e;
@@ -1247,7 +1263,7 @@ int rlhf_distill_loss_fwd_bwd(const void* logits, int logits_dtype, long long st
         return e;
     if (topk_stride_b < 0 || topk_stride_t < 0) return RLHF_ERR_STRIDE;
     if ((mode != RLHF_DISTILL_PLAIN && mode != RLHF_DISTILL_NORMALISED && mode != RLHF_DISTILL_TAIL) ||
-        !std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(grad_scale))
+        !temperature_ok(temperature) || !std::isfinite(grad_scale))
         return RLHF_ERR_SCALAR;
     if (!aligned(topk_ids, 4) || !aligned(topk_logprobs, 4) || !aligned(lengths, 4) || !aligned(out_loss, 4) ||
         !aligned(out_row_loss, 4))

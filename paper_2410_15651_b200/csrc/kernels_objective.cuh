@@ -116,7 +116,7 @@ __device__ inline void pair_objective(int kind, double h, double beta, double e,
         const double lo = x / (1.0 + x), hi = 1.0 / (1.0 + x);         // sigma(-|h|), sigma(|h|)
         const double nl_pos = h >= 0.0 ? soft : soft - h;              // -log sigma(h)
         const double nl_neg = h >= 0.0 ? soft + h : soft;              // -log sigma(-h)
-        loss = (1.0 - e) * nl_pos + e * nl_neg;
+        loss = (1.0 - e) * nl_pos + (e == 0.0 ? 0.0 : e * nl_neg);     // (h = +inf, a rejected token that is deleted: 0)
         dh = e * (h >= 0.0 ? hi : lo) - (1.0 - e) * (h >= 0.0 ? lo : hi);
     } else if (kind == kPrefHinge) {
         loss = 1.0 - h > 0.0 ? 1.0 - h : 0.0;

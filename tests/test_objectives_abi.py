@@ -127,3 +127,31 @@ def test_binding_says_what_is_wrong_with_cpu_tensors():
                  lambda: binding.preference_loss_fwd_bwd(z, ids, n, f, 0, 0.1, 0.0, 0.0, False, 1.0, ws)):
         with pytest.raises(ValueError, match="CUDA tensor"):
             call()
+
+
+def test_temperatures_whose_scale_or_square_leaves_fp32(lib, p):
+    names = "logits dtype sb st lengths B T V K tau oid olp ws wsn stream".split()
+    topk = caller(lib, "rlhf_topk_logprobs", names, dict(rows(p, lib.rlhf_workspace_bytes(2, 4)), K=4, tau=1.0, oid=p, olp=p))
+    names = "logits dtype sb st tid tlp ksb kst K lengths B T V mode tau gs loss row dl dsb dst ws wsn stream".split()
+    d = dict(rows(p, lib.rlhf_workspace_bytes(2, 4)), tid=p, tlp=p, ksb=16, kst=4, K=4, mode=0, tau=1.0, gs=1.0, loss=p, row=None)
+    distill = caller(lib, "rlhf_distill_loss_fwd_bwd", names, d)
+    for tau in (1e-45, 1e-39, 1e-30, 0.9e-3, 1.1e18, 1e20, 3e38):
+        assert topk(tau=tau) == SCALAR and distill(tau=tau) == SCALAR, tau
+    for tau in (1e-3, 1e18):                             # accepted: the next check answers
+        assert topk(tau=tau, wsn=100) == WORKSPACE and distill(tau=tau, wsn=100) == WORKSPACE
+
+
+def test_log_probs_written_over_an_input(lib, p):
+    names = "logits dtype sb st ids isb lengths lp_ref B T V kind beta margin eps mean gs loss rew dl dsb dst lpn ws wsn stream".split()
+    d = dict(rows(p, lib.rlhf_workspace_bytes(2, 4)), lp_ref=p + 256, kind=0, beta=0.1, margin=0.0, eps=0.0, mean=0, gs=1.0,
+             loss=p, rew=p, lpn=p + 512)
+    call = caller(lib, "rlhf_preference_loss_fwd_bwd", names, d)
+    assert call(lpn=p + 256) == STRIDE and call(lpn=p + 256 + 4) == STRIDE and call(lpn=p + 256 - 4) == STRIDE
+    assert call(wsn=100) == WORKSPACE and call(wsn=100, lpn=p + 256 + 32) == WORKSPACE
+    names = "logits dtype sb st ids isb lengths lp_old lp_ref adv asb ast B T V lo hi kl red gs lpg lkl dl dsb dst lpn ws wsn stream".split()
+    d = dict(rows(p, lib.rlhf_workspace_bytes(2, 4)), lp_old=p + 256, lp_ref=p + 512, adv=p + 768, asb=4, ast=1, lo=0.2, hi=0.3,
+             kl=0.1, red=0, gs=1.0, lpg=p, lkl=p + 4, lpn=p + 2048)
+    call = caller(lib, "rlhf_policy_kl_loss_fwd_bwd", names, d)
+    for at in (256, 512, 768):
+        assert call(lpn=p + at) == STRIDE and call(lpn=p + at + 4) == STRIDE, at
+    assert call(wsn=100) == WORKSPACE
