@@ -98,12 +98,14 @@ __device__ __forceinline__ void acc_rebase(Acc& a, float newM)
     a.M = newM;
 }
 
-// One element, any order; used by the scalar kernels.
+// One element, any order; used by the scalar kernels.  kApart: the exponent is not rounded before M is taken off, for rows
+// far from 0.
+template <bool kApart = false>
 __device__ __forceinline__ void acc_add(Acc& a, float z, bool is_label)
 {
     float x = z * kLog2e;
     if (x - a.M > kRebase) acc_rebase(a, x);
-    float e = ex2(x - a.M);
+    float e = ex2(kApart ? fmaf(z, kLog2e, -a.M) : x - a.M);
     if (is_label) a.ey = e; else a.s += e;
 }
 

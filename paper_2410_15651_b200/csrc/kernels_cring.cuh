@@ -685,7 +685,11 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 release(c);
             }
         } else {
-            const float mag = ex2(M + (lg2(fabsf(g)) - r.lse2));       // |g| 2^M / sum, M this thread's reference
+            // |g| 2^(M - tot.M) / sum, M this thread's reference.  (Step 4 through lse, whose last place is that of the largest
+            // exponent; the others without it, for rows far from 0 and small temperatures.)
+            const float mag = kDistill || p.objective != kObjPpo
+                                  ? ex2((M - tot.M) + (lg2(fabsf(g)) - lg2(tot.s + tot.ey)))
+                                  : ex2(M + (lg2(fabsf(g)) - r.lse2));
             const float2 sc2 = splat2(g > 0.f ? -mag : mag);
             const float dy = g * r.one_m_py;
             auto emit = [&](auto last, const float2 (&ev)[4], int j, uint4* chunk, int u) {

@@ -198,7 +198,6 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRow
 
         // ---- pass 2: the gradient
         const float f = row_scale * distill_factor(ti, tot.y, tot.y / (tot.y + tot.z));
-        const float c2 = -(tot.x + l2);
         for (uint32_t v = tid; v < r.nvec; v += kDistillThreads) {
             const uint4 q = *(r.vecs + v);
             float zz[8];
@@ -206,7 +205,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRow
             const bool named = may_hold(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                zz[i] = f == 0.f ? 0.f : f * ex2(fmaf(zz[i], dt.scale, c2));
+                zz[i] = f == 0.f ? 0.f : f * ex2(fmaf(zz[i], dt.scale, -tot.x) - l2);
                 const int e = (int)(v * 8u + (uint32_t)i) - (int)r.eoff;
                 if (named && e >= 0 && e < p.V) {
                     const int k = distill_find(s_tab, e);

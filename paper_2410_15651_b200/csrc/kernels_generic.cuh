@@ -191,8 +191,11 @@ __global__ void __launch_bounds__(kGenericThreads) row_generic_kernel(RowArgs p)
         // every thread reads z_y before the block barrier, i.e. before any in-place write of this row
         const float zy = El<kF16>::widen(row[y]);
         Acc a = acc_empty();
-        for (int v = threadIdx.x; v < p.V; v += blockDim.x)
-            acc_add(a, El<kF16>::widen(row[v]), v == (int)y);
+        const bool apart = kLoss && p.objective != kObjPpo;
+        if (apart)
+            for (int v = threadIdx.x; v < p.V; v += blockDim.x) acc_add<true>(a, El<kF16>::widen(row[v]), v == (int)y);
+        else
+            for (int v = threadIdx.x; v < p.V; v += blockDim.x) acc_add(a, El<kF16>::widen(row[v]), v == (int)y);
         a = block_merge(a, s_acc);
         RowResult r = row_finish(a, zy);
 
@@ -212,11 +215,13 @@ __global__ void __launch_bounds__(kGenericThreads) row_generic_kernel(RowArgs p)
             for (int v = threadIdx.x; v < p.V; v += blockDim.x) drow[v] = 0;
         } else {
             // |g| * p_v = 2^(x_v - lse2 + log2|g|); the sign is applied to the packed result
-            const float c2 = log2f(fabsf(g)) - r.lse2;
+            // (as one constant in step 4; beside it as -M and the rest, which keeps its last places in rows far from 0)
+            const float c2 = apart ? -a.M : log2f(fabsf(g)) - r.lse2;
+            const float rest = apart ? log2f(fabsf(g)) - log2f(a.s + a.ey) : 0.f;
             const uint16_t sign = g > 0.f ? 0x8000u : 0u;
             for (int v = threadIdx.x; v < p.V; v += blockDim.x) {
                 float z = El<kF16>::widen(row[v]);                    // read before the in-place write
-                float d = ex2(fmaf(z, kLog2e, c2));
+                float d = ex2(fmaf(z, kLog2e, c2) + rest);
                 uint16_t h = (uint16_t)(El<kF16>::pack2(d, 0.f) & 0xffffu) ^ sign;
                 if (v == (int)y) h = (uint16_t)(El<kF16>::pack2(g * r.one_m_py, 0.f) & 0xffffu);
                 drow[v] = h;

@@ -209,25 +209,27 @@ __device__ __forceinline__ uint4 mask_vec_outside(const uint4& q, int jlo, int j
 }
 
 // dlogits for 8 entries: sign * 2^(x + c2), packed to bf16.  The scaling runs two entries at a time on
-// the packed fp32x2 FMA of sm_100; the exponentials stay on the special-function unit.
-template <bool kF16 = false>
-__device__ __forceinline__ uint4 grad_vec(const uint4& q, float c2, uint32_t sign2)
+// the packed fp32x2 FMA of sm_100; the exponentials stay on the special-function unit.  kApart: 2^((x + c2) + rest), for
+// the objectives beside step 4 (c2 = -M alone, see row_generic_kernel).
+template <bool kF16 = false, bool kApart = false>
+__device__ __forceinline__ uint4 grad_vec(const uint4& q, float c2, uint32_t sign2, float rest = 0.f)
 {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
     uint32_t o[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const float2 x = __ffma2_rn(El<kF16>::unpack2(w[k]), splat2(kLog2e), splat2(c2));
+        float2 x = __ffma2_rn(El<kF16>::unpack2(w[k]), splat2(kLog2e), splat2(c2));
+        if (kApart) x = __fadd2_rn(x, splat2(rest));
         o[k] = El<kF16>::pack2(ex2(x.x), ex2(x.y)) ^ sign2;
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-template <int U, bool kF16 = false>
-__device__ __forceinline__ void grad_vecs(const uint4 (&q)[U], uint4 (&o)[U], float c2, uint32_t sign2)
+template <int U, bool kF16 = false, bool kApart = false>
+__device__ __forceinline__ void grad_vecs(const uint4 (&q)[U], uint4 (&o)[U], float c2, uint32_t sign2, float rest = 0.f)
 {
 #pragma unroll
-    for (int u = 0; u < U; ++u) o[u] = grad_vec<kF16>(q[u], c2, sign2);
+    for (int u = 0; u < U; ++u) o[u] = grad_vec<kF16, kApart>(q[u], c2, sign2, rest);
 }
 
 template <bool kF16 = false>
@@ -545,7 +547,9 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
         if (ra.resident) { slot = slot0; phase = phase0; }
         unsigned char* dst = (unsigned char*)(p.dlogits + (long long)b * p.dl_stride_b + (long long)t * p.dl_stride_t) +
                              (size_t)tid * 16;
-        const float c2 = log2f(fabsf(g)) - r.lse2;
+        const bool apart = p.objective != kObjPpo;
+        const float c2 = apart ? -tot.M : log2f(fabsf(g)) - r.lse2;
+        const float rest = apart ? log2f(fabsf(g)) - log2f(tot.s + tot.ey) : 0.f;
         const uint32_t sign2 = g > 0.f ? 0x80008000u : 0u;
         const float dy = g * r.one_m_py;
         for (int c = 0; c < chunks; ++c, dst += kChunk) {
@@ -556,7 +560,8 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
 #pragma unroll
                 for (int u = 0; u < U; ++u) q[u] = src[u * kCons];
                 uint4 o[U];
-                grad_vecs<U>(q, o, c2, sign2);
+                if (apart) grad_vecs<U, false, true>(q, o, c2, sign2, rest);
+                else grad_vecs<U>(q, o, c2, sign2);
 #pragma unroll
                 for (int u = 0; u < U; ++u) store_v4(dst + (size_t)u * kCons * 16, o[u]);
             } else {
@@ -567,7 +572,7 @@ __global__ void __launch_bounds__(NW * 32 + 32, NW == 16 ? 1 : 3) row_ring_kerne
                     if (v < nvec) {
                         uint4 o = make_uint4(0, 0, 0, 0);
                         if (g != 0.f) {
-                            o = grad_vec(src[u * kCons], c2, sign2);
+                            o = apart ? grad_vec<false, true>(src[u * kCons], c2, sign2, rest) : grad_vec(src[u * kCons], c2, sign2);
                             if (v == yvec) patch_label(o, yj, dy);
                         }
                         store_v4(dst + (size_t)u * kCons * 16, o);

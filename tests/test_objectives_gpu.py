@@ -343,19 +343,28 @@ def teacher_entries(z, K, temperature, gen, noise=1.0):
     return ids, lt
 
 
-def check_distill(z, ids, lt, lengths, mode, temperature, scale, out=None, z64=None):
+def check_distill(z, ids, lt, lengths, mode, temperature, scale, out=None, z64=None, reach=64):
     B, T, V = z.shape
     z64 = z.double() if z64 is None else z64
     ws = lib.workspace(B, T, DEV)
     got = lib.distill_loss_fwd_bwd(z, ids, lt, lengths, mode, temperature, scale, ws, out)
     loss, rows, d, parts = ref.distill(z64, ids, lt, lengths, mode, temperature, scale)
     # a row's loss is a sum of p (log p - log q) with sum p <= 1 (+ p_0 of the same kind): every log is off by LP at most,
-    # and the weights' relative errors (2^-22) meet logs below 64
-    each = temperature ** 2 * (2 * LP + 2 ** -22 * 64)
+    # and the weights' relative errors (2^-22) meet logs below 64.  Where |x - M| reaches further, every rounding of it, and
+    # the logs that the weights meet, grow in proportion.
+    each = temperature ** 2 * (2 * LP + 2 ** -22 * 64) * reach / 64
     if got.row_loss is not None:
         off = (got.row_loss.double() - rows).abs()
         assert (off <= each + 2 ** -23 * rows.abs()).all(), off.max().item()
     assert abs(got.loss.item() - loss.item()) <= each + 2 ** -23 * abs(loss.item())
+    if reach > 64:
+        # An entry outside the list is e * mag with e = 2^(x - M) and mag = |g| 2^(M - Mmax) / sum; a thread's M is such that
+        # e <= 2^64, and fp32 flushes below 2^-126: mag's flush loses at most 2^64 * 2^-126 = 2^-62, that of e at most |g| * 2^-126.
+        q = torch.softmax(z64 / temperature, dim=2)
+        outside = torch.ones_like(q).scatter_(2, ids.long().clamp(min=0), 0.0).bool() & (q > 0)
+        g = torch.where(outside, parts / q.clamp(min=1e-300), 0.0).amax(dim=2, keepdim=True)
+        lost = (2.0 ** -62 + g * 2.0 ** -126).expand_as(d)
+        parts = parts + lost / LP
     check_gradient(got.dlogits, d, parts)
     return got, ws
 
@@ -476,3 +485,106 @@ def test_distill_without_tokens_and_lengths_out_of_range():
         assert (got.loss == 0).all() and (got.dlogits == 0).all() and lib.poll_status(ws) == 0
         _, ws = check_distill(z, ids, lt, torch.tensor([9, -1, 2], dtype=torch.int32, device=DEV), 2, 1.0, 1.0)
         assert lib.poll_status(ws) == 32
+
+
+def test_preference_with_deleted_tokens():
+    """A response that holds a token its row deletes has log-prob -inf.  Where it is the rejected one, h = +inf: the pair is won
+    (loss 0, no gradient).  Where it is the chosen one the loss is infinite and the gradient that of h -> -inf: f = -beta."""
+    gen = torch.Generator(device=DEV).manual_seed(51)
+    for T, V in ((3, 1000), (3, 20000), (700, 8200)):
+        B = 4
+        z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+        ids, lengths = labels(B, T, V, gen), torch.full((B,), T, dtype=torch.int32, device=DEV)
+        z[2, 1, ids[2, 1]] = float("-inf")               # pair 0: the rejected response
+        ws = lib.workspace(B, T, DEV)
+        for kind in (lib.PREF_SIGMOID, lib.PREF_HINGE):
+            got = lib.preference_loss_fwd_bwd(z, ids, lengths, None, kind, 0.01, 0.0, 0.0, False, 1.0, ws)
+            _, lp, _ = ref.label_logprobs(z.double(), ids, lengths)
+            h = 0.01 * (lp[1].sum() - lp[3].sum())
+            want = (torch.nn.functional.softplus(-h) if kind == 0 else (1 - h).clamp(min=0)) / 2
+            # T log-probs of LP each, twice, times beta; both losses' slope in h is at most 1
+            assert abs(got.loss.item() - want.item()) <= 0.01 * T * LP + 2.0 ** -23 * want.item()
+            assert got.rewards[2].item() == float("-inf") and torch.isfinite(got.rewards[[0, 1, 3]]).all()
+            assert (got.dlogits[0] == 0).all() and (got.dlogits[2] == 0).all() and not torch.isnan(got.dlogits).any()
+        z[0], ids[0], z[2], ids[2] = z[2].clone(), ids[2].clone(), z[0].clone(), ids[0].clone()
+        got = lib.preference_loss_fwd_bwd(z, ids, lengths, None, lib.PREF_SIGMOID, 0.01, 0.0, 0.0, False, 1.0, ws)
+        assert got.loss.item() == float("inf") and got.rewards[0].item() == float("-inf")
+        assert not torch.isnan(got.dlogits).any() and (got.dlogits[0] != 0).any()
+        assert lib.poll_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype,base", [(HF, 20000.0), (HF, -20000.0), (BF, 2.0 ** 20)])
+@pytest.mark.parametrize("V", [1000, 1001, 8200, 20000, 20001, 50272, 128256])
+def test_distill_far_logits(V, dtype, base):
+    """Rows far from 0: differences to the row's maximum are what counts, and they are exact."""
+    gen = torch.Generator(device=DEV).manual_seed(52)
+    B, T, K = 2, 3, 20
+    step = 16.0 if dtype == HF else 2.0 ** 13            # spacing of the type there
+    z = torch.full((B, T, V), base, dtype=dtype, device=DEV)
+    z[:, 1] -= step * torch.randint(0, 2, (B, V), generator=gen, device=DEV).to(dtype)
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    ids, lt = teacher_entries(torch.zeros_like(z), K, 1.0, gen)
+    for mode in (0, 1, 2):
+        for temperature in (1.0, 0.5) if dtype == HF else (float(step), ):
+            check_distill(z, ids, lt, lengths, mode, temperature, 1000.0)
+
+
+@pytest.mark.parametrize("temperature", [0.05, 20.0, 1000.0])
+@pytest.mark.parametrize("V", [1000, 20000, 50257, 128256])
+def test_small_and_large_temperatures(V, temperature):
+    gen = torch.Generator(device=DEV).manual_seed(53)
+    B, T = 2, 4
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    lengths = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    assert z.float().abs().max().item() * 2 * 1.45 / 0.05 <= 1024
+    check_topk(z, lengths, 30, temperature)
+    ids, lt = teacher_entries(z, 30, temperature, gen)
+    for mode in (0, 1, 2):
+        check_distill(z, ids, lt, lengths, mode, temperature, 100.0, reach=1024 if temperature < 1 else 64)
+
+
+@pytest.mark.parametrize("K", [1, 64, 65, 256])
+@pytest.mark.parametrize("V", [8184, 8192, 8193, 32768, 52000, 53760, 57344, 57352, 61440, 65528, 65536, 65544, 106496, 114688,
+                               114696, 131072, 212992, 229376, 229384, 262144])
+def test_distill_at_the_borders_of_the_kernels(V, K):
+    gen = torch.Generator(device=DEV).manual_seed(V + K)
+    B, T = 2, 3
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    ids, lt = teacher_entries(z, K, 1.0, gen)
+    lengths = torch.tensor([T, 1], dtype=torch.int32, device=DEV)
+    _, ws = check_distill(z, ids, lt, lengths, 2, 1.0, 100.0)
+    assert lib.poll_status(ws) == 0
+
+
+def test_distill_strides_of_single_positions():
+    """The stride of an axis with one position says nothing."""
+    gen = torch.Generator(device=DEV).manual_seed(54)
+    z, _ = ref.row_logits(1, 1, 1000, BF, gen, DEV)
+    lengths = torch.ones(1, dtype=torch.int32, device=DEV)
+    for K in (1, 8):
+        ids, lt = teacher_entries(z, K, 1.0, gen)
+        got, _ = check_distill(z, ids.as_strided((1, 1, K), (40, 3, 1)), lt.as_strided((1, 1, K), (0, 77, 1)), lengths, 2, 1.0, 1.0)
+    one = lt[:, :, :1].as_strided((1, 1, 1), (5, 5, 9))
+    check_distill(z, ids[:, :, :1], one, lengths, 0, 1.0, 1.0)
+    z, _ = ref.row_logits(2, 3, 1000, BF, gen, DEV)
+    ids, lt = teacher_entries(z, 8, 1.0, gen)
+    with pytest.raises(ValueError, match="strides"):
+        lib.distill_loss_fwd_bwd(z, ids, lt.transpose(0, 1).contiguous().transpose(0, 1), torch.ones(2, dtype=torch.int32, device=DEV),
+                                 0, 1.0, 1.0, lib.workspace(2, 3, DEV))
+
+
+@pytest.mark.parametrize("dtype,base", [(HF, 20000.0), (HF, -20000.0), (BF, 2.0 ** 20)])
+@pytest.mark.parametrize("V", [1000, 1001, 8200, 20000, 20001, 50272, 128256, 300000])
+def test_policy_and_preference_far_logits(V, dtype, base):
+    """As above for the objectives of one token per row; a row's entries are one, two or more steps of their type apart."""
+    gen = torch.Generator(device=DEV).manual_seed(55)
+    B, T = 2, 3
+    step = 16.0 if dtype == HF else 2.0 ** 13
+    z = torch.full((B, T, V), base, dtype=dtype, device=DEV)
+    few = torch.randint(0, V, (B, 5), generator=gen, device=DEV)
+    z[:, 1].scatter_(1, few, base - step)
+    ids, lengths = labels(B, T, V, gen), torch.full((B,), T, dtype=torch.int32, device=DEV)
+    ids[:, 1] = torch.where((few == ids[:, 1:2]).any(dim=1), (few.max(dim=1).values + 1) % V, ids[:, 1])
+    lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
+    check_policy(z, ids, lengths, lp_old, lp_ref, adv, 0.1, 0, 1000.0)
+    check_preference(z, ids, lengths, lp_ref, 0, 0.3, 0.1, 0.0, False, 1000.0)
