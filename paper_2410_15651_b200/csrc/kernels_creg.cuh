@@ -642,6 +642,8 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     __shared__ __align__(16) float4 s_xchg[2][kCluster];     // per row parity: (M, s, ey, zy) of every block of the cluster
     __shared__ __align__(8) unsigned long long s_xbar[2];
     static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
+    // rows that may be announced and not yet read by their target warp: those in the buffers, the row being taken, two ahead
+    static_assert(kCregMaxBufs + 3 <= kDistillRows, "an announcement must not replace one that has not been read");
     static_assert(kCregMaxBufs * 16 <= 64, "the mbarriers of the buffers take the 64 bytes after the zero buffer");
     __shared__ uint32_t s_tmem_base;
     // kDistill: barriers ready / patched of every buffer, announced of every row that the target warps learn of, told / spare

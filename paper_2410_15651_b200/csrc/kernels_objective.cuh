@@ -83,8 +83,8 @@ __global__ void __launch_bounds__(kFinalThreads) row_sums_kernel(RowSumArgs p)
 }
 
 // ---------------------------------------------------------------- pairs of the preference loss
-// One block per pair (sequences i and i + B/2): the log ratio of each sequence is a sum over its tokens, added in double
-// precision in a fixed order; thread 0 forms the pair's loss and the factor that every token's gradient of the two
+// One block per pair (sequences i and i + B/2), half of its threads per sequence: the log ratio of each is a sum over its
+// tokens, added in double precision in a fixed order; thread 0 forms the pair's loss and the factor that every token's gradient of the two
 // sequences carries.  The block that finishes last adds the pairs' losses in a fixed order.
 struct PairArgs {
     const float* lp;            // [B,T] log-probs of the current logits (0 at padding and at ids out of range)
@@ -129,19 +129,6 @@ __device__ inline void pair_objective(int kind, double h, double beta, double e,
     }
 }
 
-// Sum over the valid tokens of sequence b of lp - lp_ref, by the whole block; thread 0 gets it.
-__device__ inline double sequence_log_ratio(const PairArgs& p, int b, int len, double* s_red)
-{
-    double s = 0.0;
-    const long long base = (long long)b * p.T;
-    for (int t = threadIdx.x; t < len; t += kPairThreads) {
-        const long long y = __ldg(p.ids + (long long)b * p.ids_stride_b + t);
-        if (y < 0 || y >= p.V) continue;
-        s += (double)p.lp[base + t] - (p.lp_ref ? (double)__ldg(p.lp_ref + base + t) : 0.0);
-    }
-    return block_sum_double<kPairThreads>(s, s_red);
-}
-
 __global__ void __launch_bounds__(kPairThreads) preference_pair_kernel(PairArgs p)
 {
     __shared__ double s_red[kPairThreads / 32];
@@ -152,9 +139,24 @@ __global__ void __launch_bounds__(kPairThreads) preference_pair_kernel(PairArgs 
     for (int i = blockIdx.x; i < half; i += gridDim.x) {
         const int bc = i, br = i + half;
         const int nc = clamp_len(__ldg(p.lengths + bc), p.T), nr = clamp_len(__ldg(p.lengths + br), p.T);
-        double sc = sequence_log_ratio(p, bc, nc, s_red);
-        double sr = sequence_log_ratio(p, br, nr, s_red);
+        // half the block per sequence: each warp leaves its sum, thread 0 adds them in warp order
+        const bool rejected = threadIdx.x >= kPairThreads / 2;
+        const int b = rejected ? br : bc, len = rejected ? nr : nc;
+        const long long base = (long long)b * p.T;
+        double s = 0.0;
+        for (int t = threadIdx.x & (kPairThreads / 2 - 1); t < len; t += kPairThreads / 2) {
+            const long long y = __ldg(p.ids + (long long)b * p.ids_stride_b + t);
+            const float lp = p.lp[base + t], lp_ref = p.lp_ref ? __ldg(p.lp_ref + base + t) : 0.f;
+            if (y >= 0 && y < p.V) s += (double)lp - (double)lp_ref;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        __syncthreads();                 // the sums of the block's previous pair have been read
+        if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = s;
+        __syncthreads();
         if (threadIdx.x == 0) {
+            double sc = 0.0, sr = 0.0;
+            for (int w = 0; w < kPairThreads / 64; ++w) { sc += s_red[w]; sr += s_red[kPairThreads / 64 + w]; }
             const double wc = p.length_mean && nc > 0 ? 1.0 / nc : 1.0, wr = p.length_mean && nr > 0 ? 1.0 / nr : 1.0;
             sc *= wc;
             sr *= wr;
@@ -167,8 +169,10 @@ __global__ void __launch_bounds__(kPairThreads) preference_pair_kernel(PairArgs 
             const double f = (double)p.grad_scale * beta * dh / (double)half;
             p.seq_factor[bc] = (float)(f * wc);
             p.seq_factor[br] = (float)(-f * wr);
+            if (half == 1) *p.out_loss = (float)loss;
         }
     }
+    if (half == 1) return;               // a single pair: nothing to add up
     if (threadIdx.x == 0) {
         __threadfence();
         s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
