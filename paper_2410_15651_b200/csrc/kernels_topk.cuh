@@ -12,9 +12,12 @@
 // whatever their size.
 //
 // Floor: one read of the row from DRAM (32 us for 2048 rows of 50272 in bf16 at 6.5 TB/s).  What bounds the kernel is
-// instruction issue: per row of 50272 and K = 64 14,600 warp instructions, some 9,000 of them for the stream (one ex2 and
-// half a packed maximum per logit), the others for the selection, which the warps of a block share.  Measured on such rows
-// and dropped, with their time over this kernel's: a row per warp (all rows of a batch are then in flight, L2 does not hold
+// the chain of dependent steps that selects a row, while its block loads nothing new: the same rows of 50272
+// take 1.9 times as long at K = 256 as at K = 64, and 0.8 times at K = 8.  Neither DRAM (45%) nor the issue slots (49%) are full,
+// and a warp waits 6.9 of 14.2 cycles per instruction for global loads.  Per row and K = 64 there are 14,600 warp
+// instructions, some 9,000 of them for the stream (one ex2 and half a packed maximum per logit).  Measured on such rows and
+// dropped, with their time over this kernel's: the first 8 to 32 KB of the next row brought to L2 before the selection (0.99
+// to 1.03, and 1.04 at V = 1000); a row per warp (all rows of a batch are then in flight, L2 does not hold
 // them, and what is read again comes from DRAM in sectors: 1.43; with groups of whole lines 0.93, but 1.13 at K = 256 and
 // 1.18 at V = 128256); separate streaming and selecting warps (1.25: one warp selects for 25 us); rows through a ring of
 // bulk copies (1.05).
@@ -543,7 +546,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_block_kernel(BlockLpArg
             float zt = kTopkFloor, st = 0.f;
             for (int w = 0; w < NT / 32; ++w) zt = fmaxf(zt, s_part[par][w].x);
             for (int w = 0; w < NT / 32; ++w) st += s_part[par][w].y * ex2((s_part[par][w].x - zt) * kLog2e);
-            p.out_lp[row] = bad_id ? 0.f : (float)(0.6931471805599453 * ((double)(zy - zt) * (double)kLog2e - log2_split(st)));
+            // (the difference of the logits is exact; through kLog2e, 1.3e-8 below log2(e), every log-prob of a sequence would
+            // be 7e-8 too large)
+            p.out_lp[row] = bad_id ? 0.f : (float)((double)zy - (double)zt - 0.6931471805599453 * log2_split(st));
         }
     }
     if (blockIdx.x == 0) block_count_valid(p.lengths, p.B, p.T, s_cnt, p.status);   // flags lengths out of range

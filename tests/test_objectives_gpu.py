@@ -588,3 +588,19 @@ def test_policy_and_preference_far_logits(V, dtype, base):
     lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
     check_policy(z, ids, lengths, lp_old, lp_ref, adv, 0.1, 0, 1000.0)
     check_preference(z, ids, lengths, lp_ref, 0, 0.3, 0.1, 0.0, False, 1000.0)
+
+
+def test_log_probs_of_few_rows_have_no_bias():
+    """A reward adds a sequence's log-probs, so that an error of the same sign in each counts.  Of 2048 log-probs near -10 (fp32
+    spacing 2^-20, rounded to the nearest: standard deviation 2^-20 / sqrt(12) = 2.8e-7, and 2e-7 for that of the sum behind it)
+    the mean is off by chance by 3.4e-7 / sqrt(2048) = 7.6e-9; five times that is allowed."""
+    gen = torch.Generator(device=DEV).manual_seed(56)
+    total, count = 0.0, 0
+    for _ in range(32):
+        z, _ = ref.row_logits(2, 32, 32000, BF, gen, DEV)
+        ids, lengths = labels(2, 32, 32000, gen), torch.full((2,), 32, dtype=torch.int32, device=DEV)
+        got = lib.preference_loss_fwd_bwd(z, ids, lengths, None, 0, 0.1, 0.0, 0.0, False, 1.0, lib.workspace(2, 32, DEV))
+        _, lp, _ = ref.label_logprobs(z.double(), ids, lengths)
+        total += (got.lp_new.double() - lp).sum().item()
+        count += lp.numel()
+    assert abs(total / count) <= 5 * 7.6e-9
