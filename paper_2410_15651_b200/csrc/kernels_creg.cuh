@@ -136,11 +136,18 @@ struct TargetInfo {
     float pr[4];             // sum p over the entries of each block's slice
 };
 
-// Factor of a row's entries that are not the teacher's: d loss / d z_v = factor * q_v / tau.  s: the student's mass on
-// them, relative; q0 = s / (s + ey).  No such entry, or a mass below the fp32 range: the tail term is left out.
+// Whether a row's loss has the tail term: the teacher has mass outside its entries, and so has the student (s: its mass there,
+// relative).  Loss, factor and the entries' gradients all ask here, so that the gradient is that of the loss.
+__device__ __forceinline__ bool distill_has_tail(const TargetInfo& ti, float s) { return ti.p0 > 0.f && s > 0.f; }
+
+// Weight of q_v in the gradient of a teacher's entry, d loss / d z_v = (weight * q_v - p_v) / tau: the weights of the terms that
+// the loss has.
+__device__ __forceinline__ float distill_weight(const TargetInfo& ti, float s) { return distill_has_tail(ti, s) ? ti.W : ti.P; }
+
+// Factor of a row's entries that are not the teacher's: d loss / d z_v = factor * q_v / tau.  q0 = s / (s + ey).
 __device__ __forceinline__ float distill_factor(const TargetInfo& ti, float s, float q0)
 {
-    return ti.p0 > 0.f && s > 0.f ? ti.W - ti.p0 / q0 : ti.P;
+    return distill_has_tail(ti, s) ? ti.W - ti.p0 / q0 : ti.P;
 }
 
 // Loss of a row.  With x the scaled logits and M a reference, zy = sum_k p_k (x_k - M); s and ey are the sums of 2^(x-M)
@@ -150,7 +157,7 @@ __device__ __forceinline__ double distill_loss(const TargetInfo& ti, float zy, f
     constexpr double ln2 = 0.6931471805599453;
     const double l2 = log2_split(s + ey);
     double L = ti.H - ln2 * ((double)zy - (double)ti.P * l2);
-    if (ti.p0 > 0.f && s > 0.f) L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (log2_split(s) - l2));
+    if (distill_has_tail(ti, s)) L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (log2_split(s) - l2));
     return L;
 }
 
@@ -604,12 +611,12 @@ template <bool kF16>
 __device__ __forceinline__ void distill_values_few(const EntrySet& es, const float4& tot, const TargetInfo& ti, float xscale,
                                                float row_scale, int lane)
 {
-    const float l2 = log2f(tot.y + tot.z);
+    const float l2 = log2f(tot.y + tot.z), weight = distill_weight(ti, tot.y);
 #pragma unroll 1
     for (int k = lane; k < es.K; k += 32)
         if (es.pos[k] >= 0) {
             const float q = ex2(fmaf(es.z[k], xscale, -tot.x) - l2);
-            es.p[k] = __uint_as_float(El<kF16>::pack2(row_scale * fmaf(ti.W, q, -es.p[k]), 0.f) & 0xffffu);
+            es.p[k] = __uint_as_float(El<kF16>::pack2(row_scale * fmaf(weight, q, -es.p[k]), 0.f) & 0xffffu);
         }
 }
 // ---------------------------------------------------------------- the kernel
@@ -981,7 +988,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(spare(i));                // the set has been read
             } else {
-                const float l2 = log2f(tot.y + tot.z);
+                const float l2 = log2f(tot.y + tot.z), weight = distill_weight(ti, tot.y);
                 int pos[kPer];
                 uint32_t value[kPer];
 #pragma unroll
@@ -992,7 +999,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                     if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(i)[k];
                     if (32 * j < dt.K && pos[j] >= 0) {
                         const float q = ex2(fmaf(t_z(i)[k], xscale, -tot.x) - l2);
-                        value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -t_p(i)[k]), 0.f) & 0xffffu;
+                        value[j] = El<kF16>::pack2(row_scale * fmaf(weight, q, -t_p(i)[k]), 0.f) & 0xffffu;
                     }
                 }
                 __syncwarp();

@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
             if (flat < 0) break;
             const float4 tot = s_total[i & (kCringTargets - 1)];     // M, mass outside, mass of the entries, sum p (x - M)
             const TargetInfo ti = s_target[i & (kCringTargets - 1)];
-            const float l2 = log2f(tot.y + tot.z);
+            const float l2 = log2f(tot.y + tot.z), weight = distill_weight(ti, tot.y);
             const int* tp = t_pos(i);
             int pos[kPer];
             uint32_t value[kPer];
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 if (32 * j < dt.K && k < dt.K) pos[j] = tp[k];
                 if (32 * j < dt.K && pos[j] >= 0) {
                     const float q = ex2(fmaf(((const float*)tp)[2 * Kpad + k], xscale, -tot.x) - l2);
-                    value[j] = El<kF16>::pack2(row_scale * fmaf(ti.W, q, -((const float*)tp)[Kpad + k]), 0.f) & 0xffffu;
+                    value[j] = El<kF16>::pack2(row_scale * fmaf(weight, q, -((const float*)tp)[Kpad + k]), 0.f) & 0xffffu;
                 }
             }
             __syncwarp();

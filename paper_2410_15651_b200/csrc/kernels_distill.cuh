@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRow
         const float4 tot = s_tot;
         const TargetInfo ti = s_ti;
         const float l2 = log2f(tot.y + tot.z);
-        if (first) s_grad[tid] = row_scale * fmaf(ti.W, ex2(fmaf(z, dt.scale, -tot.x) - l2), -pk);
+        if (first) s_grad[tid] = row_scale * fmaf(distill_weight(ti, tot.y), ex2(fmaf(z, dt.scale, -tot.x) - l2), -pk);
         __syncthreads();
 
         // ---- pass 2: the gradient

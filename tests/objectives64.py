@@ -124,7 +124,7 @@ def distill(z, topk_ids, topk_logprobs, lengths, mode, temperature, grad_scale):
         l0 = torch.logsumexp(lq.masked_fill(named, float("-inf")), dim=2, keepdim=True)
         there = (p0 > 0) & (l0 > float("-inf"))
         L = L + torch.where(there, p0 * (torch.log(p0) - l0), 0.0)[..., 0]
-        W = P + p0
+        W = torch.where(there, P + p0, P)
         out = torch.where(there, W - p0 * torch.exp(-l0), P)
         size = torch.where(there, W + p0 * torch.exp(-l0), P)
     else:
