@@ -330,8 +330,9 @@ typedef enum {
  *                        = grad_scale * temperature / N * (W - p_0 / q_0) q_v   otherwise
  * with W = p_0 + sum_k p_k (p_0 = 0 outside the tail mode, and where the tail term is left out); the gradient is that of
  * *out_loss, times grad_scale.  An entry named twice has the sum of its weights (log p_k stays that of each mention).  Entries -1 are unused; others outside
- * [0,V) set RLHF_ERR_ID_RANGE and count as unused.  A token without entries adds 0 to a plain or normalised loss.  Where no
- * vocabulary entry is left outside S, or their mass is below the range of fp32, the tail term is left out.  A deleted
+ * [0,V) set RLHF_ERR_ID_RANGE and count as unused.  A token without entries adds 0 to a plain or normalised loss.  Where the
+ * student has no mass outside S (it has deleted every other entry) the tail term is left out; a mass there of any size is not
+ * none.  A deleted
  * student entry (-inf) with p_k > 0 makes the loss infinite, as the definition has it.
  * Finite logits must satisfy |z| / temperature <= 1e9.  A gradient below 2^-62 may be written as 0, and so may that of an
  * entry with q_v < 2^-126.

@@ -66,9 +66,9 @@ struct RowInfo {
     unsigned pad;
 };
 
-// Block-wide total of the partial sums, as consumer_reduce but with log2(NW) cross-warp steps.
+// Block-wide total of the partial sums without the generated token's term, as consumer_reduce but with log2(NW) cross-warp steps.
 template <int NW>
-__device__ __forceinline__ Acc creg_reduce(const Acc& a, float2* s_part, const LabelInfo* s_lab, int warp, int lane)
+__device__ __forceinline__ Acc creg_reduce_rest(const Acc& a, float2* s_part, int warp, int lane)
 {
     float M = a.M;
 #pragma unroll
@@ -89,14 +89,25 @@ __device__ __forceinline__ Acc creg_reduce(const Acc& a, float2* s_part, const L
     // lanes >= 2*kTop did not take part; everyone takes lane 0's result
     Mt = __shfl_sync(0xffffffffu, Mt, 0);
     st = __shfl_sync(0xffffffffu, st, 0);
-    const LabelInfo li = *s_lab;
+    return Acc{Mt, st, 0.f};
+}
+
+// The same sum and another's term against the larger of the two references.
+__device__ __forceinline__ Acc creg_add_label(const Acc& rest, const LabelInfo& li)
+{
     Acc tot;
-    tot.M = fmaxf(Mt, li.M);
-    tot.s = st * ex2(Mt - tot.M);
+    tot.M = fmaxf(rest.M, li.M);
+    tot.s = rest.s * ex2(rest.M - tot.M);
     tot.ey = li.ey * ex2(li.M - tot.M);
     return tot;
 }
 
+template <int NW>
+__device__ __forceinline__ Acc creg_reduce(const Acc& a, float2* s_part, const LabelInfo* s_lab, int warp, int lane)
+{
+    const Acc rest = creg_reduce_rest<NW>(a, s_part, warp, lane);
+    return creg_add_label(rest, *s_lab);
+}
 
 #ifndef RLHF_CREG_REGVECS_ONLY
 #define RLHF_CREG_REGVECS_ONLY 8
@@ -136,28 +147,42 @@ struct TargetInfo {
     float pr[4];             // sum p over the entries of each block's slice
 };
 
-// Whether a row's loss has the tail term: the teacher has mass outside its entries, and so has the student (s: its mass there,
-// relative).  Loss, factor and the entries' gradients all ask here, so that the gradient is that of the loss.
-__device__ __forceinline__ bool distill_has_tail(const TargetInfo& ti, float s) { return ti.p0 > 0.f && s > 0.f; }
+// A row's sums.  x are the scaled logits, M the row's reference.  The mass outside the teacher's entries is kept against a
+// reference of its own too: against M it may be far below the range of fp32, and the tail term takes its logarithm and its inverse.
+struct DistillTotals {
+    float M, s, ey;          // sums of 2^(x - M) over the entries that are not the teacher's and over those that are
+    float zy;                // sum_k p_k (x_k - M)
+    float Mo, so;            // sum of 2^(x - Mo) over the entries that are not the teacher's: at least 1/2, or 0 if there is none
+};
+
+// Whether a row's loss has the tail term: the teacher has mass outside its entries, and so has the student.  Loss, factor and the
+// entries' gradients all ask here, so that the gradient is that of the loss.
+__device__ __forceinline__ bool distill_has_tail(const TargetInfo& ti, float so) { return ti.p0 > 0.f && so > 0.f; }
 
 // Weight of q_v in the gradient of a teacher's entry, d loss / d z_v = (weight * q_v - p_v) / tau: the weights of the terms that
 // the loss has.
-__device__ __forceinline__ float distill_weight(const TargetInfo& ti, float s) { return distill_has_tail(ti, s) ? ti.W : ti.P; }
+__device__ __forceinline__ float distill_weight(const TargetInfo& ti, float so) { return distill_has_tail(ti, so) ? ti.W : ti.P; }
 
-// Factor of a row's entries that are not the teacher's: d loss / d z_v = factor * q_v / tau.  q0 = s / (s + ey).
-__device__ __forceinline__ float distill_factor(const TargetInfo& ti, float s, float q0)
+// The gradient of a row's entries that are not the teacher's, d loss / d z_v = factor * 2^(x_v - M) / sum / tau: P q_v, and
+// (W - p0 / q0) q_v = (W q0 - p0) q_v / q0 where there is a tail term, q0 the student's mass outside.  There M and sum are those
+// of the mass outside alone, so that neither 1 / q0 nor q_v leaves the range of fp32.
+struct DistillOutside {
+    float factor, M, sum;
+};
+__device__ __forceinline__ DistillOutside distill_outside(const TargetInfo& ti, const DistillTotals& t, float q0)
 {
-    return distill_has_tail(ti, s) ? ti.W - ti.p0 / q0 : ti.P;
+    if (distill_has_tail(ti, t.so)) return DistillOutside{fmaf(ti.W, q0, -ti.p0), t.Mo, t.so};
+    return DistillOutside{ti.P, t.M, t.s + t.ey};
 }
 
-// Loss of a row.  With x the scaled logits and M a reference, zy = sum_k p_k (x_k - M); s and ey are the sums of 2^(x-M)
-// over the other and over the teacher's entries.
-__device__ __forceinline__ double distill_loss(const TargetInfo& ti, float zy, float s, float ey)
+// Loss of a row.
+__device__ __forceinline__ double distill_loss(const TargetInfo& ti, const DistillTotals& t)
 {
     constexpr double ln2 = 0.6931471805599453;
-    const double l2 = log2_split(s + ey);
-    double L = ti.H - ln2 * ((double)zy - (double)ti.P * l2);
-    if (distill_has_tail(ti, s)) L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (log2_split(s) - l2));
+    const double l2 = log2_split(t.s + t.ey);
+    double L = ti.H - ln2 * ((double)t.zy - (double)ti.P * l2);
+    if (distill_has_tail(ti, t.so))
+        L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (log2_split(t.so) + ((double)t.Mo - (double)t.M) - l2));
     return L;
 }
 
@@ -608,17 +633,43 @@ __device__ __forceinline__ void distill_publish_few(const DistillArgs& dt, float
 
 // The gradients of the entries, as 16-bit patterns in the place of the weights.
 template <bool kF16>
-__device__ __forceinline__ void distill_values_few(const EntrySet& es, const float4& tot, const TargetInfo& ti, float xscale,
+__device__ __forceinline__ void distill_values_few(const EntrySet& es, const DistillTotals& tot, const TargetInfo& ti, float xscale,
                                                float row_scale, int lane)
 {
-    const float l2 = log2f(tot.y + tot.z), weight = distill_weight(ti, tot.y);
+    const float l2 = log2f(tot.s + tot.ey), weight = distill_weight(ti, tot.so);
 #pragma unroll 1
     for (int k = lane; k < es.K; k += 32)
         if (es.pos[k] >= 0) {
-            const float q = ex2(fmaf(es.z[k], xscale, -tot.x) - l2);
+            const float q = ex2(fmaf(es.z[k], xscale, -tot.M) - l2);
             es.p[k] = __uint_as_float(El<kF16>::pack2(row_scale * fmaf(weight, q, -es.p[k]), 0.f) & 0xffffu);
         }
 }
+
+// The row's sums from those of the cluster's blocks, added in rank order: the same in every block.  xchg: (Mo, so, M, ey) of every
+// block, M the reference of its entries, then their zy against that M.
+template <int kCluster>
+__device__ __forceinline__ void distill_cluster_totals(const float4* xchg, const TargetInfo& ti, Acc& rest, Acc& tot, float& zy)
+{
+    float Mo = kFloorM;
+#pragma unroll
+    for (int r = 0; r < kCluster; ++r) Mo = fmaxf(Mo, xchg[r].x);
+    float so = 0.f, M = Mo;
+#pragma unroll
+    for (int r = 0; r < kCluster; ++r) {
+        so = fmaf(xchg[r].y, ex2(xchg[r].x - Mo), so);
+        M = fmaxf(M, xchg[r].z);
+    }
+    float ey = 0.f;
+    zy = 0.f;
+#pragma unroll
+    for (int r = 0; r < kCluster; ++r) {
+        ey = fmaf(xchg[r].w, ex2(xchg[r].z - M), ey);
+        zy += fmaf(ti.pr[r], xchg[r].z - M, xchg[kCluster + r].x);
+    }
+    rest = Acc{Mo, so, 0.f};
+    tot = Acc{M, so * ex2(Mo - M), ey};
+}
+
 // ---------------------------------------------------------------- the kernel
 // kTmem: a thread's vectors beyond the first kRegVecsTmem keep their exponentials in tensor memory; otherwise a
 // thread has at most kRegVecsOnly vectors and registers hold all of them.  kF16: logits and gradient are IEEE
@@ -646,7 +697,8 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     __shared__ double s_dbl[32];
     __shared__ double s_loss[2];
     __shared__ int s_last;
-    __shared__ __align__(16) float4 s_xchg[2][kCluster];     // per row parity: (M, s, ey, zy) of every block of the cluster
+    // per row parity: (M, s, ey, zy) of every block of the cluster; kDistill: (Mo, so, M, ey) and zy, M the entries' reference
+    __shared__ __align__(16) float4 s_xchg[2][kDistill ? 2 * kCluster : kCluster];
     __shared__ __align__(8) unsigned long long s_xbar[2];
     static_assert(NW <= 16, "the final sums take 16 doubles of scratch each");
     // rows that may be announced and not yet read by their target warp: those in the buffers, the row being taken, two ahead
@@ -660,7 +712,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
     __shared__ TargetRow s_trow[kDistill ? kDistillRows : 1];
     __shared__ TargetInfo s_target[kSetsHere];
     __shared__ LabelInfo s_tlab[kSetsHere];
-    __shared__ float4 s_total[kSetsHere];
+    __shared__ DistillTotals s_total[kSetsHere];
 
     const RowArgs& p = ca.row;
     const DistillArgs& dt = ca.distill;
@@ -973,7 +1025,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
             const long long flat = s_row[buf].flat;
             if (flat < 0) break;
             // the gradients of the entries, while the consumers write the others
-            const float4 tot = s_total[i & (kDistillSets - 1)];      // M, mass outside, mass of the entries, sum p (x - M)
+            const DistillTotals tot = s_total[i & (kDistillSets - 1)];
             const TargetInfo ti = s_target[i & (kDistillSets - 1)];
             if (few) {
                 const EntrySet es{t_pos(i), t_p(i), t_z(i), dt.K};
@@ -988,7 +1040,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(spare(i));                // the set has been read
             } else {
-                const float l2 = log2f(tot.y + tot.z), weight = distill_weight(ti, tot.y);
+                const float l2 = log2f(tot.s + tot.ey), weight = distill_weight(ti, tot.so);
                 int pos[kPer];
                 uint32_t value[kPer];
 #pragma unroll
@@ -998,7 +1050,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
                     value[j] = 0;
                     if (32 * j < dt.K && k < dt.K) pos[j] = t_pos(i)[k];
                     if (32 * j < dt.K && pos[j] >= 0) {
-                        const float q = ex2(fmaf(t_z(i)[k], xscale, -tot.x) - l2);
+                        const float q = ex2(fmaf(t_z(i)[k], xscale, -tot.M) - l2);
                         value[j] = El<kF16>::pack2(row_scale * fmaf(weight, q, -t_p(i)[k]), 0.f) & 0xffffu;
                     }
                 }
@@ -1017,7 +1069,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
             if (lane == 0) {
                 mbar_arrive(patched(buf));
                 if (crank == 0) {
-                    const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot.w, tot.y, tot.z));
+                    const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot));
                     p.row_loss[flat] = L;
                     if (p.out_lp_new) p.out_lp_new[flat] = L;
                 }
@@ -1170,61 +1222,74 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
         if (lane == 0) s_sum[par][warp] = ws;
-        Acc tot;
+        Acc tot, rest;                                               // kDistill: rest is the sum outside, against its own reference
         if (!consumer_barrier_or<NW>(diverged || aborted)) {
             tot.M = Mref;
             tot.s = sum_warp_sums<NW>(s_sum[par]);
-            if (kDistill) {
-                const LabelInfo li = s_tlab[ts];
-                tot.M = fmaxf(Mref, li.M);
-                tot.s *= ex2(Mref - tot.M);
-                tot.ey = li.ey * ex2(li.M - tot.M);
-            } else {
-                tot.ey = s_lab[par].ey;
-            }
+            if (kDistill) rest = Acc{Mref, tot.s, 0.f};
+            else tot.ey = s_lab[par].ey;
         } else {
             // a wait that ran out somewhere in the block ends the block's work here, for all its threads alike
             if (consumer_barrier_or<NW>(aborted)) { aborted = true; break; }
-            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], kDistill ? &s_tlab[ts] : &s_lab[par], warp, lane);
+            if (kDistill) rest = creg_reduce_rest<NW>(Acc{M, vs, 0.f}, s_part[par], warp, lane);
+            else tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], &s_lab[par], warp, lane);
         }
-        // the generated token's logit; kDistill: sum over the slice's teacher entries of p (x - M), M the total's reference
-        float zy_row = kDistill ? fmaf(s_tlab[ts].pad, s_tlab[ts].M - tot.M, s_tlab[ts].zy) : s_lab[par].zy;
+        float zy_row = kDistill ? 0.f : s_lab[par].zy;               // the generated token's logit; kDistill: DistillTotals::zy
+        if (kDistill && kCluster == 1) {
+            const LabelInfo li = s_tlab[ts];
+            tot = creg_add_label(rest, li);
+            zy_row = fmaf(li.pad, li.M - tot.M, li.zy);
+        }
 
         if (kCluster > 1) {
-            // every block of the cluster sends its slice's (M, s, ey, zy) to every block, itself included
+            // every block of the cluster sends its slice's sums to every block, itself included
             if (tid == 0) {
-                mbar_arrive_expect_tx(xbar_addr + 8u * par, 16u * kCluster);
-                const float4 mine = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                mbar_arrive_expect_tx(xbar_addr + 8u * par, (kDistill ? 32u : 16u) * kCluster);
+                const LabelInfo li = kDistill ? s_tlab[ts] : LabelInfo{};
+                const float4 mine = kDistill ? make_float4(rest.M, rest.s, li.M, li.ey) : make_float4(tot.M, tot.s, tot.ey, zy_row);
                 const uint32_t slot = smem_u32(&s_xchg[par][crank]);
 #pragma unroll
-                for (int r = 0; r < kCluster; ++r)
+                for (int r = 0; r < kCluster; ++r) {
                     remote_store_v4(map_to_rank(slot, (uint32_t)r), mine, map_to_rank(xbar_addr + 8u * par, (uint32_t)r));
+                    if (kDistill)
+                        remote_store_v4(map_to_rank(slot + 16u * kCluster, (uint32_t)r), make_float4(li.zy, 0.f, 0.f, 0.f),
+                                        map_to_rank(xbar_addr + 8u * par, (uint32_t)r));
+                }
             }
             if (!aborted && !mbar_try_wait_cluster(xbar_addr + 8u * par, use))
                 if (!mbar_wait_cluster_slow(xbar_addr + 8u * par, use, p.status, p.wait_limit_ns)) aborted = true;
             aborted = __any_sync(0xffffffffu, aborted);
-            float Mx = kFloorM;
+            if (kDistill) {
+                distill_cluster_totals<kCluster>(s_xchg[par], s_target[ts], rest, tot, zy_row);
+            } else {
+                float Mx = kFloorM;
 #pragma unroll
-            for (int r = 0; r < kCluster; ++r) Mx = fmaxf(Mx, s_xchg[par][r].x);
-            float sx = 0.f, eyx = 0.f, zx = 0.f;
+                for (int r = 0; r < kCluster; ++r) Mx = fmaxf(Mx, s_xchg[par][r].x);
+                float sx = 0.f, eyx = 0.f, zx = 0.f;
 #pragma unroll
-            for (int r = 0; r < kCluster; ++r) {                   // in rank order: the same total in every block
-                const float4 part = s_xchg[par][r];
-                const float sc = ex2(part.x - Mx);
-                sx = fmaf(part.y, sc, sx);
-                eyx = fmaf(part.z, sc, eyx);
-                zx += kDistill ? fmaf(s_target[ts].pr[r], part.x - Mx, part.w) : part.w;
+                for (int r = 0; r < kCluster; ++r) {               // in rank order: the same total in every block
+                    const float4 part = s_xchg[par][r];
+                    const float sc = ex2(part.x - Mx);
+                    sx = fmaf(part.y, sc, sx);
+                    eyx = fmaf(part.z, sc, eyx);
+                    zx += part.w;
+                }
+                tot = Acc{Mx, sx, eyx};
+                zy_row = zx;
             }
-            tot = Acc{Mx, sx, eyx};
-            zy_row = zx;
         }
         RowResult r = row_finish_fast(tot, zy_row);
 
         float loss = 0.f, kl = 0.f, g = 0.f;
+        float den_M = tot.M, den = tot.s + tot.ey;                   // what the exponentials are relative to in the gradient
         if (kDistill) {
-            g = -(scale_over_N * dt.tau) * distill_factor(s_target[ts], tot.s, r.one_m_py);
+            const DistillTotals totals_row{tot.M, tot.s, tot.ey, zy_row, rest.M, rest.s};
+            const DistillOutside outside = distill_outside(s_target[ts], totals_row, r.one_m_py);
+            g = -(scale_over_N * dt.tau) * outside.factor;
+            den_M = outside.M;
+            den = outside.sum;
             if (tid == 0) {
-                s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                s_total[ts] = totals_row;
                 mbar_arrive(totals(i));
             }
         } else if (!ri.bad_id) {
@@ -1254,10 +1319,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_creg_
         if (g == 0.f) {
             for (int j = 0; j < cnt; ++j) dst[(size_t)j * kCons] = make_uint4(0, 0, 0, 0);
         } else {
-            // |g| 2^(M - tot.M) / sum, M this thread's reference.  (Step 4 through lse, whose last place is that of the largest
+            // |g| 2^(M - den_M) / den, M this thread's reference.  (Step 4 through lse, whose last place is that of the largest
             // exponent; the others without it, for rows far from 0 and small temperatures.)
             const float mag = kDistill || p.objective != kObjPpo
-                                  ? ex2((M - tot.M) + (lg2(fabsf(g)) - lg2(tot.s + tot.ey)))
+                                  ? ex2((M - den_M) + (lg2(fabsf(g)) - lg2(den)))
                                   : ex2(M + (lg2(fabsf(g)) - r.lse2));
             const float2 sc2 = splat2(g > 0.f ? -mag : mag);
             const float dy = g * r.one_m_py;

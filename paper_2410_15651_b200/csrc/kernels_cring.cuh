@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
     __shared__ double s_dbl[32];
     __shared__ double s_loss[2];
     __shared__ int s_last;
-    __shared__ __align__(16) float4 s_xchg[2][kCluster];     // per row parity: (M, s, ey, zy) of every block of the cluster
+    // per row parity: (M, s, ey, zy) of every block of the cluster; kDistill: as distill_cluster_totals takes them
+    __shared__ __align__(16) float4 s_xchg[2][kDistill ? 2 * kCluster : kCluster];
     __shared__ __align__(8) unsigned long long s_xbar[2];
     __shared__ uint32_t s_tmem_base;
     // kDistill: barriers ready / patched of every slot, announced of every row info, told / spare / totals of every set of
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
     __shared__ TargetRow s_trow[kDistill ? kCringRows : 1];
     __shared__ TargetInfo s_target[kDistill ? kCringTargets : 1];
     __shared__ LabelInfo s_tlab[kDistill ? kCringTargets : 1];
-    __shared__ float4 s_total[kDistill ? kCringTargets : 1];
+    __shared__ DistillTotals s_total[kDistill ? kCringTargets : 1];
 
     const RowArgs& p = ca.row;
     const DistillArgs& dt = ca.distill;
@@ -404,9 +405,9 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
             if (aborted) break;
             const long long flat = s_row[i & (kCringRows - 1)].flat;
             if (flat < 0) break;
-            const float4 tot = s_total[i & (kCringTargets - 1)];     // M, mass outside, mass of the entries, sum p (x - M)
+            const DistillTotals tot = s_total[i & (kCringTargets - 1)];
             const TargetInfo ti = s_target[i & (kCringTargets - 1)];
-            const float l2 = log2f(tot.y + tot.z), weight = distill_weight(ti, tot.y);
+            const float l2 = log2f(tot.s + tot.ey), weight = distill_weight(ti, tot.so);
             const int* tp = t_pos(i);
             int pos[kPer];
             uint32_t value[kPer];
@@ -417,7 +418,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 value[j] = 0;
                 if (32 * j < dt.K && k < dt.K) pos[j] = tp[k];
                 if (32 * j < dt.K && pos[j] >= 0) {
-                    const float q = ex2(fmaf(((const float*)tp)[2 * Kpad + k], xscale, -tot.x) - l2);
+                    const float q = ex2(fmaf(((const float*)tp)[2 * Kpad + k], xscale, -tot.M) - l2);
                     value[j] = El<kF16>::pack2(row_scale * fmaf(weight, q, -((const float*)tp)[Kpad + k]), 0.f) & 0xffffu;
                 }
             }
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
             }
             if (aborted) break;
             if (lane == 0 && crank == 0) {
-                const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot.w, tot.y, tot.z));
+                const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot));
                 p.row_loss[flat] = L;
                 if (p.out_lp_new) p.out_lp_new[flat] = L;
             }
@@ -590,61 +591,74 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
         if (lane == 0) s_sum[par][warp] = ws;
-        Acc tot;
+        Acc tot, rest;                                               // kDistill: rest is the sum outside, against its own reference
         if (!consumer_barrier_or<NW>(diverged || aborted)) {
             tot.M = Mref;
             tot.s = sum_warp_sums<NW>(s_sum[par]);
-            if (kDistill) {
-                const LabelInfo li = s_tlab[ts];
-                tot.M = fmaxf(Mref, li.M);
-                tot.s *= ex2(Mref - tot.M);
-                tot.ey = li.ey * ex2(li.M - tot.M);
-            } else {
-                tot.ey = s_lab[par].ey;
-            }
+            if (kDistill) rest = Acc{Mref, tot.s, 0.f};
+            else tot.ey = s_lab[par].ey;
         } else {
             // a wait that ran out somewhere in the block ends the block's work here, for all its threads alike
             if (consumer_barrier_or<NW>(aborted)) { aborted = true; break; }
-            tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], kDistill ? &s_tlab[ts] : &s_lab[par], warp, lane);
+            if (kDistill) rest = creg_reduce_rest<NW>(Acc{M, vs, 0.f}, s_part[par], warp, lane);
+            else tot = creg_reduce<NW>(Acc{M, vs, 0.f}, s_part[par], &s_lab[par], warp, lane);
         }
-        // the generated token's logit; kDistill: sum over the slice's teacher entries of p (x - M), M the total's reference
-        float zy_row = kDistill ? fmaf(s_tlab[ts].pad, s_tlab[ts].M - tot.M, s_tlab[ts].zy) : s_lab[par].zy;
+        float zy_row = kDistill ? 0.f : s_lab[par].zy;               // the generated token's logit; kDistill: DistillTotals::zy
+        if (kDistill && kCluster == 1) {
+            const LabelInfo li = s_tlab[ts];
+            tot = creg_add_label(rest, li);
+            zy_row = fmaf(li.pad, li.M - tot.M, li.zy);
+        }
 
         if (kCluster > 1) {
-            // every block of the cluster sends its slice's (M, s, ey, zy) to every block, itself included
+            // every block of the cluster sends its slice's sums to every block, itself included
             if (tid == 0) {
-                mbar_arrive_expect_tx(xbar_addr + 8u * par, 16u * kCluster);
-                const float4 mine = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                mbar_arrive_expect_tx(xbar_addr + 8u * par, (kDistill ? 32u : 16u) * kCluster);
+                const LabelInfo li = kDistill ? s_tlab[ts] : LabelInfo{};
+                const float4 mine = kDistill ? make_float4(rest.M, rest.s, li.M, li.ey) : make_float4(tot.M, tot.s, tot.ey, zy_row);
                 const uint32_t slot = smem_u32(&s_xchg[par][crank]);
 #pragma unroll
-                for (int r = 0; r < kCluster; ++r)
+                for (int r = 0; r < kCluster; ++r) {
                     remote_store_v4(map_to_rank(slot, (uint32_t)r), mine, map_to_rank(xbar_addr + 8u * par, (uint32_t)r));
+                    if (kDistill)
+                        remote_store_v4(map_to_rank(slot + 16u * kCluster, (uint32_t)r), make_float4(li.zy, 0.f, 0.f, 0.f),
+                                        map_to_rank(xbar_addr + 8u * par, (uint32_t)r));
+                }
             }
             if (!mbar_try_wait_cluster(xbar_addr + 8u * par, use))
                 if (!mbar_wait_cluster_slow(xbar_addr + 8u * par, use, p.status, p.wait_limit_ns)) aborted = true;
             aborted = __any_sync(0xffffffffu, aborted);
-            float Mx = kFloorM;
+            if (kDistill) {
+                distill_cluster_totals<kCluster>(s_xchg[par], s_target[ts], rest, tot, zy_row);
+            } else {
+                float Mx = kFloorM;
 #pragma unroll
-            for (int r = 0; r < kCluster; ++r) Mx = fmaxf(Mx, s_xchg[par][r].x);
-            float sx = 0.f, eyx = 0.f, zx = 0.f;
+                for (int r = 0; r < kCluster; ++r) Mx = fmaxf(Mx, s_xchg[par][r].x);
+                float sx = 0.f, eyx = 0.f, zx = 0.f;
 #pragma unroll
-            for (int r = 0; r < kCluster; ++r) {                   // in rank order: the same total in every block
-                const float4 part = s_xchg[par][r];
-                const float sc = ex2(part.x - Mx);
-                sx = fmaf(part.y, sc, sx);
-                eyx = fmaf(part.z, sc, eyx);
-                zx += kDistill ? fmaf(s_target[ts].pr[r], part.x - Mx, part.w) : part.w;
+                for (int r = 0; r < kCluster; ++r) {               // in rank order: the same total in every block
+                    const float4 part = s_xchg[par][r];
+                    const float sc = ex2(part.x - Mx);
+                    sx = fmaf(part.y, sc, sx);
+                    eyx = fmaf(part.z, sc, eyx);
+                    zx += part.w;
+                }
+                tot = Acc{Mx, sx, eyx};
+                zy_row = zx;
             }
-            tot = Acc{Mx, sx, eyx};
-            zy_row = zx;
         }
         RowResult r = row_finish_fast(tot, zy_row);
 
         float loss = 0.f, kl = 0.f, g = 0.f;
+        float den_M = tot.M, den = tot.s + tot.ey;                   // what the exponentials are relative to in the gradient
         if (kDistill) {
-            g = -(scale_over_N * dt.tau) * distill_factor(s_target[ts], tot.s, r.one_m_py);
+            const DistillTotals totals_row{tot.M, tot.s, tot.ey, zy_row, rest.M, rest.s};
+            const DistillOutside outside = distill_outside(s_target[ts], totals_row, r.one_m_py);
+            g = -(scale_over_N * dt.tau) * outside.factor;
+            den_M = outside.M;
+            den = outside.sum;
             if (tid == 0) {
-                s_total[ts] = make_float4(tot.M, tot.s, tot.ey, zy_row);
+                s_total[ts] = totals_row;
                 mbar_arrive(totals(i));
             }
         } else if (!ri.bad_id) {
@@ -685,10 +699,10 @@ __global__ void __launch_bounds__(NW * 32 + (kDistill ? 128 : 32), 1) loss_cring
                 release(c);
             }
         } else {
-            // |g| 2^(M - tot.M) / sum, M this thread's reference.  (Step 4 through lse, whose last place is that of the largest
+            // |g| 2^(M - den_M) / den, M this thread's reference.  (Step 4 through lse, whose last place is that of the largest
             // exponent; the others without it, for rows far from 0 and small temperatures.)
             const float mag = kDistill || p.objective != kObjPpo
-                                  ? ex2((M - tot.M) + (lg2(fabsf(g)) - lg2(tot.s + tot.ey)))
+                                  ? ex2((M - den_M) + (lg2(fabsf(g)) - lg2(den)))
                                   : ex2(M + (lg2(fabsf(g)) - r.lse2));
             const float2 sc2 = splat2(g > 0.f ? -mag : mag);
             const float dy = g * r.one_m_py;

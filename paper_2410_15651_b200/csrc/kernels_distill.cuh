@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRow
     __shared__ long long s_cnt[33];
     __shared__ TargetInfo s_ti;
     __shared__ int s_twice;
-    __shared__ float4 s_tot;
+    __shared__ DistillTotals s_tot;
     const RowArgs& p = da.row;
     const DistillArgs& dt = da.distill;
     const int tid = threadIdx.x;
@@ -181,23 +181,23 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRow
             ti.W = dt.mode == kDistillTail ? (float)(P > 1.0 ? P : 1.0) : (float)P;
             if (!(P == P)) ti.W = ti.P;
             const float Mx = fmaxf(a.M, Mt);
-            const float out = a.s * ex2(a.M - Mx), in = (float)ey * ex2(Mt - Mx);
+            const DistillTotals tot{Mx, a.s * ex2(a.M - Mx), (float)ey * ex2(Mt - Mx), fmaf((float)P, Mt - Mx, (float)zy), a.M, a.s};
             s_ti = ti;
-            s_tot = make_float4(Mx, out, in, 0.f);
-            const float L = (float)((double)dt.tau * (double)dt.tau *
-                                    distill_loss(ti, fmaf((float)P, Mt - Mx, (float)zy), out, in));
+            s_tot = tot;
+            const float L = (float)((double)dt.tau * (double)dt.tau * distill_loss(ti, tot));
             p.row_loss[flat] = L;
             if (p.out_lp_new) p.out_lp_new[flat] = L;
         }
         __syncthreads();
-        const float4 tot = s_tot;
+        const DistillTotals tot = s_tot;
         const TargetInfo ti = s_ti;
-        const float l2 = log2f(tot.y + tot.z);
-        if (first) s_grad[tid] = row_scale * fmaf(distill_weight(ti, tot.y), ex2(fmaf(z, dt.scale, -tot.x) - l2), -pk);
+        if (first)
+            s_grad[tid] = row_scale * fmaf(distill_weight(ti, tot.so), ex2(fmaf(z, dt.scale, -tot.M) - log2f(tot.s + tot.ey)), -pk);
         __syncthreads();
 
         // ---- pass 2: the gradient
-        const float f = row_scale * distill_factor(ti, tot.y, tot.y / (tot.y + tot.z));
+        const DistillOutside outside = distill_outside(ti, tot, tot.s / (tot.s + tot.ey));
+        const float f = row_scale * outside.factor, l2 = log2f(outside.sum);
         for (uint32_t v = tid; v < r.nvec; v += kDistillThreads) {
             const uint4 q = *(r.vecs + v);
             float zz[8];
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_row_kernel(DistillRow
             const bool named = may_hold(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                zz[i] = f == 0.f ? 0.f : f * ex2(fmaf(zz[i], dt.scale, -tot.x) - l2);
+                zz[i] = f == 0.f ? 0.f : f * ex2(fmaf(zz[i], dt.scale, -outside.M) - l2);
                 const int e = (int)(v * 8u + (uint32_t)i) - (int)r.eoff;
                 if (named && e >= 0 && e < p.V) {
                     const int k = distill_find(s_tab, e);
