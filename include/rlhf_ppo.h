@@ -329,11 +329,11 @@ typedef enum {
  *     out_dlogits[b,t,v] = grad_scale * temperature / N * (W q_v - p_v)        v in S
  *                        = grad_scale * temperature / N * (W - p_0 / q_0) q_v   otherwise
  * with W = p_0 + sum_k p_k (p_0 = 0 outside the tail mode, and where the tail term is left out); the gradient is that of
- * *out_loss, times grad_scale.  An entry named twice has the sum of its weights (log p_k stays that of each mention).  Entries -1 are unused; others outside
- * [0,V) set RLHF_ERR_ID_RANGE and count as unused.  A token without entries adds 0 to a plain or normalised loss.  Where the
- * student has no mass outside S (it has deleted every other entry) the tail term is left out; a mass there of any size is not
- * none.  A deleted
- * student entry (-inf) with p_k > 0 makes the loss infinite, as the definition has it.
+ * *out_loss, times grad_scale.  An entry named twice has the sum of its weights (log p_k stays that of each mention).
+ * Entries -1 are unused; others outside [0,V) set RLHF_ERR_ID_RANGE and count as unused.  A token without entries adds 0 to a
+ * plain or normalised loss.  Where the student has no mass outside S (every other entry is deleted) the tail term is left out;
+ * a mass there, however small, is not none.  A deleted student entry (-inf) with p_k > 0 makes the loss infinite, as the
+ * definition has it.
  * Finite logits must satisfy |z| / temperature <= 1e9.  A gradient below 2^-62 may be written as 0, and so may that of an
  * entry with q_v < 2^-126.
  *   logits, lengths, out_dlogits   as step 4 (logits_dtype: rlhf_dtype_t of both tensors; in place allowed)
@@ -366,6 +366,7 @@ typedef enum {
  *     out_dlogits[b,t,v] = g * ([v == y] - exp(z_v - lse))           rounded to the logits' type
  *     *out_loss_pg = sum w l_pg      *out_loss_kl = sum w l_kl       (kl_coef is not applied to the latter)
  * A token whose id is out of range gives 0 to both sums and a zero row; it keeps its weight.  No valid token: all 0.
+ * kl_coef = 0 leaves the KL out of the gradient, whatever its value; *out_loss_kl is still formed.
  *   logits, ids, lengths, out_dlogits, out_lp_new   as step 4 (logits_dtype: rlhf_dtype_t of both tensors; in place allowed)
  *   lp_old, lp_ref   fp32 [B,T]; lp_ref may be NULL (no KL term: l_kl = 0)   read
  *   adv              fp32, adv[b*adv_stride_b + t*adv_stride_t] (strides in elements, >= 0; adv_stride_t = 0 for one

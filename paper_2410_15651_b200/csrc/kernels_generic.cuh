@@ -76,9 +76,10 @@ __device__ __forceinline__ RowScalars load_row_scalars(const RowArgs& p, int b, 
 }
 
 // exp(d) - 1 - d without cancellation: the Taylor series where it is short (|d| <= 1/2: the first term left out is
-// below 2^-25 of the sum), else the difference.
+// below 2^-25 of the sum), else the difference (inf at d = inf, a token that the row deletes).
 __device__ __forceinline__ float exp_excess(float d)
 {
+    if (d > 100.f) return expm1f(d);                  // inf
     if (fabsf(d) > 0.5f) return expm1f(d) - d;
     float s = 1.f / 3628800.f;
     s = fmaf(s, d, 1.f / 362880.f);
@@ -122,7 +123,8 @@ __device__ __forceinline__ PolicyTerm policy_term(const RowArgs& p, const RowSca
 __device__ __forceinline__ float policy_gradient(const RowArgs& p, const RowScalars& s, const PolicyTerm& q, float scale)
 {
     const float d_pg = q.free ? q.unclipped : 0.f;
-    const float d_kl = p.lp_ref ? p.kl_coef * (1.f - ex2((s.lp_ref - q.lp) * kLog2e)) : 0.f;
+    // (kl_coef = 0 reports the KL without training on it: 0 * inf, where the reference is 89 nats above or more, is not formed)
+    const float d_kl = p.lp_ref && p.kl_coef != 0.f ? p.kl_coef * (1.f - ex2((s.lp_ref - q.lp) * kLog2e)) : 0.f;
     return scale * s.w * (d_pg + d_kl);
 }
 // The token's terms in the two losses.
