@@ -114,7 +114,8 @@ __device__ __forceinline__ PolicyTerm policy_term(const RowArgs& p, const RowSca
     PolicyTerm q;
     q.lp = kFast ? kLn2 * (fmaf(zy, kLog2e, -tot.M) - lg2(tot.s + tot.ey)) : lp_relative(tot, zy);
     const float rho = kFast ? ex2((q.lp - s.lp_old) * kLog2e) : expf(q.lp - s.lp_old);
-    q.unclipped = -s.adv * rho;
+    // (an advantage of 0, a group of equal scores, has no policy part at a ratio beyond fp32 either: not 0 * inf)
+    q.unclipped = -s.adv * (s.adv == 0.f && rho > 1.f ? 1.f : rho);
     q.clipped = -s.adv * fminf(fmaxf(rho, p.ratio_lo), p.ratio_hi);
     q.free = !(q.unclipped < q.clipped);                              // NaN stays in
     return q;

@@ -42,3 +42,23 @@ def test_kl_reported_but_not_trained_on(V, dtype):
     assert abs(got.loss[0].item() - pg.item()) <= 8 * LP + 2 ** -23 * abs(pg.item())
     assert got.loss[1].item() == float("inf") and got.lp_new[0, 0].item() == float("-inf")
     assert lib.poll_status(ws) == 0
+
+
+@pytest.mark.parametrize("V", VOCABULARIES)
+def test_no_advantage_and_a_ratio_beyond_fp32(V):
+    """An advantage of 0 (a group of equal scores) leaves the policy part out, at any ratio: exp(lp - lp_old) = exp(190)."""
+    gen = torch.Generator(device=DEV).manual_seed(V + 1)
+    B, T = 2, 3
+    z, _ = ref.row_logits(B, T, V, BF, gen, DEV)
+    ids, lengths = labels(B, T, V, gen), torch.full((B,), T, dtype=torch.int32, device=DEV)
+    lp_old, lp_ref, adv = policy_inputs(z, ids, lengths, gen, False)
+    adv[0], lp_old[0, 1] = 0.0, -200.0
+    adv[1, 0], lp_old[1, 0] = 1.0, -200.0                # clipped: the loss is -1.3, no gradient
+    for kl_coef in (0.1, 0.0):
+        ws = lib.workspace(B, T, DEV)
+        got = lib.policy_kl_loss_fwd_bwd(z, ids, lengths, lp_old, lp_ref, adv, 0.2, 0.3, kl_coef, 0, 100.0, ws)
+        pg, kl, d, lp, size = ref.policy_kl(z.double(), ids, lengths, lp_old, lp_ref, adv, 0.2, 0.3, kl_coef, 0, 100.0)
+        part = torch.softmax(z.double(), dim=2) + torch.nn.functional.one_hot(ids, V)
+        check_gradient(got.dlogits, d, size[..., None] * part)
+        assert abs(got.loss[0].item() - pg.item()) <= 8 * LP + 2 ** -23 * abs(pg.item())
+        assert abs(got.loss[1].item() - kl.item()) <= 8 * LP + 2 ** -23 * abs(kl.item())
