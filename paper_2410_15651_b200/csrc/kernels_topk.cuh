@@ -515,8 +515,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_block_kernel(BlockLpArg
     pdl_wait_prior_grid();
     pdl_release_next_grid();
     const long long total = (long long)p.B * p.T;
-    int par = 0;
-    for (long long row = blockIdx.x; row < total; row += gridDim.x, par ^= 1) {
+    int par = 0;                                                     // set of parts of the next valid row
+    for (long long row = blockIdx.x; row < total; row += gridDim.x) {
         const int b = (int)(row / p.T), t = (int)(row % p.T);
         if (t >= clamp_len(__ldg(p.lengths + b), p.T)) {
             if (tid == 0) p.out_lp[row] = 0.f;
@@ -541,7 +541,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_block_kernel(BlockLpArg
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sw += __shfl_xor_sync(0xffffffffu, sw, o);
         if (lane == 0) s_part[par][warp] = make_float2(zw, sw);
-        __syncthreads();                                             // (the two sets of parts alternate)
+        // The two sets of parts alternate from one valid row to the next: a set is written again behind the barrier of the row
+        // between, which thread 0 reaches when it has read the set.  (A padded row passes no barrier and takes no set.)
+        __syncthreads();
         if (tid == 0) {
             float zt = kTopkFloor, st = 0.f;
             for (int w = 0; w < NT / 32; ++w) zt = fmaxf(zt, s_part[par][w].x);
@@ -550,6 +552,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_block_kernel(BlockLpArg
             // be 7e-8 too large)
             p.out_lp[row] = bad_id ? 0.f : (float)((double)zy - (double)zt - 0.6931471805599453 * log2_split(st));
         }
+        par ^= 1;
     }
     if (blockIdx.x == 0) block_count_valid(p.lengths, p.B, p.T, s_cnt, p.status);   // flags lengths out of range
 }
