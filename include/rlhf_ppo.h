@@ -340,7 +340,8 @@ typedef enum {
  *   topk_ids, topk_logprobs   int32 / fp32, [b*topk_stride_b + t*topk_stride_t + k], strides >= 0 in elements; the
  *                  log-probs are the teacher's at this temperature                                    read
  *   out_loss       fp32 scalar (device)                                                               written
- *   out_row_loss   fp32 [B,T] or NULL: temperature^2 L of every token, 0 at padding                   written if given
+ *   out_row_loss   fp32 [B,T] or NULL: temperature^2 L of every token, 0 at padding; must not overlap the entries
+ *                  (RLHF_ERR_STRIDE)                                                                  written if given
  *   0 < K <= RLHF_TOPK_MAX (else RLHF_ERR_SHAPE); temperature in [1e-3, 1e18].   workspace as for step 1.
  */
 int rlhf_distill_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,

@@ -469,6 +469,14 @@ bool overlap(const float* a, const float* b, int B, int T)
     return a && b && x < y + n && y < x + n;
 }
 
+// A contiguous [B,T] fp32 array (null: no) shares bytes with the span of 4-byte elements [b*sb + t*st + k], k < K.
+bool overlap_strided(const float* a, const void* b, int B, int T, long long sb, long long st, int K)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), n = 4 * (uintptr_t)B * (uintptr_t)T;
+    const uintptr_t m = 4 * ((uintptr_t)(B - 1) * (uintptr_t)sb + (uintptr_t)(T - 1) * (uintptr_t)st + (uintptr_t)K);
+    return a && x < y + m && y < x + n;
+}
+
 // Host-side checks of the loss call's arguments, the workspace apart (shared by the two loss entry points).
 int check_loss_args(const void* logits, long long stride_b, long long stride_t, const long long* ids,
                     long long ids_stride_b, const int* lengths, const float* lp_old, const float* adv,
@@ -1117,10 +1125,8 @@ int rlhf_policy_kl_loss_fwd_bwd(const void* logits, int logits_dtype, long long 
     if (!aligned(ids, 8) || !aligned(lengths, 4) || !aligned(lp_old, 4) || !aligned(lp_ref, 4) || !aligned(adv, 4) ||
         !aligned(out_loss_pg, 4) || !aligned(out_loss_kl, 4) || !aligned(out_lp_new, 4))
         return RLHF_ERR_ALIGN;
-    const uintptr_t adv_begin = reinterpret_cast<uintptr_t>(adv), lp_begin = reinterpret_cast<uintptr_t>(out_lp_new);
-    const uintptr_t adv_bytes = 4 * ((uintptr_t)(B - 1) * (uintptr_t)adv_stride_b + (uintptr_t)(T - 1) * (uintptr_t)adv_stride_t + 1);
     if (overlap(out_lp_new, lp_old, B, T) || overlap(out_lp_new, lp_ref, B, T) ||
-        (out_lp_new && lp_begin < adv_begin + adv_bytes && adv_begin < lp_begin + 4 * (uintptr_t)B * (uintptr_t)T))
+        overlap_strided(out_lp_new, adv, B, T, adv_stride_b, adv_stride_t, 1))
         return RLHF_ERR_STRIDE;
     if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
     DeviceInfo dev;
@@ -1268,6 +1274,9 @@ int rlhf_distill_loss_fwd_bwd(const void* logits, int logits_dtype, long long st
     if (!aligned(topk_ids, 4) || !aligned(topk_logprobs, 4) || !aligned(lengths, 4) || !aligned(out_loss, 4) ||
         !aligned(out_row_loss, 4))
         return RLHF_ERR_ALIGN;
+    if (overlap_strided(out_row_loss, topk_ids, B, T, topk_stride_b, topk_stride_t, K) ||
+        overlap_strided(out_row_loss, topk_logprobs, B, T, topk_stride_b, topk_stride_t, K))
+        return RLHF_ERR_STRIDE;
     if (int e = check_workspace(workspace, workspace_bytes, objective_workspace_bytes(B, T))) return e;
     DeviceInfo dev;
     if (int e = device_info(dev)) return e;
