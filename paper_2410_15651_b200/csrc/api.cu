@@ -300,6 +300,9 @@ CringPlan plan_cring(unsigned row_bytes, const DeviceInfo& dev, int K = 0)
         // a slice's chunks stay in the ring from pass 1 to pass 2, and the kernel is fast only while at least five
         // more slots prefetch the next slice
         if (C < 3 || C > R - 5 || kCringU * C - kRegVecsTmem > kTmemVecs) continue;
+        // distillation: the consumers tell the patch warp of the end of the rows, i, on the barrier of row i - kCringTargets, which
+        // it has passed because the end is announced in a slot that held a chunk of that row or of a later one
+        if (K > 0 && kCringTargets * C < R) continue;
         if ((size_t)row_vecs <= (size_t)(c - 1) * sv) continue;        // every block of the cluster has a share
         unsigned cols = 32;
         while (cols < (unsigned)(kCringU * C - kRegVecsTmem) * 8u * ((kCregWarps + 3) / 4)) cols *= 2;
