@@ -459,10 +459,13 @@ __device__ __forceinline__ void distill_publish(const DistillArgs& dt, float xsc
 
 // The same for few entries (kDistillFew at most), with loops that are not unrolled and entries that stay in shared memory.
 // With a copy of every step per entry of a lane, most of them jumped over, the helping warps' code drives the consumers' out of
-// the instruction cache: V = 32000, K = 64 took 209 us against 166 us of the objective with one token, and the warps waited for
-// instructions 3.5 of 13.5 cycles per issue; it takes 169 us like this.  With many entries the unrolled steps are faster (K =
-// 256: 194 against 258 us).
-constexpr int kDistillFew = 64;
+// the instruction cache: at V = 32000, K = 64 the warps waited for instructions 3.5 of 13.5 cycles per issue.  With many entries
+// the unrolled steps are faster.  Rolled / unrolled, us, bf16, plain mode:
+//     K                          64         96        128        160        256
+//     16 x 512 rows of 32000   173 / 216  185 / 217  194 / 193  220 / 194  267 / 198
+//     16 x 256 rows of 50272   146 / 145  148 / 145  152 / 146  158 / 146  176 / 148
+//     16 x 256 rows of 80000   242 / 267  250 / 269  261 / 267  275 / 267  308 / 270
+constexpr int kDistillFew = 96;
 
 struct EntrySet {
     int* pos;                // position in the block's slice, or -1

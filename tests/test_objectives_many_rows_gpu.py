@@ -36,7 +36,7 @@ def gradient_shares(lengths, T, scale):
 @pytest.mark.parametrize("B,T,V,dtype", [(16, 190, 8200, BF), (16, 190, 20000, BF), (16, 190, 8201, HF), (16, 190, 20003, BF),
                                          (10, 120, 80000, BF), (16, 150, 57344, HF), (10, 120, 128256, BF), (20, 250, 1000, BF),
                                          (20, 250, 1001, HF)])
-@pytest.mark.parametrize("K", [8, 64, 65, 200])
+@pytest.mark.parametrize("K", [8, 64, 65, 96, 97, 200])
 def test_distill(B, T, V, dtype, K):
     gen = torch.Generator(device=DEV).manual_seed(V + K)
     z, lengths = batch(B, T, V, dtype, gen), ragged(B, T, gen)
