@@ -587,9 +587,10 @@ int launch_topk_as(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 }
 
 // Threads per row.  1024 where there are no more rows than SMs and a row keeps them busy (one row of 50272: 13 us against
-// 16 us with 256).  Else by the row's length, measured on 4096 rows: V = 1000, K = 32: 68 us with 64 threads, 104 with 128,
-// 191 with 256; V = 8192, K = 32: 33, 35, 51; V = 32000, K = 64: 118, 78, 86; relative to the
-// fastest, V = 50272, K = 256: 2.06, 1, 1.05; V = 128256, K = 128: 2.36, 1.15, 1.
+// 16 us with 256).  Else by the row's length; 4096 full rows with 64 / 128 / 256 threads, us: V = 1000, K = 32: 26 / 32 / 54 (16384
+// rows: 63 / 104 / 189); V = 8192, K = 32: 35 / 36 / 53 (16384 rows: 94 / 123 / 187); V = 16384, K = 32: 49 / 47 / 67; V = 32000,
+// K = 64: 96 / 81 / 90; V = 50272, K = 64: 138 / 110 / 112, K = 256: 325 / 203 / 211; V = 80000, K = 64: 209 / 167 / 162;
+// V = 128256, K = 128: 419 / 285 / 258.
 template <bool kF16>
 int launch_topk(const TopkArgs& ta, const DeviceInfo& dev, cudaStream_t s)
 {

@@ -1,6 +1,10 @@
 // Distillation from a teacher's entries for rows outside the range of loss_creg_kernel<..., kDistill> (kernels_creg.cuh):
-// rows shorter than 16 KB or longer than a cluster of four blocks holds, and gradient rows laid out off their logits rows'
-// 16-byte boundaries.
+// rows shorter than 16 KB or longer than a cluster of four blocks holds, rows off 16-byte boundaries that one block does not hold
+// (more than 53241 entries), and gradient rows laid out off their logits rows' 16-byte boundaries.
+//
+// A rare case is served plainly: the kernel is bound by its own instructions, not by DRAM.  4096 rows, bf16, K = 64: V = 1000 81 us,
+// 8176 164 us (floor 20), 53249 534 us (133), 100277 964 us (250; V = 100280 on the fast kernel 277), 151643 1427 us; V = 50272
+// with gradients at another offset 607 us (146 at the same).
 //
 // One block per row, dealt statically; the row is read twice, the second time from L2.  The teacher's entries go into a
 // small hash table in shared memory (entry -> position in the list); a bitmap over the row's 16-byte vectors (mod 4096)

@@ -102,8 +102,9 @@ __device__ __forceinline__ float lp_relative(const Acc& a, float zy)
 }
 
 // A token of kObjPolicyKl.  A whole block waits for the gradient once per row, so that it forms it by a short chain on the
-// hardware's ex2 and lg2 (kFast; relative error about 2^-22, as in row_finish_fast); 1 - exp(d) loses its relative accuracy
-// at small d, where it is small beside the policy part.  The loss terms are formed by one thread, without the shortcuts.
+// hardware's ex2 and lg2 (kFast; relative error about 2^-22, as in row_finish_fast).  1 - exp(d) loses its relative accuracy at
+// small d: its absolute error of about 2^-22 is that of lp, and so of d, itself (half a step of fp32 from 4 to 8 is 2^-22), also where
+// it is the whole gradient (a clipped token, an advantage of 0).  The loss terms are formed by one thread, without the shortcuts.
 struct PolicyTerm {
     float lp, unclipped, clipped;
     bool free;                  // the unclipped branch is active

@@ -11,10 +11,11 @@
 // Exponents are formed as (z - maximum) * log2(e) / temperature: the difference of two 16-bit values is exact or nearly so,
 // whatever their size.
 //
-// Floor: one read of the row from DRAM (32 us for 2048 rows of 50272 in bf16 at 6.5 TB/s).  What bounds the kernel is
-// the chain of dependent steps that selects a row, while its block loads nothing new: the same rows of 50272
-// take 1.9 times as long at K = 256 as at K = 64, and 0.8 times at K = 8.  Neither DRAM (45%) nor the issue slots (49%) are full,
-// and a warp waits 6.9 of 14.2 cycles per instruction for global loads.  Per row and K = 64 there are 14,600 warp
+// Floor: one read of the row from DRAM (32 us for 2048 rows of 50272 in bf16 at 6.5 TB/s).  Nothing is full: DRAM 45%, issue slots
+// 48%, and a warp waits 6.9 of 14.1 cycles per instruction for global loads.  Too few rows are streamed at a time: a block that
+// selects a row loads nothing new, and at 64 registers an SM holds 1024 threads.  The same rows of 50272 take 1.8 times as long
+// at K = 256 as at K = 64 (candidates are ranked pair by pair), and 0.8 times at K = 8.  Fewer registers for more blocks per SM, and
+// a sort of the candidates, are not tried.  Per row and K = 64 there are 14,600 warp
 // instructions, some 9,000 of them for the stream (one ex2 and half a packed maximum per logit).  Measured on such rows and
 // dropped, with their time over this kernel's: the first 8 to 32 KB of the next row brought to L2 before the selection (0.99
 // to 1.03, and 1.04 at V = 1000); a row per warp (all rows of a batch are then in flight, L2 does not hold

@@ -10,8 +10,8 @@ from test_objectives_gpu import BF, DEV, HF, LP, check_distill, check_gradient
 pytestmark = pytest.mark.gpu
 
 # rows below 16 KB, off 16-byte boundaries, in one block (registers alone, and with tensor memory), beyond one block and off a
-# boundary, in the chunk ring (one block, two), in clusters of two and four with whole-slice buffers, beyond every cluster
-VOCABULARIES = [1000, 1001, 8200, 20000, 50257, 57353, 57344, 80000, 128256, 212992, 300000]
+# boundary, in the chunk ring (one block, two, four), in clusters of two to four with whole-slice buffers, beyond every cluster
+VOCABULARIES = [1000, 1001, 8200, 20000, 50257, 57353, 57344, 80000, 128256, 150000, 212992, 230000, 300000]
 
 
 def entries_of(V, K, shape, gen, first):
