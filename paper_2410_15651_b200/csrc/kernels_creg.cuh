@@ -175,14 +175,18 @@ __device__ __forceinline__ DistillOutside distill_outside(const TargetInfo& ti, 
     return DistillOutside{ti.P, t.M, t.s + t.ey};
 }
 
-// Loss of a row.
+// Loss of a row.  The logarithm of the mass outside is taken of s while that is in range: s and the sum s + ey share the error of
+// the ex2 (2^-22) that brought s to the row's reference, and where most of the mass is outside it cancels (row losses at 16 x 256
+// rows of 50272, tail mode: 1.5e-7 off, 2.5e-7 with so throughout).
 __device__ __forceinline__ double distill_loss(const TargetInfo& ti, const DistillTotals& t)
 {
     constexpr double ln2 = 0.6931471805599453;
     const double l2 = log2_split(t.s + t.ey);
     double L = ti.H - ln2 * ((double)t.zy - (double)ti.P * l2);
-    if (distill_has_tail(ti, t.so))
-        L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (log2_split(t.so) + ((double)t.Mo - (double)t.M) - l2));
+    if (distill_has_tail(ti, t.so)) {
+        const double lo = t.s > 1e-20f ? log2_split(t.s) : log2_split(t.so) + ((double)t.Mo - (double)t.M);
+        L += (double)ti.p0 * ln2 * (log2_split(ti.p0) - (lo - l2));
+    }
     return L;
 }
 
