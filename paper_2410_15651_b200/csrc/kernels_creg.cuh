@@ -176,7 +176,7 @@ __device__ __forceinline__ DistillOutside distill_outside(const TargetInfo& ti, 
 }
 
 // Loss of a row.  The logarithm of the mass outside is taken of s while that is in range: s and the sum s + ey share the error of
-// the ex2 (2^-22) that brought s to the row's reference, and where most of the mass is outside it cancels (row losses at 16 x 256
+// the ex2 (2^-22) that brought s to the row's reference, and where most of the mass is outside it cancels (row losses at 8 x 64
 // rows of 50272, tail mode: 1.5e-7 off, 2.5e-7 with so throughout).
 __device__ __forceinline__ double distill_loss(const TargetInfo& ti, const DistillTotals& t)
 {
