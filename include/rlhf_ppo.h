@@ -23,6 +23,16 @@
  *   rlhf_topk_logprobs             a teacher's K largest log-probs per token
  *   rlhf_distill_loss_fwd_bwd      distillation of a student from those
  *
+ * of the distribution that a rollout's tokens are drawn from, where penalties, a bias, a grammar or a temperature stand
+ * between the logits and the softmax:
+ *
+ *   rlhf_shape_logits, rlhf_shape_logits_bwd         the shaped logits, and the gradient through the shaping
+ *   rlhf_shaped_logprobs, rlhf_shaped_logprobs_bwd   log-probs (and entropy) under them, and their gradient
+ *
+ * and of a policy with experts:
+ *
+ *   rlhf_router_loss_fwd_bwd       balance loss of the router's logits, with the experts' counts
+ *
  * The paper gives these quantities in prose only; the formulas are the standard definitions and
  * are written out beside each function.
  *
@@ -78,7 +88,8 @@ typedef enum {
     /* device-detected, sticky in the workspace, bit flags (may be OR-ed together) */
     RLHF_ERR_ID_RANGE = 16,     /* a generated-token id outside [0,V) at a valid position */
     RLHF_ERR_LENGTH_RANGE = 32, /* a length outside [0,T] (clamped) */
-    RLHF_ERR_TIMEOUT = 64       /* an internal bounded wait ran out; outputs of this call are invalid */
+    RLHF_ERR_TIMEOUT = 64,      /* an internal bounded wait ran out; outputs of this call are invalid */
+    RLHF_ERR_VALUE_RANGE = 128  /* a setting of a sequence (rlhf_shaping_t) outside its range (taken as neutral) */
 } rlhf_status_t;
 
 /* Element type of a logits tensor (and of the gradient written for it): the two 16-bit floating-point
@@ -89,7 +100,8 @@ typedef enum {
  * below that bound (with grad_scale = 1 it always does), else the entry becomes +-inf. */
 typedef enum {
     RLHF_BF16 = 0,
-    RLHF_F16 = 1
+    RLHF_F16 = 1,
+    RLHF_F32 = 2                /* where a function names it: shaped logits that are written, logits of a router */
 } rlhf_dtype_t;
 
 /* Human-readable name of a status (static storage; flags are joined with '|'). Host, never NULL. */
@@ -414,6 +426,152 @@ int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long
                                  int length_mean, float grad_scale, float* out_loss, float* out_rewards,
                                  void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
                                  float* out_lp_new, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * What stands between a model's logits and the distribution that tokens are drawn from.  A struct on the host; its pointers
+ * are device pointers, read by the call's kernels.  All of them may be NULL (and the lengths 0): that part is left out.
+ *
+ * Row (b,t) belongs to position start[b] + t of the answer of sequence b.  Its history H is the prompt and the answer's tokens
+ * before that position, prompt[b, 0 .. prompt_lengths[b]) and tokens[b, 0 .. start[b] + t); c_v is how often the latter
+ * holds v.  For t < lengths[b],
+ *     z1 = z_v * r  if z_v < 0,  z_v / r  otherwise       where v is in H; else z_v            (r = repetition[b])
+ *     z2 = z1 - frequency[b] * c_v - presence[b] * [c_v > 0]
+ *     x_v = (z2 + bias_v) / temperature[b]                where the mask allows v; else -inf, whatever z_v and bias_v are.
+ * A decoding step has T = 1 and start[b] tokens so far; the rows of whole answers have start = NULL and tokens = ids.
+ *   prompt, tokens   int64, [b*stride_b + i], i < prompt_len / tokens_len.  An id of -1 is no token (padding); another one outside
+ *                    [0,V) sets RLHF_ERR_ID_RANGE and is none.  Tokens from start[b] + lengths[b] - 1 on are not read.
+ *   prompt_lengths   int32 [B]; NULL: prompt_len.   start   int32 [B]; NULL: 0.  A prompt length outside [0, prompt_len], a
+ *                    negative start, or tokens that end before a row's history (start[b] + lengths[b] - 1 > tokens_len) set
+ *                    RLHF_ERR_LENGTH_RANGE; what there is counts.
+ *   repetition, temperature   fp32 [B], in [1e-3, 1e18];   frequency, presence   fp32 [B], |.| <= 1e18.  Others set
+ *                    RLHF_ERR_VALUE_RANGE and are taken as 1 and 0.
+ *   bias             fp32 [b*bias_stride_b + v] (stride 0: one for all sequences)
+ *   mask             bit v % 32 of the 32-bit word [b*mask_stride_b + t*mask_stride_t + v/32] is 1 where v is allowed (strides in
+ *                    words, 0 to share); bits from V on say nothing.
+ */
+typedef struct {
+    const long long* prompt;
+    long long prompt_stride_b;
+    const int* prompt_lengths;
+    int prompt_len;
+    int tokens_len;
+    const long long* tokens;
+    long long tokens_stride_b;
+    const int* start;
+    const float* repetition;
+    const float* frequency;
+    const float* presence;
+    const float* temperature;
+    const float* bias;
+    long long bias_stride_b;
+    const unsigned int* mask;
+    long long mask_stride_b;
+    long long mask_stride_t;
+} rlhf_shaping_t;
+
+/*
+ * The shaped logits, out[b,t,v] = x_v: for a sampler, or for any loss of this library that is to see them.
+ *   logits   bf16 or binary16 (logits_dtype) through (stride_b, stride_t)      read
+ *   out      the same type, or fp32 (out_dtype); through (out_stride_b, out_stride_t); 0 at padded rows.  May be the logits
+ *            buffer itself with the same type and strides; with penalties alone, then, only the history's entries are touched
+ *            (and padded rows), must not otherwise overlap it or what the shaping reads     written
+ * 16-bit outputs are rounded to nearest even: what a loss reads is then a distribution up to 2^-8 (bf16; fp16 2^-11) of |x_v| off.
+ * rlhf_shaped_logprobs rounds nothing.   workspace as for step 1.
+ */
+int rlhf_shape_logits(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                      const rlhf_shaping_t* shaping, const int* lengths, int B, int T, int V,
+                      void* out, int out_dtype, long long out_stride_b, long long out_stride_t,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient through the shaping: with d the gradient of a loss with respect to x,
+ *     out_dlogits[b,t,v] = d_v / temperature[b] * (v in H ? (z_v < 0 ? r : 1/r) : 1)   where the mask allows v, else 0
+ * (0 whatever d_v is there), and 0 at padded rows.  The penalties, the bias and the temperature are constants.
+ *   dshaped      type logits_dtype, through (ds_stride_b, ds_stride_t)                     read
+ *   logits       as given to rlhf_shape_logits (the signs of the history's entries)        read
+ *   out_dlogits  type logits_dtype; may be dshaped itself with the same strides (without mask and temperature, then, only the
+ *                history's entries are touched, and padded rows); not the logits           written
+ */
+int rlhf_shape_logits_bwd(const void* dshaped, int logits_dtype, long long ds_stride_b, long long ds_stride_t,
+                          const void* logits, long long stride_b, long long stride_t,
+                          const rlhf_shaping_t* shaping, const int* lengths, int B, int T, int V,
+                          void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Step 1 under the shaped logits, without writing them.  For t < lengths[b], with y = ids[b,t] and p = softmax(x):
+ *     out_logprobs[b,t] = x_y - log sum_v exp(x_v)
+ *     out_lse[b,t,:]    = two numbers whose sum is log sum_v exp(x_v) (the second alone is small: rows far from 0)
+ *     out_entropy[b,t]  = - sum_v p_v log p_v
+ * and 0 at padded positions.  A token at -inf (masked, say) has log-prob -inf; so has every token of a row that the mask
+ * leaves empty, whose entropy is 0.  A token whose id is out of range has log-prob 0 and sets the flag.
+ *   logits, ids, lengths   as rlhf_gather_logprobs_ex                          read
+ *   out_logprobs fp32 [B,T], out_lse fp32 [B,T,2] (8-byte aligned), out_entropy fp32 [B,T] or NULL     written
+ *   workspace as for step 1.
+ */
+int rlhf_shaped_logprobs(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                         const long long* ids, long long ids_stride_b, const rlhf_shaping_t* shaping, const int* lengths,
+                         int B, int T, int V, float* out_logprobs, float* out_lse, float* out_entropy,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient: with g and h the gradients of a loss with respect to the log-probs and the entropies,
+ *     dx_v = g[b,t] * ([v == y] - p_v) - h[b,t] * p_v * (log p_v + entropy[b,t])
+ * through the shaping as in rlhf_shape_logits_bwd; rounded once.  An entry at x_v = -inf has gradient 0, so has a row that the
+ * mask leaves empty; a token whose id is out of range has g = 0.
+ *   logprobs, lse, entropy   what rlhf_shaped_logprobs wrote for the same arguments (entropy: with grad_entropy)    read
+ *   grad_logprobs fp32 [B,T], grad_entropy fp32 [B,T] or NULL (none)                                             read
+ *   out_dlogits   type logits_dtype; 0 at padded rows; may be the logits buffer itself with the same strides      written
+ */
+int rlhf_shaped_logprobs_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                             const long long* ids, long long ids_stride_b, const rlhf_shaping_t* shaping, const int* lengths,
+                             int B, int T, int V, const float* logprobs, const float* lse, const float* entropy,
+                             const float* grad_logprobs, const float* grad_entropy,
+                             void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* A token's probabilities over the experts. */
+typedef enum {
+    RLHF_ROUTER_SOFTMAX = 0,    /* p = softmax(z) */
+    RLHF_ROUTER_SIGMOID = 1     /* p_e = sigmoid(z_e) / sum_j sigmoid(z_j) */
+} rlhf_router_scoring_t;
+
+/* Over what the experts are to be balanced. */
+typedef enum {
+    RLHF_ROUTER_BATCH = 0,      /* all valid tokens of a layer */
+    RLHF_ROUTER_SEQUENCE = 1    /* each sequence by itself; the loss is the mean over the non-empty ones */
+} rlhf_router_scope_t;
+
+/*
+ * Balance loss of the routers of a policy with experts, and its gradient: L layers, E experts, K of them chosen by each of the
+ * N valid tokens of a layer.  With c_e how often the group's n tokens (RLHF_ROUTER_BATCH: all N; RLHF_ROUTER_SEQUENCE: those
+ * of one sequence) chose expert e, f_e = E * c_e / (K * n) (1 where the experts are balanced) and p as above,
+ *     out_loss[l,0] = (1/n) sum_tokens sum_e f_e p_e       (1 where they are balanced; mean over the non-empty sequences)
+ *     out_loss[l,1] = (1/N) sum_tokens (log sum_e exp(z_e))^2                       if z_coef != 0, else 0
+ *     out_dlogits   = grad_scale * d (balance_coef * out_loss[l,0] + z_coef * out_loss[l,1]) / dz     with f constant
+ * out_counts = c, int32 [L,E] (RLHF_ROUTER_SEQUENCE: [L,B,E]).  No valid token: all 0.  The losses are summed in double
+ * precision in a fixed order; the coefficients are not applied to them.
+ * The choice: expert_ids, an expert chosen twice by a token counting twice, -1 none, others outside [0,E) none with
+ * RLHF_ERR_ID_RANGE; or, where expert_ids is NULL, the K largest logits of each token (of equal ones the lowest expert), which
+ * out_ids then says in descending order, 0 at padded positions.
+ * An expert at -inf has p = 0 and gradient 0; a token whose experts all are adds 0 to the losses.  Finite logits must satisfy |z| <= 1e38.  With several ranks each balances its own
+ * tokens.
+ *   logits       bf16, binary16 or fp32 (logits_dtype), [l*stride_l + b*stride_b + t*stride_t + e]                 read
+ *   expert_ids   int32 or NULL, [l*ids_stride_l + b*ids_stride_b + t*ids_stride_t + k]                          read
+ *   lengths      int32 [B]: tokens of a sequence that are routed, the prompt's among them                        read
+ *   out_dlogits  type logits_dtype through its own strides; 0 at padded positions; may be the logits buffer with the same
+ *                strides                                                                                        written
+ *   out_ids      int32 [L,B,T,K] or NULL; not written if expert_ids is given                                      written
+ *   L, B, T, E > 0, E <= 1024, L*B*T <= 2^29, 0 < K <= E (else RLHF_ERR_SHAPE); coefficients finite; z_coef = 0 unless
+ *   RLHF_ROUTER_SOFTMAX.   workspace   >= rlhf_router_workspace_bytes(L,B,T,E), 256-B aligned, initialised.
+ */
+size_t rlhf_router_workspace_bytes(int L, int B, int T, int E);
+int rlhf_router_loss_fwd_bwd(const void* logits, int logits_dtype, long long stride_l, long long stride_b, long long stride_t,
+                             const int* expert_ids, long long ids_stride_l, long long ids_stride_b, long long ids_stride_t,
+                             const int* lengths, int L, int B, int T, int E, int K, int scoring, int scope,
+                             float balance_coef, float z_coef, float grad_scale, float* out_loss, int* out_counts, int* out_ids,
+                             void* out_dlogits, long long dl_stride_l, long long dl_stride_b, long long dl_stride_t,
+                             void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Step 4 for callers that cannot provide a workspace.  (The paper has no counterpart to this

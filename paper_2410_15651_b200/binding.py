@@ -21,6 +21,17 @@ _f32 = ctypes.c_float
 _vp = ctypes.c_void_p
 _sz = ctypes.c_size_t
 
+
+class ShapingStruct(ctypes.Structure):
+    """rlhf_shaping_t"""
+    _fields_ = [("prompt", _vp), ("prompt_stride_b", _i64), ("prompt_lengths", _vp), ("prompt_len", _int),
+                ("tokens_len", _int), ("tokens", _vp), ("tokens_stride_b", _i64), ("start", _vp), ("repetition", _vp),
+                ("frequency", _vp), ("presence", _vp), ("temperature", _vp), ("bias", _vp), ("bias_stride_b", _i64),
+                ("mask", _vp), ("mask_stride_b", _i64), ("mask_stride_t", _i64)]
+
+
+_shp = ctypes.POINTER(ShapingStruct)
+
 # name -> (restype, argtypes); mirrors include/rlhf_ppo.h
 SIGNATURES = {
     "rlhf_status_string": (ctypes.c_char_p, [_int]),
@@ -58,12 +69,24 @@ SIGNATURES = {
     "rlhf_preference_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _int, _int, _int,
                                             _int, _f32, _f32, _f32, _int, _f32, _vp, _vp,
                                             _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "rlhf_shape_logits": (_int, [_vp, _int, _i64, _i64, _shp, _vp, _int, _int, _int, _vp, _int, _i64, _i64, _vp, _sz, _vp]),
+    "rlhf_shape_logits_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _i64, _shp, _vp, _int, _int, _int, _vp, _i64, _i64,
+                                     _vp, _sz, _vp]),
+    "rlhf_shaped_logprobs": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _shp, _vp, _int, _int, _int, _vp, _vp, _vp,
+                                    _vp, _sz, _vp]),
+    "rlhf_shaped_logprobs_bwd": (_int, [_vp, _int, _i64, _i64, _vp, _i64, _shp, _vp, _int, _int, _int, _vp, _vp, _vp, _vp, _vp,
+                                        _vp, _i64, _i64, _vp, _sz, _vp]),
+    "rlhf_router_workspace_bytes": (_sz, [_int, _int, _int, _int]),
+    "rlhf_router_loss_fwd_bwd": (_int, [_vp, _int, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _int, _int, _int, _int, _int,
+                                        _int, _int, _f32, _f32, _f32, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _sz, _vp]),
 }
 
 NOALLOC_MAX_TOKENS = 65536
 MEAN_TOKENS, MEAN_SEQUENCES = 0, 1                    # rlhf_reduction_t
 DISTILL_PLAIN, DISTILL_NORMALISED, DISTILL_TAIL = 0, 1, 2   # rlhf_distill_t
 PREF_SIGMOID, PREF_HINGE, PREF_SQUARED = 0, 1, 2      # rlhf_preference_t
+ROUTER_SOFTMAX, ROUTER_SIGMOID = 0, 1                 # rlhf_router_scoring_t
+ROUTER_BATCH, ROUTER_SEQUENCE = 0, 1                  # rlhf_router_scope_t
 
 _lib = None
 
@@ -610,4 +633,221 @@ def preference_loss_fwd_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: to
           margin, label_smoothing, int(length_mean), grad_scale, _arg(out.loss, (1,), _F32, dev, "out.loss"),
           _arg(out.rewards, (B,), _F32, dev, "out.rewards"), *_dlogits(out.dlogits, logits, dev),
           _opt(out.lp_new, (B, T), _F32, dev, "out.lp_new"), *_ws(ws, dev))
+    return out
+
+
+# ---------------------------------------------------------------- shaped logits
+class Shaping:
+    """rlhf_shaping_t for B sequences over a vocabulary of V: the settings of a rollout and the history that its penalties
+    look at.  The tensors are read by every call that is given this object (they may be changed in place between calls, as a
+    decoding loop does with `tokens` and `start`), and are kept alive by it.
+
+      tokens [B,S] int64      the answer's tokens; those before a row are its history
+      start [B] int32         tokens before the first row (none: 0)
+      prompt [B,P] int64      -1: padding;  prompt_lengths [B] int32 (none: P)
+      repetition, frequency, presence, temperature [B] fp32
+      bias [V] or [B,V] fp32
+      mask [B,W] or [B,T,W] int32, W = ceil(V / 32) words of allowed entries (any strides; a first axis of 1 is shared)
+    """
+
+    def __init__(self, B: int, V: int, tokens: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
+                 prompt: Optional[torch.Tensor] = None, prompt_lengths: Optional[torch.Tensor] = None,
+                 repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                 presence: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                 bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None):
+        given = {k: t for k, t in dict(tokens=tokens, start=start, prompt=prompt, prompt_lengths=prompt_lengths,
+                                       repetition=repetition, frequency=frequency, presence=presence,
+                                       temperature=temperature, bias=bias, mask=mask).items() if t is not None}
+        for name, t in given.items():
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a CUDA tensor (the library has no CPU path)")
+        self.B, self.V, self.tensors = B, V, given
+        self.mask_rows = 0                               # rows that the mask has of a sequence; 0: any number
+        self.dev = next((t.get_device() for t in given.values()), None)
+        c = self.struct = ShapingStruct()
+        for name in ("tokens", "prompt"):
+            if name not in given:
+                continue
+            t = _dev(given[name], torch.int64, name)
+            if t.dim() != 2 or t.shape[0] != B or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError(f"{name} must be [{B},n] with a contiguous last axis")
+            setattr(c, name, t.data_ptr())
+            setattr(c, name + "_stride_b", t.stride(0))
+            setattr(c, name + "_len", t.shape[1])
+        for name, dtype in (("start", torch.int32), ("prompt_lengths", torch.int32), ("repetition", _F32), ("frequency", _F32),
+                            ("presence", _F32), ("temperature", _F32)):
+            if name in given:
+                setattr(c, name, _arg(given[name], (B,), dtype, self.dev, name))
+        if bias is not None:
+            _dev(bias, _F32, "bias")
+            if bias.shape not in ((V,), (B, V)) or (V > 1 and bias.stride(-1) != 1):
+                raise ValueError(f"bias must be [{V}] or [{B},{V}] with a contiguous vocabulary axis")
+            c.bias, c.bias_stride_b = bias.data_ptr(), bias.stride(0) if bias.dim() == 2 else 0
+        if mask is not None:
+            _dev(mask, torch.int32, "mask")
+            W = (V + 31) // 32
+            if mask.dim() not in (2, 3) or mask.shape[0] not in (1, B) or mask.shape[-1] != W or (W > 1 and mask.stride(-1) != 1):
+                raise ValueError(f"mask must be [{B},{W}] or [{B},T,{W}] with contiguous words")
+            c.mask, c.mask_stride_b = mask.data_ptr(), mask.stride(0) if mask.shape[0] > 1 else 0
+            if mask.dim() == 3 and mask.shape[1] != 1:
+                self.mask_rows, c.mask_stride_t = mask.shape[1], mask.stride(1)
+        for name, t in given.items():
+            _same_device(t, self.dev, name)
+        self._pointer = ctypes.pointer(c)
+
+    def pointer(self, B: int, T: int, V: int, dev: int):
+        """The struct for a call on [B,T,V] logits of this device."""
+        if self.B != B or self.V != V or (self.mask_rows and self.mask_rows != T):
+            raise ValueError(f"the shaping is for {self.B} sequences over {self.V} entries"
+                             + (f" and {self.mask_rows} rows" if self.mask_rows else "") + f", the logits are [{B},{T},{V}]")
+        if self.dev is not None and self.dev != dev:
+            raise ValueError(f"the shaping is on cuda:{self.dev}, the logits on cuda:{dev}")
+        return self._pointer
+
+
+SHAPED_DTYPES = {torch.bfloat16: 0, torch.float16: 1, _F32: 2}
+
+
+def _rows_out(t: torch.Tensor, logits: torch.Tensor, dev: int, what: str) -> Tuple[int, int, int]:
+    """(address, stride_b, stride_t) of a tensor of the logits' shape."""
+    if t.shape != logits.shape:
+        raise ValueError(f"{what} must have the shape of logits")
+    _same_device(t, dev, what)
+    sb, st, sv = t.stride()
+    if sv != 1 and t.shape[2] > 1:
+        raise ValueError(f"{what} must have a contiguous vocabulary axis")
+    return t.data_ptr(), sb, st
+
+
+def shape_logits(logits: torch.Tensor, lengths: torch.Tensor, shaping: Shaping, ws: torch.Tensor,
+                 out: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """rlhf_shape_logits: the shaped logits, in the logits' type or fp32 (`dtype`, or that of `out`); `out` may be the logits."""
+    B, T, V, sb, st, dev = _rows(logits)
+    if out is None:
+        out = torch.empty((B, T, V), dtype=dtype or logits.dtype, device=logits.device)
+    if out.dtype is not (dtype or out.dtype) or out.dtype not in (logits.dtype, _F32):
+        raise TypeError("out must have the element type of logits, or float32")
+    p, osb, ost = _rows_out(out, logits, dev, "out")
+    _call("rlhf_shape_logits", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st, shaping.pointer(B, T, V, dev),
+          _arg(lengths, (B,), torch.int32, dev, "lengths"), B, T, V, p, SHAPED_DTYPES[out.dtype], osb, ost, *_ws(ws, dev))
+    return out
+
+
+def shape_logits_bwd(dshaped: torch.Tensor, logits: torch.Tensor, lengths: torch.Tensor, shaping: Shaping, ws: torch.Tensor,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """rlhf_shape_logits_bwd: the gradient with respect to the logits, from the one with respect to the shaped logits (of the
+    logits' type); `out` may be dshaped."""
+    B, T, V, sb, st, dev = _rows(logits)
+    if dshaped.dtype is not logits.dtype:
+        raise TypeError("dshaped must have the element type of logits")
+    if out is None:
+        out = _like(logits)
+    d, dsb, dst = _rows_out(dshaped, logits, dev, "dshaped")
+    _call("rlhf_shape_logits_bwd", dev, d, DTYPES[logits.dtype], dsb, dst, logits.data_ptr(), sb, st,
+          shaping.pointer(B, T, V, dev), _arg(lengths, (B,), torch.int32, dev, "lengths"), B, T, V,
+          *_dlogits(out, logits, dev), *_ws(ws, dev))
+    return out
+
+
+class ShapedLogprobs:
+    """What shaped_logprobs writes and shaped_logprobs_bwd reads: log-probs [B,T], the normaliser in two parts [B,T,2] and,
+    if wanted, the entropy [B,T]; reusable from call to call."""
+
+    def __init__(self, logits: torch.Tensor, want_entropy: bool = False, logprobs: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None):
+        B, T, _ = logits.shape
+        new = lambda *n: logits.new_empty(n, dtype=_F32)  # noqa: E731
+        self.logprobs = new(B, T) if logprobs is None else logprobs
+        self.lse = new(B, T, 2) if lse is None else lse
+        self.entropy = new(B, T) if entropy is None and want_entropy else entropy
+
+
+def shaped_logprobs(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor, shaping: Shaping, ws: torch.Tensor,
+                    want_entropy: bool = False, out: Optional[ShapedLogprobs] = None) -> ShapedLogprobs:
+    """rlhf_shaped_logprobs: log-probs (and entropy, if wanted or if `out` has a place for it) under the shaped logits."""
+    B, T, V, sb, st, dev = _rows(logits)
+    if out is None:
+        out = ShapedLogprobs(logits, want_entropy)
+    _call("rlhf_shaped_logprobs", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st, *_ids_arg(ids, B, T, dev),
+          shaping.pointer(B, T, V, dev), _arg(lengths, (B,), torch.int32, dev, "lengths"), B, T, V,
+          _arg(out.logprobs, (B, T), _F32, dev, "out.logprobs"), _arg(out.lse, (B, T, 2), _F32, dev, "out.lse"),
+          _opt(out.entropy, (B, T), _F32, dev, "out.entropy"), *_ws(ws, dev))
+    return out
+
+
+def shaped_logprobs_bwd(logits: torch.Tensor, ids: torch.Tensor, lengths: torch.Tensor, shaping: Shaping,
+                        forward: ShapedLogprobs, grad_logprobs: torch.Tensor, grad_entropy: Optional[torch.Tensor],
+                        ws: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """rlhf_shaped_logprobs_bwd: the gradient with respect to the logits; `out` may be the logits."""
+    B, T, V, sb, st, dev = _rows(logits)
+    if out is None:
+        out = _like(logits)
+    _call("rlhf_shaped_logprobs_bwd", dev, logits.data_ptr(), DTYPES[logits.dtype], sb, st, *_ids_arg(ids, B, T, dev),
+          shaping.pointer(B, T, V, dev), _arg(lengths, (B,), torch.int32, dev, "lengths"), B, T, V,
+          _arg(forward.logprobs, (B, T), _F32, dev, "forward.logprobs"), _arg(forward.lse, (B, T, 2), _F32, dev, "forward.lse"),
+          _opt(forward.entropy, (B, T), _F32, dev, "forward.entropy"),
+          _arg(grad_logprobs, (B, T), _F32, dev, "grad_logprobs"), _opt(grad_entropy, (B, T), _F32, dev, "grad_entropy"),
+          *_dlogits(out, logits, dev), *_ws(ws, dev))
+    return out
+
+
+# ---------------------------------------------------------------- the router of a policy with experts
+def router_workspace_bytes(L: int, B: int, T: int, E: int) -> int:
+    return int(lib().rlhf_router_workspace_bytes(L, B, T, E))
+
+
+def router_workspace(L: int, B: int, T: int, E: int, device) -> torch.Tensor:
+    """Allocate (through torch) and initialise a workspace for router_loss_fwd_bwd on [L,B,T,E] logits."""
+    ws = torch.empty(router_workspace_bytes(L, B, T, E), dtype=torch.uint8, device=device)
+    with torch.cuda.device(ws.device):
+        _check(lib().rlhf_workspace_init(ws.data_ptr(), ws.numel(), _stream(ws)), "rlhf_workspace_init")
+    return ws
+
+
+class RouterOutputs:
+    """Buffers written by router_loss_fwd_bwd; reusable from call to call."""
+
+    def __init__(self, logits: torch.Tensor, k: int, scope: int, in_place: bool = False, want_ids: bool = True):
+        L, B, T, E = logits.shape
+        new = lambda dtype, *n: logits.new_empty(n, dtype=dtype)  # noqa: E731
+        self.loss = new(_F32, L, 2)                                                  # [balance, z-loss] of every layer
+        self.counts = new(torch.int32, L, B, E) if scope == ROUTER_SEQUENCE else new(torch.int32, L, E)
+        self.dlogits = logits if in_place else _like(logits)
+        self.ids = new(torch.int32, L, B, T, max(k, 0)) if want_ids else None
+
+
+def router_loss_fwd_bwd(logits: torch.Tensor, lengths: torch.Tensor, k: int, scoring: int, scope: int, balance_coef: float,
+                        z_coef: float, grad_scale: float, ws: torch.Tensor, expert_ids: Optional[torch.Tensor] = None,
+                        out: Optional[RouterOutputs] = None) -> RouterOutputs:
+    """rlhf_router_loss_fwd_bwd on [L,B,T,E] router logits (bf16, fp16 or fp32).  The k experts of a token are `expert_ids`
+    ([L,B,T,k] int32, -1: none) or, without them, its k largest logits, which `out.ids` then holds; `scoring` is ROUTER_SOFTMAX or
+    ROUTER_SIGMOID, `scope` ROUTER_BATCH or ROUTER_SEQUENCE."""
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor (the library has no CPU path)")
+    if logits.dtype not in SHAPED_DTYPES:
+        raise TypeError(f"logits must be bfloat16, float16 or float32, got {logits.dtype}")
+    if logits.dim() != 4 or (logits.shape[3] > 1 and logits.stride(3) != 1):
+        raise ValueError("logits must be [L,B,T,E] with a contiguous expert axis")
+    L, B, T, E = logits.shape
+    dev = logits.get_device()
+    if out is None:
+        out = RouterOutputs(logits, k, scope, want_ids=expert_ids is None)
+    if out.dlogits.dtype is not logits.dtype:
+        raise TypeError("out.dlogits must have the element type of logits")
+    if out.dlogits.shape != logits.shape or (E > 1 and out.dlogits.stride(3) != 1):
+        raise ValueError("out.dlogits must have the shape of logits and a contiguous expert axis")
+    _same_device(out.dlogits, dev, "out.dlogits")
+    given, gs = None, (0, 0, 0)
+    if expert_ids is not None:
+        _dev(expert_ids, torch.int32, "expert_ids")
+        _same_device(expert_ids, dev, "expert_ids")
+        if expert_ids.shape != (L, B, T, k) or (k > 1 and expert_ids.stride(3) != 1):
+            raise ValueError(f"expert_ids must be [{L},{B},{T},{k}] with a contiguous last axis")
+        given, gs = expert_ids.data_ptr(), expert_ids.stride()[:3]
+    counts = (L, B, E) if scope == ROUTER_SEQUENCE else (L, E)
+    _call("rlhf_router_loss_fwd_bwd", dev, logits.data_ptr(), SHAPED_DTYPES[logits.dtype], *logits.stride()[:3], given, *gs,
+          _arg(lengths, (B,), torch.int32, dev, "lengths"), L, B, T, E, k, scoring, scope, balance_coef, z_coef, grad_scale,
+          _arg(out.loss, (L, 2), _F32, dev, "out.loss"), _arg(out.counts, counts, torch.int32, dev, "out.counts"),
+          _opt(out.ids, (L, B, T, k), torch.int32, dev, "out.ids"), out.dlogits.data_ptr(), *out.dlogits.stride()[:3],
+          *_ws(ws, dev))
     return out

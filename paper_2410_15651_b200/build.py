@@ -17,7 +17,7 @@ LIB = os.path.join(PKG, "librlhf_ppo.so")
 NVCC_FLAGS = [
     "-std=c++17", "-O3", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+    "-Xcompiler", "-fPIC", "-cudart", "static",
 ]
 
 
@@ -37,19 +37,31 @@ def stale() -> bool:
     return any(os.path.getmtime(f) > t for f in _inputs())
 
 
+def _run(commands, verbose: bool) -> None:
+    running = [(c, subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for c in commands]
+    for (c, p), out in zip(running, [p.communicate()[0] for _, p in running]):
+        if p.returncode != 0 or verbose:
+            sys.stderr.write(out)
+        if p.returncode != 0:
+            raise RuntimeError("nvcc failed: " + " ".join(c))
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile csrc/*.cu into librlhf_ppo.so beside this file; returns its path."""
     if not force and not stale():
         return LIB
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     tmp = LIB + f".{os.getpid()}.tmp"
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + sources()
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("nvcc failed: " + " ".join(cmd))
-    if verbose:
-        sys.stderr.write(res.stdout + res.stderr)
+    objects = [f"{tmp}.{os.path.basename(f)}.o" for f in sources()]
+    try:
+        # the sources at the same time, then one link
+        _run([[nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", o, f]
+              for o, f in zip(objects, sources())], verbose)
+        _run([[nvcc] + NVCC_FLAGS + ["-shared", "-o", tmp] + objects], verbose)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     os.replace(tmp, LIB)
     return LIB
 

@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "host.cuh"
 #include "kernels_generic.cuh"
 #include "kernels_ring.cuh"
 #include "kernels_creg.cuh"
@@ -24,120 +25,13 @@ namespace {
 
 using namespace rlhf;
 
-thread_local char g_cuda_error[256] = "";
-
-int cuda_fail(cudaError_t e, const char* what)
-{
-    snprintf(g_cuda_error, sizeof g_cuda_error, "%s: %s", what, cudaGetErrorString(e));
-    return RLHF_ERR_CUDA;
-}
-
-#define RLHF_CUDA(call)                                   \
-    do {                                                  \
-        cudaError_t e_ = (call);                          \
-        if (e_ != cudaSuccess) return cuda_fail(e_, #call); \
-    } while (0)
-
-// Workspace layout (bytes): [0,4) status flags, [4,8) reduction ticket, [8,16) mean and 1/std of the
-// advantage whitening, [16,20) row counter of the kernels that deal their rows dynamically, [256, kRowLossOffset) block
-// partial sums of the two losses (2 doubles per block of the kernel that reduces them),
-// [kRowLossOffset, +4*B*T) per-token policy loss terms (kernels without the fused finalisation), then, for the objectives
-// beside step 4, 8*B*T bytes more: per-token KL terms (policy loss with KL); the factor of each sequence and, from
-// 4*B*T on, the loss of each pair (preference loss).
-constexpr size_t kPartialsOffset = 256;
-constexpr size_t kRowLossOffset = 24576;
-constexpr int kMaxFusedBlocks = (int)((kRowLossOffset - kPartialsOffset) / 16);   // block partials that fit the header
-
-constexpr long long kMaxTokens = 1ll << 29;
 static_assert(RLHF_TOPK_MAX == kTopkMax && RLHF_TOPK_MAX == kDistillMax, "the public bound and the kernels' agree");
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-int check_shape(int B, int T, int V)
-{
-    if (B <= 0 || T <= 0 || V <= 0) return RLHF_ERR_SHAPE;
-    // the log-prob kernel walks up to 2*B*T rows (two tensors in one launch) plus one grid stride with 32-bit
-    // indices, so B*T stays at or below 2^29
-    if ((long long)B * (long long)T > kMaxTokens) return RLHF_ERR_SHAPE;
-    return RLHF_OK;
-}
-
-// Bytes of the workspace that rlhf_ppo_loss_fwd_bwd touches: header + per-token policy loss terms.
-size_t loss_workspace_bytes(int B, int T) { return kRowLossOffset + 4 * (size_t)B * (size_t)T; }
-
-// Bytes that the other objectives touch.
-size_t objective_workspace_bytes(int B, int T) { return kRowLossOffset + 12 * (size_t)B * (size_t)T; }
-
-int check_workspace(const void* ws, size_t bytes, size_t need)
-{
-    if (!ws) return RLHF_ERR_NULL;
-    if (!aligned(ws, 256)) return RLHF_ERR_ALIGN;
-    if (bytes < need) return RLHF_ERR_WORKSPACE;
-    return RLHF_OK;
-}
-
-struct DeviceInfo {
-    int sm_count = 0;
-    int max_smem_optin = 0;     // per block
-    int smem_per_sm = 0;
-};
-
-// Queried per call: the library keeps no state, and the two attributes are cheap to read.
-int device_info(DeviceInfo& d)
-{
-    int dev = 0;
-    RLHF_CUDA(cudaGetDevice(&dev));
-    RLHF_CUDA(cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, dev));
-    RLHF_CUDA(cudaDeviceGetAttribute(&d.max_smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev));
-    RLHF_CUDA(cudaDeviceGetAttribute(&d.smem_per_sm, cudaDevAttrMaxSharedMemoryPerMultiprocessor, dev));
-    return RLHF_OK;
-}
 
 // Rows can take the 16-byte path if every row starts on a 16-byte boundary and is a whole number
 // of 16-byte vectors long.
 bool rows_16B(const void* base, long long stride_b, long long stride_t, int V)
 {
     return aligned(base, 16) && (stride_b % 8) == 0 && (stride_t % 8) == 0 && (V % 8) == 0;
-}
-
-// Launches `kernel` with programmatic stream serialisation allowed (see pdl_wait_prior_grid): the launch
-// itself and the kernel's set-up overlap the tail of the kernel before it in the stream.
-// `cluster` > 1 launches the grid as thread-block clusters of that many blocks.
-void fill_launch_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int grid, int block, size_t smem,
-                        int cluster, cudaStream_t s)
-{
-    cfg = cudaLaunchConfig_t{};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3((unsigned)block);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cluster > 1) {
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)cluster;
-        attr[1].val.clusterDim.y = 1;
-        attr[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
-    }
-}
-
-template <typename... Params, typename... Args>
-cudaError_t launch_kernel_cluster(void (*kernel)(Params...), int grid, int block, size_t smem, int cluster,
-                                  cudaStream_t s, Args&&... args)
-{
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    fill_launch_config(cfg, attr, grid, block, smem, cluster, s);
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
-}
-
-template <typename... Params, typename... Args>
-cudaError_t launch_kernel(void (*kernel)(Params...), int grid, int block, size_t smem, cudaStream_t s, Args&&... args)
-{
-    return launch_kernel_cluster(kernel, grid, block, smem, 1, s, static_cast<Args&&>(args)...);
 }
 
 template <int NW, int U>
@@ -437,16 +331,6 @@ int launch_loss_rows(const RowArgs& a, bool f16, const DeviceInfo& dev, cudaStre
     return launch_ring_as<8, 2>(ra, pl, grid, s);
 }
 
-// The row kernels run with the largest shared-memory carve-out.  A kernel that prefers another
-// split makes the SMs switch configuration before and after it, which costs microseconds per
-// launch; so the small kernels between them ask for the same carve-out.
-template <typename K>
-int keep_max_carveout(K kernel)
-{
-    RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
-    return RLHF_OK;
-}
-
 // What every call that reads logits and writes their gradient checks of the two tensors and the token ids.
 int check_rows(const void* logits, int logits_dtype, long long stride_b, long long stride_t, long long ids_stride_b,
                int B, int T, int V, const void* out_dlogits, long long dl_stride_b, long long dl_stride_t)
@@ -461,9 +345,6 @@ int check_rows(const void* logits, int logits_dtype, long long stride_b, long lo
     if (!aligned(logits, 2) || !aligned(out_dlogits, 2)) return RLHF_ERR_ALIGN;
     return RLHF_OK;
 }
-
-// Temperatures whose square is a number in fp32, and that leave logits of 1e6 below 1e9.  (NaN is none.)
-bool temperature_ok(float t) { return t >= 1e-3f && t <= 1e18f; }
 
 // The two [B,T] fp32 arrays share bytes (null: they do not).
 bool overlap(const float* a, const float* b, int B, int T)
@@ -505,13 +386,6 @@ int check_loss_args(const void* logits, long long stride_b, long long stride_t, 
         !aligned(returns, 4) || !aligned(out_loss_pg, 4) || !aligned(out_loss_vf, 4) ||
         !aligned(out_dvalues, 4) || (out_lp_new && !aligned(out_lp_new, 4)))
         return RLHF_ERR_ALIGN;
-    return RLHF_OK;
-}
-
-int launch_check(const char* what)
-{
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(e, what);
     return RLHF_OK;
 }
 
@@ -688,8 +562,8 @@ const char* rlhf_status_string(int status)
         case RLHF_ERR_TOO_LARGE: return "RLHF_ERR_TOO_LARGE";
         default: break;
     }
-    if (status > 0 && (status & ~(RLHF_ERR_ID_RANGE | RLHF_ERR_LENGTH_RANGE | RLHF_ERR_TIMEOUT)) == 0) {
-        static const char* const names[8] = {
+    if (status > 0 && (status & ~(RLHF_ERR_ID_RANGE | RLHF_ERR_LENGTH_RANGE | RLHF_ERR_TIMEOUT | RLHF_ERR_VALUE_RANGE)) == 0) {
+        static const char* const names[16] = {
             "RLHF_OK",
             "RLHF_ERR_ID_RANGE",
             "RLHF_ERR_LENGTH_RANGE",
@@ -698,8 +572,16 @@ const char* rlhf_status_string(int status)
             "RLHF_ERR_ID_RANGE|RLHF_ERR_TIMEOUT",
             "RLHF_ERR_LENGTH_RANGE|RLHF_ERR_TIMEOUT",
             "RLHF_ERR_ID_RANGE|RLHF_ERR_LENGTH_RANGE|RLHF_ERR_TIMEOUT",
+            "RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_ID_RANGE|RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_LENGTH_RANGE|RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_ID_RANGE|RLHF_ERR_LENGTH_RANGE|RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_TIMEOUT|RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_ID_RANGE|RLHF_ERR_TIMEOUT|RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_LENGTH_RANGE|RLHF_ERR_TIMEOUT|RLHF_ERR_VALUE_RANGE",
+            "RLHF_ERR_ID_RANGE|RLHF_ERR_LENGTH_RANGE|RLHF_ERR_TIMEOUT|RLHF_ERR_VALUE_RANGE",
         };
-        return names[(status >> 4) & 7];
+        return names[(status >> 4) & 15];
     }
     return "RLHF_ERR_UNKNOWN";
 }

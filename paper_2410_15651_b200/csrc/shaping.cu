@@ -1,0 +1,252 @@
+// Entry points of the operators on shaped logits: argument checks and launches.
+#include <algorithm>
+
+#include "common.cuh"
+#include "host.cuh"
+#include "kernels_shaping.cuh"
+
+namespace {
+
+using namespace rlhf;
+
+// The shaping's arguments into the kernel's form.
+int check_shaping(const rlhf_shaping_t* sh, ShapingArgs& out)
+{
+    if (!sh) return RLHF_ERR_NULL;
+    if (sh->prompt_len < 0 || sh->tokens_len < 0) return RLHF_ERR_SHAPE;
+    if ((sh->prompt_len > 0 && !sh->prompt) || (sh->tokens_len > 0 && !sh->tokens)) return RLHF_ERR_NULL;
+    if (sh->prompt_stride_b < 0 || sh->tokens_stride_b < 0 || sh->bias_stride_b < 0 || sh->mask_stride_b < 0 ||
+        sh->mask_stride_t < 0)
+        return RLHF_ERR_STRIDE;
+    if (!aligned(sh->prompt, 8) || !aligned(sh->tokens, 8) || !aligned(sh->prompt_lengths, 4) || !aligned(sh->start, 4) ||
+        !aligned(sh->repetition, 4) || !aligned(sh->frequency, 4) || !aligned(sh->presence, 4) ||
+        !aligned(sh->temperature, 4) || !aligned(sh->bias, 4) || !aligned(sh->mask, 4))
+        return RLHF_ERR_ALIGN;
+    out.tokens = sh->tokens_len > 0 ? sh->tokens : nullptr;
+    out.tokens_stride_b = sh->tokens_stride_b;
+    out.S = sh->tokens_len;
+    out.start = sh->start;
+    out.prompt = sh->prompt;
+    out.prompt_stride_b = sh->prompt_stride_b;
+    out.prompt_lengths = sh->prompt_len > 0 ? sh->prompt_lengths : nullptr;
+    out.P = sh->prompt_len;
+    out.repetition = sh->repetition;
+    out.frequency = sh->frequency;
+    out.presence = sh->presence;
+    out.temperature = sh->temperature;
+    out.bias = sh->bias;
+    out.bias_stride_b = sh->bias_stride_b;
+    out.mask = sh->mask;
+    out.mask_stride_b = sh->mask_stride_b;
+    out.mask_stride_t = sh->mask_stride_t;
+    return RLHF_OK;
+}
+
+// Rows that are read: strides in elements.
+int check_read_rows(const void* rows, long long sb, long long st, int T, int V)
+{
+    if (sb < 0 || st < 0 || (T > 1 && st < V)) return RLHF_ERR_STRIDE;
+    return aligned(rows, 2) ? RLHF_OK : RLHF_ERR_ALIGN;
+}
+
+// Rows that are written: none overlaps another.
+int check_written_rows(const void* rows, size_t size, long long sb, long long st, int B, int T, int V)
+{
+    if (sb < 0 || st < 0 || (T > 1 && st < V)) return RLHF_ERR_STRIDE;
+    if (B > 1 && sb < (T > 1 ? (long long)(T - 1) * st : 0) + V) return RLHF_ERR_STRIDE;
+    return aligned(rows, size) ? RLHF_OK : RLHF_ERR_ALIGN;
+}
+
+int check_common(int dtype, const int* lengths, int B, int T, int V, const void* ws, size_t ws_bytes)
+{
+    if (dtype != RLHF_BF16 && dtype != RLHF_F16) return RLHF_ERR_SCALAR;
+    if (int e = check_shape(B, T, V)) return e;
+    if (!aligned(lengths, 4)) return RLHF_ERR_ALIGN;
+    return check_workspace(ws, ws_bytes, objective_workspace_bytes(B, T));
+}
+
+// Rows whose 16-byte blocks all start at a multiple of 16 bytes from the row (an axis of one position has no stride).
+bool rows_aligned(const void* base, size_t size, long long sb, long long st, int B, int T)
+{
+    const long long per = (long long)(16 / size);
+    return aligned(base, 16) && (B == 1 || sb % per == 0) && (T == 1 || st % per == 0);
+}
+
+template <int kMode, bool kF16, bool kAny>
+int launch_shaping_as(const ShapeKernelArgs& a, int grid, int threads, size_t smem, cudaStream_t s)
+{
+    auto kernel = shaping_kernel<kMode, kF16, kAny>;
+    RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (int e = keep_max_carveout(kernel)) return e;
+    RLHF_CUDA(launch_kernel_cluster(kernel, grid, threads, smem, kMode == kShapeLp ? a.cluster : 1, s, a));
+    return launch_check("shaping_kernel");
+}
+
+template <int kMode>
+int launch_shaping(ShapeKernelArgs& a, bool f16, bool any, cudaStream_t s)
+{
+    DeviceInfo dev;
+    if (int e = device_info(dev)) return e;
+    const int vecs = (a.V + (any ? 14 : 7)) / 8;           // most vectors that hold a row's entries
+    a.n_slices = (vecs + kShapeSliceVecs - 1) / kShapeSliceVecs;
+    a.slice_vecs = (vecs + a.n_slices - 1) / a.n_slices;
+    // log-probs: a row's slices meet in a cluster; what does not fit one is taken in turns
+    a.cluster = kMode == kShapeLp ? std::min(a.n_slices, kShapeMaxCluster) : a.n_slices;
+    const int threads = std::min(kShapeThreads, std::max(64, (a.slice_vecs + 31) / 32 * 32));
+    // rows of a segment: as many as leave every SM a few blocks
+    const long long rows = (long long)a.B * a.T;
+    const long long want = rows * a.cluster / ((long long)dev.sm_count * 8);
+    a.rows_per_item = (int)std::min<long long>({kShapeMaxRows, a.T, std::max<long long>(1, want)});
+    const long long segments = (a.T + a.rows_per_item - 1) / a.rows_per_item;
+    const long long grid = segments * a.B * a.cluster;
+    if (grid > 0x7fffffffll) return RLHF_ERR_SHAPE;
+
+    a.uses_counts = a.sh.tokens && (a.sh.frequency || a.sh.presence) && kMode != kShapeBwd;
+    a.uses_history = (a.sh.repetition && (a.sh.tokens || a.sh.P > 0)) || a.uses_counts;
+    const int entries = a.slice_vecs * 8 + (any ? 16 : 0);
+    a.bits_words = a.uses_history ? ((entries >> 5) + 2 + 3) / 4 * 4 : 0;
+    const size_t smem = 4 * (size_t)a.bits_words + (a.uses_counts ? 4 * (size_t)entries : 0);
+    if (any)
+        return f16 ? launch_shaping_as<kMode, true, true>(a, (int)grid, threads, smem, s)
+                   : launch_shaping_as<kMode, false, true>(a, (int)grid, threads, smem, s);
+    return f16 ? launch_shaping_as<kMode, true, false>(a, (int)grid, threads, smem, s)
+               : launch_shaping_as<kMode, false, false>(a, (int)grid, threads, smem, s);
+}
+
+// Nothing but penalties: outside the history a row is what it was.
+bool only_history(const ShapingArgs& sh) { return !sh.bias && !sh.mask && !sh.temperature; }
+
+}  // namespace
+
+extern "C" {
+
+int rlhf_shape_logits(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                      const rlhf_shaping_t* shaping, const int* lengths, int B, int T, int V,
+                      void* out, int out_dtype, long long out_stride_b, long long out_stride_t,
+                      void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !lengths || !out) return RLHF_ERR_NULL;
+    ShapeKernelArgs a{};
+    if (int e = check_shaping(shaping, a.sh)) return e;
+    if (int e = check_common(logits_dtype, lengths, B, T, V, workspace, workspace_bytes)) return e;
+    if (out_dtype != logits_dtype && out_dtype != RLHF_F32) return RLHF_ERR_SCALAR;
+    const size_t size = out_dtype == RLHF_F32 ? 4 : 2;
+    if (int e = check_read_rows(logits, stride_b, stride_t, T, V)) return e;
+    if (int e = check_written_rows(out, size, out_stride_b, out_stride_t, B, T, V)) return e;
+    if (out == logits && (size != 2 || (B > 1 && out_stride_b != stride_b) || (T > 1 && out_stride_t != stride_t)))
+        return RLHF_ERR_STRIDE;
+    a.src = (const uint16_t*)logits;
+    a.src_stride_b = stride_b;
+    a.src_stride_t = stride_t;
+    a.dst = out;
+    a.dst_stride_b = out_stride_b;
+    a.dst_stride_t = out_stride_t;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.status = (unsigned*)workspace;
+    a.sparse = out == logits && only_history(a.sh);
+    const bool any = !rows_aligned(logits, 2, stride_b, stride_t, B, T) || !rows_aligned(out, size, out_stride_b, out_stride_t, B, T);
+    return size == 4 ? launch_shaping<kShape32>(a, logits_dtype == RLHF_F16, any, (cudaStream_t)stream)
+                     : launch_shaping<kShape16>(a, logits_dtype == RLHF_F16, any, (cudaStream_t)stream);
+}
+
+int rlhf_shape_logits_bwd(const void* dshaped, int logits_dtype, long long ds_stride_b, long long ds_stride_t,
+                          const void* logits, long long stride_b, long long stride_t,
+                          const rlhf_shaping_t* shaping, const int* lengths, int B, int T, int V,
+                          void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                          void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!dshaped || !logits || !lengths || !out_dlogits) return RLHF_ERR_NULL;
+    ShapeKernelArgs a{};
+    if (int e = check_shaping(shaping, a.sh)) return e;
+    if (int e = check_common(logits_dtype, lengths, B, T, V, workspace, workspace_bytes)) return e;
+    if (int e = check_read_rows(dshaped, ds_stride_b, ds_stride_t, T, V)) return e;
+    if (int e = check_read_rows(logits, stride_b, stride_t, T, V)) return e;
+    if (int e = check_written_rows(out_dlogits, 2, dl_stride_b, dl_stride_t, B, T, V)) return e;
+    if (out_dlogits == logits) return RLHF_ERR_STRIDE;
+    if (out_dlogits == dshaped && ((B > 1 && dl_stride_b != ds_stride_b) || (T > 1 && dl_stride_t != ds_stride_t)))
+        return RLHF_ERR_STRIDE;
+    a.src = (const uint16_t*)dshaped;
+    a.src_stride_b = ds_stride_b;
+    a.src_stride_t = ds_stride_t;
+    a.logits = (const uint16_t*)logits;
+    a.logits_stride_b = stride_b;
+    a.logits_stride_t = stride_t;
+    a.dst = out_dlogits;
+    a.dst_stride_b = dl_stride_b;
+    a.dst_stride_t = dl_stride_t;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.status = (unsigned*)workspace;
+    a.sparse = out_dlogits == dshaped && !a.sh.mask && !a.sh.temperature;
+    const bool any = !rows_aligned(dshaped, 2, ds_stride_b, ds_stride_t, B, T) || !rows_aligned(out_dlogits, 2, dl_stride_b, dl_stride_t, B, T);
+    return launch_shaping<kShapeBwd>(a, logits_dtype == RLHF_F16, any, (cudaStream_t)stream);
+}
+
+int rlhf_shaped_logprobs(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                         const long long* ids, long long ids_stride_b, const rlhf_shaping_t* shaping, const int* lengths,
+                         int B, int T, int V, float* out_logprobs, float* out_lse, float* out_entropy,
+                         void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !ids || !lengths || !out_logprobs || !out_lse) return RLHF_ERR_NULL;
+    ShapeKernelArgs a{};
+    if (int e = check_shaping(shaping, a.sh)) return e;
+    if (int e = check_common(logits_dtype, lengths, B, T, V, workspace, workspace_bytes)) return e;
+    if (int e = check_read_rows(logits, stride_b, stride_t, T, V)) return e;
+    if (ids_stride_b < 0) return RLHF_ERR_STRIDE;
+    if (!aligned(ids, 8) || !aligned(out_logprobs, 4) || !aligned(out_lse, 8) || !aligned(out_entropy, 4)) return RLHF_ERR_ALIGN;
+    a.src = (const uint16_t*)logits;
+    a.src_stride_b = stride_b;
+    a.src_stride_t = stride_t;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.ids = ids;
+    a.ids_stride_b = ids_stride_b;
+    a.out_lp = out_logprobs;
+    a.out_lse = out_lse;
+    a.out_entropy = out_entropy;
+    a.status = (unsigned*)workspace;
+    const bool any = !rows_aligned(logits, 2, stride_b, stride_t, B, T);
+    return launch_shaping<kShapeLp>(a, logits_dtype == RLHF_F16, any, (cudaStream_t)stream);
+}
+
+int rlhf_shaped_logprobs_bwd(const void* logits, int logits_dtype, long long stride_b, long long stride_t,
+                             const long long* ids, long long ids_stride_b, const rlhf_shaping_t* shaping, const int* lengths,
+                             int B, int T, int V, const float* logprobs, const float* lse, const float* entropy,
+                             const float* grad_logprobs, const float* grad_entropy,
+                             void* out_dlogits, long long dl_stride_b, long long dl_stride_t,
+                             void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!logits || !ids || !lengths || !logprobs || !lse || !grad_logprobs || !out_dlogits) return RLHF_ERR_NULL;
+    if (grad_entropy && !entropy) return RLHF_ERR_NULL;
+    ShapeKernelArgs a{};
+    if (int e = check_shaping(shaping, a.sh)) return e;
+    if (int e = check_common(logits_dtype, lengths, B, T, V, workspace, workspace_bytes)) return e;
+    if (int e = check_read_rows(logits, stride_b, stride_t, T, V)) return e;
+    if (int e = check_written_rows(out_dlogits, 2, dl_stride_b, dl_stride_t, B, T, V)) return e;
+    if (ids_stride_b < 0) return RLHF_ERR_STRIDE;
+    if (out_dlogits == logits && ((B > 1 && dl_stride_b != stride_b) || (T > 1 && dl_stride_t != stride_t))) return RLHF_ERR_STRIDE;
+    if (!aligned(ids, 8) || !aligned(logprobs, 4) || !aligned(lse, 8) || !aligned(entropy, 4) || !aligned(grad_logprobs, 4) ||
+        !aligned(grad_entropy, 4))
+        return RLHF_ERR_ALIGN;
+    a.src = (const uint16_t*)logits;
+    a.src_stride_b = stride_b;
+    a.src_stride_t = stride_t;
+    a.dst = out_dlogits;
+    a.dst_stride_b = dl_stride_b;
+    a.dst_stride_t = dl_stride_t;
+    a.lengths = lengths;
+    a.B = B; a.T = T; a.V = V;
+    a.ids = ids;
+    a.ids_stride_b = ids_stride_b;
+    a.lp = logprobs;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.grad_lp = grad_logprobs;
+    a.grad_entropy = grad_entropy;
+    a.status = (unsigned*)workspace;
+    const bool any = !rows_aligned(logits, 2, stride_b, stride_t, B, T) || !rows_aligned(out_dlogits, 2, dl_stride_b, dl_stride_t, B, T);
+    return launch_shaping<kShapeLpBwd>(a, logits_dtype == RLHF_F16, any, (cudaStream_t)stream);
+}
+
+}  // extern "C"
