@@ -1,5 +1,6 @@
 // Entry points of the operators on shaped logits: argument checks and launches.
 #include <algorithm>
+#include <mutex>
 
 #include "common.cuh"
 #include "host.cuh"
@@ -72,45 +73,91 @@ bool rows_aligned(const void* base, size_t size, long long sb, long long st, int
     return aligned(base, 16) && (B == 1 || sb % per == 0) && (T == 1 || st % per == 0);
 }
 
+// Blocks (clusters) of the kernel that the device holds at once: they only size the grid.  The answer for the last kernel and
+// shape is kept.
+template <typename K>
+int resident_units(K kernel, int cluster, int threads, size_t smem, const DeviceInfo& dev, int& out)
+{
+    static std::mutex mu;
+    static K of = nullptr;
+    static long long key = -1;
+    static int value = 0;
+    int d = 0;
+    RLHF_CUDA(cudaGetDevice(&d));
+    const long long k = (((long long)d * 16 + cluster) * 2048 + threads) * 262144 + (long long)smem;
+    std::lock_guard<std::mutex> lock(mu);
+    if (kernel != of || k != key) {
+        int n = 0;
+        if (cluster > 1) {
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            fill_launch_config(cfg, attr, dev.sm_count / cluster * cluster, threads, smem, cluster, nullptr);
+            RLHF_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+        } else {
+            RLHF_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem));
+            n *= dev.sm_count;
+        }
+        value = std::max(n, 1);
+        of = kernel;
+        key = k;
+    }
+    out = value;
+    return RLHF_OK;
+}
+
 template <int kMode, bool kF16, bool kAny>
-int launch_shaping_as(const ShapeKernelArgs& a, int grid, int threads, size_t smem, cudaStream_t s)
+int launch_shaping_as(ShapeKernelArgs& a, int warps, const DeviceInfo& dev, cudaStream_t s)
 {
     auto kernel = shaping_kernel<kMode, kF16, kAny>;
+    const size_t smem = shape_smem(a, warps, kAny).total;
     RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (int e = keep_max_carveout(kernel)) return e;
-    RLHF_CUDA(launch_kernel_cluster(kernel, grid, threads, smem, kMode == kShapeLp ? a.cluster : 1, s, a));
+    // a block per row where the rows are few or the sequences short; else as many blocks as the device holds, each with an equal
+    // share of the valid rows
+    const long long items = (long long)a.B * a.T * (kMode == kShapeLp ? 1 : a.n_slices);
+    int units = 0;
+    if (int e = resident_units(kernel, a.cluster, warps * 32, smem, dev, units)) return e;
+    a.direct = a.T < kShapeDirectRows || items <= units;
+    const long long grid = (a.direct ? items : units) * a.cluster;
+    if (grid > 0x7fffffffll) return RLHF_ERR_SHAPE;
+    RLHF_CUDA(launch_kernel_cluster(kernel, (int)grid, warps * 32, smem, a.cluster, s, a));
     return launch_check("shaping_kernel");
 }
 
+// Cuts a row into slices and segments.  Few rows are cut finer, so that they reach every SM.
 template <int kMode>
 int launch_shaping(ShapeKernelArgs& a, bool f16, bool any, cudaStream_t s)
 {
     DeviceInfo dev;
     if (int e = device_info(dev)) return e;
     const int vecs = (a.V + (any ? 14 : 7)) / 8;           // most vectors that hold a row's entries
-    a.n_slices = (vecs + kShapeSliceVecs - 1) / kShapeSliceVecs;
-    a.slice_vecs = (vecs + a.n_slices - 1) / a.n_slices;
-    // log-probs: a row's slices meet in a cluster; what does not fit one is taken in turns
-    a.cluster = kMode == kShapeLp ? std::min(a.n_slices, kShapeMaxCluster) : a.n_slices;
-    const int threads = std::min(kShapeThreads, std::max(64, (a.slice_vecs + 31) / 32 * 32));
-    // rows of a segment: as many as leave every SM a few blocks
     const long long rows = (long long)a.B * a.T;
-    const long long want = rows * a.cluster / ((long long)dev.sm_count * 8);
-    a.rows_per_item = (int)std::min<long long>({kShapeMaxRows, a.T, std::max<long long>(1, want)});
-    const long long segments = (a.T + a.rows_per_item - 1) / a.rows_per_item;
-    const long long grid = segments * a.B * a.cluster;
-    if (grid > 0x7fffffffll) return RLHF_ERR_SHAPE;
-
+    a.wait_limit_ns = kWaitLimitNs;
     a.uses_counts = a.sh.tokens && (a.sh.frequency || a.sh.presence) && kMode != kShapeBwd;
     a.uses_history = (a.sh.repetition && (a.sh.tokens || a.sh.P > 0)) || a.uses_counts;
-    const int entries = a.slice_vecs * 8 + (any ? 16 : 0);
-    a.bits_words = a.uses_history ? ((entries >> 5) + 2 + 3) / 4 * 4 : 0;
-    const size_t smem = 4 * (size_t)a.bits_words + (a.uses_counts ? 4 * (size_t)entries : 0);
+    a.wide_counts = a.sh.S > 65535;
+    const long long history = a.uses_history ? (long long)a.sh.P + a.sh.S : 0;
+    const bool short_rows = a.T < kShapeDirectRows;
+    const int warps = short_rows ? 8 : kShapeWarps;
+    const size_t room = short_rows ? 48 * 1024 : (size_t)dev.max_smem_optin - 10 * 1024;
+    const int most = short_rows ? 128 : kShapeSegment;
+    a.n_slices = 1;
+    for (;; ++a.n_slices) {
+        a.segment = (vecs + a.n_slices * warps - 1) / (a.n_slices * warps);
+        if (a.segment > most) continue;
+        if (a.segment > 32 && rows * a.n_slices < dev.sm_count && (kMode != kShapeLp || a.n_slices < kShapeMaxCluster)) continue;
+        const int entries = a.segment * warps * 8 + (any ? 16 : 0);
+        a.bits_words = a.uses_history ? (entries / 32 + 2 + 3) / 4 * 4 : 0;
+        a.list_cap = (int)((std::min<long long>(history, entries) + 15) / 16 * 16);
+        for (a.n_bufs = short_rows ? 1 : kShapeMaxBufs; a.n_bufs > 0 && shape_smem(a, warps, any).total > room; --a.n_bufs) {}
+        if (a.n_bufs >= std::min(a.T, short_rows ? 1 : 3) || (a.n_bufs > 0 && a.segment <= 8)) break;
+        if (a.segment <= 8) return RLHF_ERR_SHAPE;         // (not reached: the table of such a slice is small)
+    }
+    // log-probs: a row's slices meet in a cluster; what does not fit one is taken in turns
+    a.cluster = kMode == kShapeLp ? std::min(a.n_slices, kShapeMaxCluster) : 1;
     if (any)
-        return f16 ? launch_shaping_as<kMode, true, true>(a, (int)grid, threads, smem, s)
-                   : launch_shaping_as<kMode, false, true>(a, (int)grid, threads, smem, s);
-    return f16 ? launch_shaping_as<kMode, true, false>(a, (int)grid, threads, smem, s)
-               : launch_shaping_as<kMode, false, false>(a, (int)grid, threads, smem, s);
+        return f16 ? launch_shaping_as<kMode, true, true>(a, warps, dev, s) : launch_shaping_as<kMode, false, true>(a, warps, dev, s);
+    return f16 ? launch_shaping_as<kMode, true, false>(a, warps, dev, s) : launch_shaping_as<kMode, false, false>(a, warps, dev, s);
 }
 
 // Nothing but penalties: outside the history a row is what it was.
