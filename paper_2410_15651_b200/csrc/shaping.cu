@@ -112,51 +112,83 @@ int launch_shaping_as(ShapeKernelArgs& a, int warps, const DeviceInfo& dev, cuda
     const size_t smem = shape_smem(a, warps, kAny).total;
     RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (int e = keep_max_carveout(kernel)) return e;
-    // a block per row where the rows are few or the sequences short; else as many blocks as the device holds, each with an equal
-    // share of the valid rows
+    // as many blocks as the device holds, each with an equal share of the valid rows (log-probs of few rows: a cluster per row)
     const long long items = (long long)a.B * a.T * (kMode == kShapeLp ? 1 : a.n_slices);
     int units = 0;
     if (int e = resident_units(kernel, a.cluster, warps * 32, smem, dev, units)) return e;
-    a.direct = a.T < kShapeDirectRows || items <= units;
-    const long long grid = (a.direct ? items : units) * a.cluster;
+    a.direct = kMode == kShapeLp && (a.T < kShapeShortRows || items <= units);
+    const long long grid = (a.direct ? items : std::min<long long>(items, units)) * a.cluster;
     if (grid > 0x7fffffffll) return RLHF_ERR_SHAPE;
     RLHF_CUDA(launch_kernel_cluster(kernel, (int)grid, warps * 32, smem, a.cluster, s, a));
     return launch_check("shaping_kernel");
 }
 
-// Cuts a row into slices and segments.  Few rows are cut finer, so that they reach every SM.
+template <int kMode, bool kF16, bool kAny>
+int launch_shaping_rows_as(const ShapeKernelArgs& a, cudaStream_t s)
+{
+    auto kernel = shaping_row_kernel<kMode, kF16, kAny>;
+    const size_t smem = shape_row_smem(a, kAny);
+    RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (int e = keep_max_carveout(kernel)) return e;
+    const long long grid = (long long)a.B * a.T * a.n_slices;
+    if (grid > 0x7fffffffll) return RLHF_ERR_SHAPE;
+    RLHF_CUDA(launch_kernel(kernel, (int)grid, kRowThreads, smem, s, a));
+    return launch_check("shaping_row_kernel");
+}
+
+// Words of the bit table and places of the list for a slice of so many entries.
+void size_table(ShapeKernelArgs& a, int entries, bool bits)
+{
+    const long long history = a.uses_history ? (long long)a.sh.P + a.sh.S : 0;
+    a.bits_words = a.uses_history || bits ? (entries / 32 + 2 + 3) / 4 * 4 : 0;
+    a.list_cap = (int)((std::min<long long>(history, entries) + 1 + 15) / 16 * 16);
+}
+
+// Cuts a row into slices and segments, and chooses the kernel.
 template <int kMode>
 int launch_shaping(ShapeKernelArgs& a, bool f16, bool any, cudaStream_t s)
 {
     DeviceInfo dev;
     if (int e = device_info(dev)) return e;
+    constexpr bool kLp = kMode == kShapeLp;
     const int vecs = (a.V + (any ? 14 : 7)) / 8;           // most vectors that hold a row's entries
     const long long rows = (long long)a.B * a.T;
     a.wait_limit_ns = kWaitLimitNs;
     a.uses_counts = a.sh.tokens && (a.sh.frequency || a.sh.presence) && kMode != kShapeBwd;
     a.uses_history = (a.sh.repetition && (a.sh.tokens || a.sh.P > 0)) || a.uses_counts;
     a.wide_counts = a.sh.S > 65535;
-    const long long history = a.uses_history ? (long long)a.sh.P + a.sh.S : 0;
-    const bool short_rows = a.T < kShapeDirectRows;
-    const int warps = short_rows ? 8 : kShapeWarps;
-    const size_t room = short_rows ? 48 * 1024 : (size_t)dev.max_smem_optin - 10 * 1024;
-    const int most = short_rows ? 128 : kShapeSegment;
-    a.n_slices = 1;
-    for (;; ++a.n_slices) {
-        a.segment = (vecs + a.n_slices * warps - 1) / (a.n_slices * warps);
-        if (a.segment > most) continue;
-        if (a.segment > 32 && rows * a.n_slices < dev.sm_count && (kMode != kShapeLp || a.n_slices < kShapeMaxCluster)) continue;
-        const int entries = a.segment * warps * 8 + (any ? 16 : 0);
-        a.bits_words = a.uses_history ? (entries / 32 + 2 + 3) / 4 * 4 : 0;
-        a.list_cap = (int)((std::min<long long>(history, entries) + 15) / 16 * 16);
-        for (a.n_bufs = short_rows ? 1 : kShapeMaxBufs; a.n_bufs > 0 && shape_smem(a, warps, any).total > room; --a.n_bufs) {}
-        if (a.n_bufs >= std::min(a.T, short_rows ? 1 : 3) || (a.n_bufs > 0 && a.segment <= 8)) break;
-        if (a.segment <= 8) return RLHF_ERR_SHAPE;         // (not reached: the table of such a slice is small)
+    a.cluster = 1;
+
+    if constexpr (!kLp) {
+        // short sequences, and batches of at most four blocks per SM
+        constexpr int kMost = kRowThreads * kRowVecs;
+        const int slices = (vecs + kMost - 1) / kMost;
+        if (a.T < kShapeShortRows || rows * slices <= 4ll * dev.sm_count) {
+            a.n_slices = slices;
+            while (rows * a.n_slices < 2ll * dev.sm_count && vecs / a.n_slices > kRowThreads) ++a.n_slices;
+            a.segment = (vecs + a.n_slices - 1) / a.n_slices;
+            size_table(a, a.segment * 8 + (any ? 16 : 0), false);
+            if (any) return f16 ? launch_shaping_rows_as<kMode, true, true>(a, s) : launch_shaping_rows_as<kMode, false, true>(a, s);
+            return f16 ? launch_shaping_rows_as<kMode, true, false>(a, s) : launch_shaping_rows_as<kMode, false, false>(a, s);
+        }
+    }
+    // Segments of whole turns of a warp, with two buffers at least.  Log-probs of few rows are cut finer, so that they reach every SM.
+    constexpr int kTurn = kLp ? 64 : 32;
+    const size_t room = (size_t)dev.max_smem_optin - 12 * 1024;
+    int warps = 0;
+    for (a.n_slices = 1;; ++a.n_slices) {
+        const int per = (vecs + a.n_slices - 1) / a.n_slices;
+        a.segment = ((per + kShapeWarps - 1) / kShapeWarps + kTurn - 1) / kTurn * kTurn;
+        warps = std::max(2, (per + a.segment - 1) / a.segment);
+        if (a.segment > kShapeSegment) continue;
+        if (kLp && a.segment > kTurn && rows * a.n_slices < dev.sm_count && a.n_slices < kShapeMaxCluster) continue;
+        size_table(a, a.segment * warps * 8 + (any ? 16 : 0), kLp);
+        for (a.n_bufs = kShapeMaxBufs; a.n_bufs > 0 && shape_smem(a, warps, any).total > room; --a.n_bufs) {}
+        if (a.n_bufs >= std::min(a.T, 2)) break;
     }
     // log-probs: a row's slices meet in a cluster; what does not fit one is taken in turns
-    a.cluster = kMode == kShapeLp ? std::min(a.n_slices, kShapeMaxCluster) : 1;
-    if (any)
-        return f16 ? launch_shaping_as<kMode, true, true>(a, warps, dev, s) : launch_shaping_as<kMode, false, true>(a, warps, dev, s);
+    if (kLp) a.cluster = std::min(a.n_slices, kShapeMaxCluster);
+    if (any) return f16 ? launch_shaping_as<kMode, true, true>(a, warps, dev, s) : launch_shaping_as<kMode, false, true>(a, warps, dev, s);
     return f16 ? launch_shaping_as<kMode, true, false>(a, warps, dev, s) : launch_shaping_as<kMode, false, false>(a, warps, dev, s);
 }
 

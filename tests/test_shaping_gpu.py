@@ -133,6 +133,22 @@ def test_sizes(B, T, V, dtype):
     everything(B, T, V, dtype, ALL + ("mask_rows", "bias"), V + T, P=9, S0=5)
 
 
+# batches that are walked down sequence by sequence: several rows per block, several slices per row, rows that a cluster takes in
+# turns, more than 32 rows between two tokens' tables, many listed entries
+WALKS = [(6, 64, 50272, ALL, {}), (6, 64, 50272, ALL + ("mask_rows",), {}), (5, 70, 50257, ALL + ("mask",), {}),
+         (4, 80, 32000, ("repetition", "tokens", "prompt"), {}), (3, 50, 128256, ALL + ("bias_own",), {}), (3, 40, 151643, ALL, {}),
+         (2, 40, 400000, ALL, {}), (30, 40, 6000, ALL + ("mask_rows", "bias"), {}), (4, 40, 50257, ALL, dict(pitch=47)),
+         (4, 40, 40003, ALL + ("mask_rows",), dict(pitch=5, offset=3)), (40, 40, 1000, ("presence", "tokens", "mask"), {}), (4, 100, 20000, (), {})]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("B,T,V,parts,layout", WALKS)
+def test_walks(B, T, V, parts, layout, dtype):
+    if V == 400000 and dtype == HF:
+        B, V = 1, 280000
+    everything(B, T, V, dtype, parts, V + T, P=200, S0=100 if V % 2 else 0, repeat=300, layout=layout, density=0.9)
+
+
 @pytest.mark.parametrize("parts", [(), ("temperature",), ("bias",), ("bias_own",), ("mask",), ("mask_rows",), ("repetition", "prompt"),
                                    ("repetition", "tokens"), ("frequency", "tokens"), ("presence", "tokens"), ("repetition",),
                                    ("tokens", "prompt"), ("presence", "prompt"), ("frequency", "tokens", "prompt", "mask"),
@@ -167,14 +183,20 @@ def test_long_answers_of_one_token():
               frequency=torch.full((B,), 1e-4, device=DEV))
     ws = lib.workspace(B, T, DEV)
     got = check_shape(z, torch.full((B,), T, dtype=torch.int32, device=DEV), kw, ws, dtype=torch.float32)
+    B2, T2 = 40, 40                                      # the same in a batch that is walked down
+    y, _ = row_logits(B2, T2, V, BF, gen, DEV)
+    many = dict(tokens=torch.full((B2, S0 + T2), 5, device=DEV), start=torch.full((B2,), S0, dtype=torch.int32, device=DEV),
+                frequency=torch.full((B2,), 1e-4, device=DEV))
+    check_shape(y, torch.full((B2,), T2, dtype=torch.int32, device=DEV), many, lib.workspace(B2, T2, DEV), dtype=torch.float32)
+    check_logprobs(y, torch.full((B2, T2), 5, device=DEV), torch.full((B2,), T2, dtype=torch.int32, device=DEV), many, lib.workspace(B2, T2, DEV))
     assert abs(got[0, 0, 5].item() - (z[0, 0, 5].item() - 7.0)) < 1e-4 and lib.poll_status(ws) == 0
 
 
-@pytest.mark.parametrize("V", [3000, 3001])
+@pytest.mark.parametrize("B,T", [(4, 5), (40, 40)])
+@pytest.mark.parametrize("V", [2000, 2001])
 @pytest.mark.parametrize("parts", [ALL[:-1], ALL + ("mask",)], ids=["penalties", "dense"])
-def test_in_place(V, parts):
+def test_in_place(V, parts, B, T):
     """Everything that may be written over its input, with nothing else touched."""
-    B, T = 4, 5
     gen = torch.Generator(device=DEV).manual_seed(V)
     kw = ref.Settings(B, T, V, gen, DEV, parts, P=6).kw
     lengths, ws = mixed_lengths(B, T), lib.workspace(B, T, DEV)
