@@ -804,16 +804,24 @@ def router_workspace(L: int, B: int, T: int, E: int, device) -> torch.Tensor:
     return ws
 
 
+def _router_logits(t: torch.Tensor) -> None:
+    """Says what is wrong with router logits."""
+    if not t.is_cuda:
+        raise ValueError("logits must be a CUDA tensor (the library has no CPU path)")
+    if t.dtype not in SHAPED_DTYPES:
+        raise TypeError(f"logits must be bfloat16, float16 or float32, got {t.dtype}")
+    raise ValueError("logits must be [L,B,T,E] with a contiguous expert axis")
+
+
 class RouterOutputs:
     """Buffers written by router_loss_fwd_bwd; reusable from call to call."""
 
     def __init__(self, logits: torch.Tensor, k: int, scope: int, in_place: bool = False, want_ids: bool = True):
         L, B, T, E = logits.shape
-        new = lambda dtype, *n: logits.new_empty(n, dtype=dtype)  # noqa: E731
-        self.loss = new(_F32, L, 2)                                                  # [balance, z-loss] of every layer
-        self.counts = new(torch.int32, L, B, E) if scope == ROUTER_SEQUENCE else new(torch.int32, L, E)
+        self.loss = logits.new_empty((L, 2), dtype=_F32)                             # [balance, z-loss] of every layer
+        self.counts = logits.new_empty((L, B, E) if scope == ROUTER_SEQUENCE else (L, E), dtype=torch.int32)
         self.dlogits = logits if in_place else _like(logits)
-        self.ids = new(torch.int32, L, B, T, max(k, 0)) if want_ids else None
+        self.ids = logits.new_empty((L, B, T, max(k, 0)), dtype=torch.int32) if want_ids else None
 
 
 def router_loss_fwd_bwd(logits: torch.Tensor, lengths: torch.Tensor, k: int, scoring: int, scope: int, balance_coef: float,
@@ -822,32 +830,33 @@ def router_loss_fwd_bwd(logits: torch.Tensor, lengths: torch.Tensor, k: int, sco
     """rlhf_router_loss_fwd_bwd on [L,B,T,E] router logits (bf16, fp16 or fp32).  The k experts of a token are `expert_ids`
     ([L,B,T,k] int32, -1: none) or, without them, its k largest logits, which `out.ids` then holds; `scoring` is ROUTER_SOFTMAX or
     ROUTER_SIGMOID, `scope` ROUTER_BATCH or ROUTER_SEQUENCE."""
-    if not logits.is_cuda:
-        raise ValueError("logits must be a CUDA tensor (the library has no CPU path)")
-    if logits.dtype not in SHAPED_DTYPES:
-        raise TypeError(f"logits must be bfloat16, float16 or float32, got {logits.dtype}")
-    if logits.dim() != 4 or (logits.shape[3] > 1 and logits.stride(3) != 1):
-        raise ValueError("logits must be [L,B,T,E] with a contiguous expert axis")
+    if logits.dtype not in SHAPED_DTYPES or not logits.is_cuda or logits.dim() != 4:
+        _router_logits(logits)
     L, B, T, E = logits.shape
+    sl, sb, st, se = logits.stride()
+    if se != 1 and E > 1:
+        _router_logits(logits)
     dev = logits.get_device()
     if out is None:
         out = RouterOutputs(logits, k, scope, want_ids=expert_ids is None)
-    if out.dlogits.dtype is not logits.dtype:
+    d = out.dlogits
+    if d.dtype is not logits.dtype:
         raise TypeError("out.dlogits must have the element type of logits")
-    if out.dlogits.shape != logits.shape or (E > 1 and out.dlogits.stride(3) != 1):
+    dl, db, dt, de = d.stride()
+    if d.shape != logits.shape or (E > 1 and de != 1):
         raise ValueError("out.dlogits must have the shape of logits and a contiguous expert axis")
-    _same_device(out.dlogits, dev, "out.dlogits")
-    given, gs = None, (0, 0, 0)
+    _same_device(d, dev, "out.dlogits")
+    given, gl, gb, gt = None, 0, 0, 0
     if expert_ids is not None:
         _dev(expert_ids, torch.int32, "expert_ids")
         _same_device(expert_ids, dev, "expert_ids")
         if expert_ids.shape != (L, B, T, k) or (k > 1 and expert_ids.stride(3) != 1):
             raise ValueError(f"expert_ids must be [{L},{B},{T},{k}] with a contiguous last axis")
-        given, gs = expert_ids.data_ptr(), expert_ids.stride()[:3]
-    counts = (L, B, E) if scope == ROUTER_SEQUENCE else (L, E)
-    _call("rlhf_router_loss_fwd_bwd", dev, logits.data_ptr(), SHAPED_DTYPES[logits.dtype], *logits.stride()[:3], given, *gs,
+        given = expert_ids.data_ptr()
+        gl, gb, gt, _ = expert_ids.stride()
+    _call("rlhf_router_loss_fwd_bwd", dev, logits.data_ptr(), SHAPED_DTYPES[logits.dtype], sl, sb, st, given, gl, gb, gt,
           _arg(lengths, (B,), torch.int32, dev, "lengths"), L, B, T, E, k, scoring, scope, balance_coef, z_coef, grad_scale,
-          _arg(out.loss, (L, 2), _F32, dev, "out.loss"), _arg(out.counts, counts, torch.int32, dev, "out.counts"),
-          _opt(out.ids, (L, B, T, k), torch.int32, dev, "out.ids"), out.dlogits.data_ptr(), *out.dlogits.stride()[:3],
-          *_ws(ws, dev))
+          _arg(out.loss, (L, 2), _F32, dev, "out.loss"),
+          _arg(out.counts, (L, B, E) if scope == ROUTER_SEQUENCE else (L, E), torch.int32, dev, "out.counts"),
+          _opt(out.ids, (L, B, T, k), torch.int32, dev, "out.ids"), d.data_ptr(), dl, db, dt, *_ws(ws, dev))
     return out

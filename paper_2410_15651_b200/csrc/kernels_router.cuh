@@ -42,9 +42,8 @@ struct RouterArgs {
     unsigned* ticket;
     int* partial_counts;                     // [groups][n_partials][E]
     double* partial_loss;                    // [blocks][2]
-    int groups, n_chunks, n_partials, chunk_rows;
+    int groups, n_chunks, n_partials;
     int cluster;                             // blocks of the counting kernel that share a partial count
-    int lanes, per_lane;                     // G, and entries of a lane
     int vec_in, vec_out;                     // rows can be moved in 16-byte pieces
 };
 
@@ -54,27 +53,41 @@ template <> struct RouterEl<0> { using T = uint16_t; static __device__ __forcein
 template <> struct RouterEl<1> { using T = uint16_t; static __device__ __forceinline__ float get(uint16_t v) { return El<true>::widen(v); } };
 template <> struct RouterEl<2> { using T = float; static __device__ __forceinline__ float get(float v) { return v; } };
 
-// Which tokens a block has: rows [r0, r1) of group g.  A row is (b, t).
+// Which tokens a block has: of group g the rows (a row is (b, t)) in turns of `turn` rows, every n_chunks-th of them, so that
+// padding is shared out.
 struct RouterItem {
-    int g, l, r0, r1, b0;                    // b0: the sequence of a per-sequence group
+    int g, l, chunk, rows, b0;               // b0: the sequence of a per-sequence group
 };
 
 __device__ __forceinline__ RouterItem router_item(const RouterArgs& a, int block)
 {
     RouterItem it;
     it.g = block / a.n_chunks;
-    const int chunk = block % a.n_chunks, rows = a.per_sequence ? a.T : a.B * a.T;
+    it.chunk = block % a.n_chunks;
+    it.rows = a.per_sequence ? a.T : a.B * a.T;
     it.l = a.per_sequence ? it.g / a.B : it.g;
     it.b0 = a.per_sequence ? it.g % a.B : 0;
-    it.r0 = (int)min((long long)chunk * a.chunk_rows, (long long)rows);
-    it.r1 = (int)min((long long)it.r0 + a.chunk_rows, (long long)rows);
     return it;
 }
 
-__device__ __forceinline__ void router_row(const RouterArgs& a, const RouterItem& it, int r, int& b, int& t)
+// Row r of an item, its sequence and token, and whether it is a token of the sequence.
+struct RouterRow {
+    int b, t;
+    bool row, valid;
+};
+__device__ __forceinline__ RouterRow router_row(const RouterArgs& a, const RouterItem& it, long long r)
 {
-    if (a.per_sequence) { b = it.b0; t = r; }
-    else { b = r / a.T; t = r - b * a.T; }
+    RouterRow w{0, 0, r < it.rows, false};
+    if (!w.row) return w;
+    if (a.per_sequence) {
+        w.b = it.b0;
+        w.t = (int)r;
+    } else {
+        w.b = (int)((unsigned)r / (unsigned)a.T);
+        w.t = (int)r - w.b * a.T;
+    }
+    w.valid = w.t < __ldg(a.lengths + w.b);
+    return w;
 }
 
 // Entries e0 .. e0 + 8 NV - 1 of a row; `missing` past E.
@@ -143,8 +156,16 @@ __device__ __forceinline__ uint32_t router_key(float z)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Lanes of a token.
+__host__ __device__ constexpr int router_lanes(int E, int nv)
+{
+    int g = 1;
+    while (g * 8 * nv < E) g *= 2;
+    return g;
+}
+
 // ---------------------------------------------------------------- counts
-template <int kType, int NV>
+template <int kType, int NV, int G>
 __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __grid_constant__ RouterArgs a)
 {
     using Ty = typename RouterEl<kType>::T;
@@ -165,60 +186,122 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
     if (a.ids_in) {
         bool bad = false;
         const int* base = a.ids_in + (long long)it.l * a.ids_stride_l;
-        for (int r = it.r0 + tid; r < it.r1; r += kRouterThreads) {
-            int b, t;
-            router_row(a, it, r, b, t);
-            if (t >= __ldg(a.lengths + b)) continue;
-            const int* ids = base + (long long)b * a.ids_stride_b + (long long)t * a.ids_stride_t;
-            for (int k = 0; k < a.K; ++k) {
-                const int e = __ldg(ids + k);
+        const long long choices = (long long)kRouterThreads * a.K;     // of a turn, a choice per thread
+        for (long long r0 = (long long)it.chunk * kRouterThreads; r0 < it.rows; r0 += (long long)a.n_chunks * kRouterThreads)
+            for (long long i = tid; i < choices; i += kRouterThreads) {
+                const int row = (int)i / a.K, k = (int)i - row * a.K;
+                const RouterRow w = router_row(a, it, r0 + row);
+                if (!w.valid) continue;
+                const int e = __ldg(base + (long long)w.b * a.ids_stride_b + (long long)w.t * a.ids_stride_t + k);
                 if (e >= 0 && e < a.E) atomicAdd(s_count + e, 1);
                 else if (e != -1) bad = true;
             }
-        }
         if (bad) atomicOr(a.status, kErrIdRange);
     } else {
-        const int G = a.lanes, sub = lane & (G - 1), per_warp = 32 / G;
-        const int e0 = sub * 8 * NV;
-        const uint32_t group = (G == 32 ? 0xffffffffu : ((1u << G) - 1u)) << (lane & ~(G - 1));
-        const int step = kRouterThreads / 32 * per_warp;
+        // 16-bit logits of one vector per lane: a key orders logit and expert at once (the higher logit, then the lower expert).  A
+        // lane sorts its eight, and every turn takes the largest head.  Else a turn looks for the largest of all.
+        constexpr bool kSorted = sizeof(Ty) == 2 && NV == 1;
+        constexpr int kPerWarp = 32 / G, kTurn = kRouterThreads / 32 * kPerWarp;
+        const int sub = lane & (G - 1), e0 = sub * 8 * NV;
+        const uint32_t group = (G == 32 ? 0xffffffffu : ((1u << (G & 31)) - 1u)) << (lane & ~(G - 1));
+        const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l;
+        const int mine = warp * kPerWarp + lane / G;
+        const long long step = (long long)a.n_chunks * kTurn;
+        long long r = (long long)it.chunk * kTurn;
+        RouterRow w = router_row(a, it, r + mine);
+        float z[8 * NV];
+        auto load = [&]() {
+            if (w.valid) router_load<kType, NV>(base + (long long)w.b * a.stride_b + (long long)w.t * a.stride_t, e0, a.E, a.vec_in, 0.f, z);
+        };
+        load();
         // (every lane of a warp makes every turn: the shuffles want them all)
-        for (int r = it.r0 + warp * per_warp; r < it.r1; r += step) {
-            const int mine = r + lane / G;
-            int b = 0, t = 0;
-            bool row = mine < it.r1, valid = false;
-            if (row) {
-                router_row(a, it, mine, b, t);
-                valid = t < __ldg(a.lengths + b);
-            }
+        for (; r < it.rows; r += step) {
+            const bool row = w.row, valid = w.valid;
+            int* const out = a.out_ids && row ? a.out_ids + (((long long)it.l * a.B + w.b) * a.T + w.t) * a.K : nullptr;
             uint32_t key[8 * NV];
-            if (valid) {
-                float z[8 * NV];
-                router_load<kType, NV>((const Ty*)a.logits + (long long)it.l * a.stride_l + (long long)b * a.stride_b + (long long)t * a.stride_t,
-                                       e0, a.E, a.vec_in, 0.f, z);
 #pragma unroll
-                for (int j = 0; j < 8 * NV; ++j) key[j] = e0 + j < a.E ? router_key(z[j]) : 0u;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8 * NV; ++j) key[j] = 0u;
+            for (int j = 0; j < 8 * NV; ++j) {
+                key[j] = valid && e0 + j < a.E ? router_key(z[j]) : 0u;
+                // (the low 13 bits of a 16-bit logit's key say nothing, and there are at most 256 experts)
+                if (kSorted && key[j]) key[j] = (max(key[j], 0x100u) & 0xffffff00u) | (0xffu - (uint32_t)(e0 + j));
             }
-            int* out = a.out_ids ? a.out_ids + (((long long)it.l * a.B + b) * a.T + t) * a.K : nullptr;
-            for (int k = 0; k < a.K; ++k) {
-                uint32_t top = key[0];
-                int at = 0;
+            w = router_row(a, it, r + step + mine);
+            load();                                      // in flight meanwhile
+            if (__ballot_sync(0xffffffffu, valid) == 0u) {             // (rows of padding)
+                if (out)
+                    for (int k = sub; k < a.K; k += G) out[k] = 0;
+                continue;
+            }
+            if constexpr (kSorted) {
+                auto order = [&](int x, int y) {         // the larger first
+                    const uint32_t hi = max(key[x], key[y]), lo = min(key[x], key[y]);
+                    key[x] = hi;
+                    key[y] = lo;
+                };
+                // Batcher's odd-even merge of eight
+                order(0, 1); order(2, 3); order(4, 5); order(6, 7);
+                order(0, 2); order(1, 3); order(4, 6); order(5, 7);
+                order(1, 2); order(5, 6);
+                order(0, 4); order(1, 5); order(2, 6); order(3, 7);
+                order(2, 4); order(3, 5);
+                order(1, 2); order(3, 4); order(5, 6);
+                auto top = [&]() {
+                    uint32_t best = key[0];
 #pragma unroll
-                for (int j = 1; j < 8 * NV; ++j)
-                    if (key[j] > top) { top = key[j]; at = j; }
-                uint32_t best = top;
-                for (int o = G >> 1; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-                const uint32_t who = __ballot_sync(0xffffffffu, top == best) & group;
-                if (lane == __ffs(who) - 1) {            // the lowest expert of those that are equal
-                    const int e = min(e0 + at, a.E - 1);
-                    if (valid) atomicAdd(s_count + e, 1);
-                    if (out && row) out[k] = valid ? e : 0;
+                    for (int o = G / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+                    return best;
+                };
+                if (G >= 8 && a.K <= 8) {                // lane k of a token keeps its k-th choice
+                    uint32_t got = 0u;
 #pragma unroll
-                    for (int j = 0; j < 8 * NV; ++j)
-                        if (j == at) key[j] = 0u;
+                    for (int k = 0; k < 8; ++k) {
+                        if (k >= a.K) break;
+                        const uint32_t best = top();
+                        const bool won = key[0] == best;
+                        if (sub == k) got = best;
+#pragma unroll
+                        for (int j = 0; j < 7 - k; ++j) key[j] = won ? key[j + 1] : key[j];
+                    }
+                    if (sub < a.K) {
+                        const int e = got ? 0xff - (int)(got & 0xffu) : 0;
+                        if (got) atomicAdd(s_count + e, 1);
+                        if (out) out[sub] = e;
+                    }
+                } else {
+                    for (int k = 0; k < a.K; ++k) {
+                        const uint32_t best = top();
+                        if (key[0] == best && best != 0u) {
+#pragma unroll
+                            for (int j = 0; j < 7; ++j) key[j] = key[j + 1];
+                            key[7] = 0u;
+                            const int e = 0xff - (int)(best & 0xffu);
+                            atomicAdd(s_count + e, 1);
+                            if (out) out[k] = e;
+                        }
+                        if (out && best == 0u && sub == 0) out[k] = 0;
+                    }
+                }
+            } else {
+                for (int k = 0; k < a.K; ++k) {
+                    uint32_t top = key[0];
+#pragma unroll
+                    for (int j = 1; j < 8 * NV; ++j) top = max(top, key[j]);
+                    uint32_t best = top;
+#pragma unroll
+                    for (int o = G / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+                    const uint32_t who = __ballot_sync(0xffffffffu, top == best) & group;
+                    if (lane == __ffs(who) - 1) {        // the lowest expert of those that are equal
+                        int at = 0;
+#pragma unroll
+                        for (int j = 8 * NV - 1; j >= 0; --j)
+                            if (key[j] == best) at = j;
+#pragma unroll
+                        for (int j = 0; j < 8 * NV; ++j)
+                            if (j == at) key[j] = 0u;
+                        const int e = min(e0 + at, a.E - 1);
+                        if (valid) atomicAdd(s_count + e, 1);
+                        if (out) out[k] = valid ? e : 0;
+                    }
                 }
             }
         }
@@ -251,7 +334,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
 }
 
 // ---------------------------------------------------------------- losses and gradient
-template <int kType, int NV>
+template <int kType, int NV, int G>
 __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __grid_constant__ RouterArgs a)
 {
     using Ty = typename RouterEl<kType>::T;
@@ -280,75 +363,104 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
 
     const double wd = n > 0 ? 1.0 / ((double)n * (double)filled) : 0.0, zd = N > 0 ? 1.0 / (double)N : 0.0;
     const float wb = (float)((double)a.grad_scale * a.balance_coef * wd), wz = (float)((double)a.grad_scale * a.z_coef * 2.0 * zd);
-    const int G = a.lanes, sub = lane & (G - 1), per_warp = 32 / G;
-    const int e0 = sub * 8 * NV;
-    const int step = kRouterThreads / 32 * per_warp;
-    double sum_b = 0.0, sum_z = 0.0;
-    for (int r = it.r0 + warp * per_warp; r < it.r1; r += step) {
-        const int mine = r + lane / G;
-        int b = 0, t = 0;
-        const bool row = mine < it.r1;
-        bool valid = false;
-        if (row) {
-            router_row(a, it, mine, b, t);
-            valid = t < __ldg(a.lengths + b);
-        }
-        float p[8 * NV], slope[8 * NV];
-        if (valid)
-            router_load<kType, NV>((const Ty*)a.logits + (long long)it.l * a.stride_l + (long long)b * a.stride_b + (long long)t * a.stride_t,
-                                   e0, a.E, a.vec_in, -INFINITY, p);
-        else {
+    constexpr int kPerWarp = 32 / G, kTurn = kRouterThreads / 32 * kPerWarp;
+    const int sub = lane & (G - 1), e0 = sub * 8 * NV;
+    const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l;
+    Ty* const dbase = (Ty*)a.dlogits + (long long)it.l * a.dl_stride_l;
+    const bool with_z = a.z_coef != 0.f;
+    float2 f[4 * NV];                                    // the lane's experts are the same of every token
 #pragma unroll
-            for (int j = 0; j < 8 * NV; ++j) p[j] = -INFINITY;
-        }
-        float m = 0.f, total = 0.f, dot = 0.f;
-        if (a.scoring == kRouterSoftmax) {
-            m = p[0];
-#pragma unroll
-            for (int j = 1; j < 8 * NV; ++j) m = fmaxf(m, p[j]);
-            for (int o = G >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            if (m == -INFINITY) m = 0.f;                 // (no token, or one that may not choose: p = 0)
-#pragma unroll
-            for (int j = 0; j < 8 * NV; ++j) p[j] = ex2((p[j] - m) * kLog2e);
+    for (int j = 0; j < 4 * NV; ++j)
+        f[j] = make_float2(e0 + 2 * j < a.E ? s_f[e0 + 2 * j] : 0.f, e0 + 2 * j + 1 < a.E ? s_f[e0 + 2 * j + 1] : 0.f);
+    // sums of a block's tokens: a lane has some tens of them, added in fp32, then in double
+    float sum_dot = 0.f, sum_lse = 0.f;
+    int tokens = 0;
+    const int mine = warp * kPerWarp + lane / G;
+    const long long step = (long long)a.n_chunks * kTurn;
+    long long r = (long long)it.chunk * kTurn;
+    RouterRow w = router_row(a, it, r + mine);
+    float z[8 * NV];
+    auto load = [&]() {                                  // (a row that is no token has p = 0)
+        if (w.valid) {
+            router_load<kType, NV>(base + (long long)w.b * a.stride_b + (long long)w.t * a.stride_t, e0, a.E, a.vec_in, -INFINITY, z);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8 * NV; ++j) {
-                const float e = ex2(-fabsf(p[j]) * kLog2e), inv = 1.f / (1.f + e);
-                slope[j] = p[j] >= 0.f ? e * inv : inv;
-                p[j] = p[j] >= 0.f ? inv : e * inv;
+            for (int j = 0; j < 8 * NV; ++j) z[j] = -INFINITY;
+        }
+    };
+    load();
+    for (; r < it.rows; r += step) {
+        const bool row = w.row, valid = w.valid;
+        Ty* const dst = dbase + (long long)w.b * a.dl_stride_b + (long long)w.t * a.dl_stride_t;
+        float2 p[4 * NV], slope[4 * NV];
+#pragma unroll
+        for (int j = 0; j < 4 * NV; ++j) p[j] = make_float2(z[2 * j], z[2 * j + 1]);
+        w = router_row(a, it, r + step + mine);
+        load();                                          // in flight meanwhile
+        float m = 0.f;
+        if (a.scoring == kRouterSoftmax) {
+            m = fmaxf(p[0].x, p[0].y);
+#pragma unroll
+            for (int j = 1; j < 4 * NV; ++j) m = fmaxf(m, fmaxf(p[j].x, p[j].y));
+#pragma unroll
+            for (int o = G / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if (m == -INFINITY) m = 0.f;                 // (no token, or one that may choose no expert)
+#pragma unroll
+            for (int j = 0; j < 4 * NV; ++j) {
+                const float2 y = __fmul2_rn(__fadd2_rn(p[j], splat2(-m)), splat2(kLog2e));
+                p[j] = make_float2(ex2(y.x), ex2(y.y));
+            }
+        } else {
+            auto one = [](float v, float& rise) {
+                const float e = ex2(-fabsf(v) * kLog2e), inv = __fdividef(1.f, 1.f + e);
+                rise = v >= 0.f ? e * inv : inv;
+                return v >= 0.f ? inv : e * inv;
+            };
+#pragma unroll
+            for (int j = 0; j < 4 * NV; ++j) {
+                p[j].x = one(p[j].x, slope[j].x);
+                p[j].y = one(p[j].y, slope[j].y);
             }
         }
+        float2 t2 = splat2(0.f), d2 = splat2(0.f);
 #pragma unroll
-        for (int j = 0; j < 8 * NV; ++j) {
-            total += p[j];
-            if (e0 + j < a.E) dot = fmaf(p[j], s_f[e0 + j], dot);
+        for (int j = 0; j < 4 * NV; ++j) {
+            t2 = __fadd2_rn(t2, p[j]);
+            d2 = __ffma2_rn(p[j], f[j], d2);
         }
-        for (int o = G >> 1; o > 0; o >>= 1) {
+        float total = t2.x + t2.y, dot = d2.x + d2.y;
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) {
             total += __shfl_xor_sync(0xffffffffu, total, o);
             dot += __shfl_xor_sync(0xffffffffu, dot, o);
         }
-        const float inv = total > 0.f ? 1.f / total : (total == 0.f ? 0.f : total);
+        const float inv = total > 0.f ? __fdividef(1.f, total) : total;            // (0 stays 0, NaN NaN)
         dot *= inv;
         float lse = 0.f;
-        if (a.scoring == kRouterSoftmax && total > 0.f) lse = m + logf(total);
+        if (with_z && total > 0.f) lse = m + logf(total);
         if (row) {
-            const float gz = a.z_coef != 0.f ? wz * lse : 0.f;
+            const float pb = inv * wb, gz = with_z ? inv * wz * lse : 0.f;
             float d[8 * NV];
 #pragma unroll
-            for (int j = 0; j < 8 * NV; ++j) {
-                const float f = e0 + j < a.E ? s_f[e0 + j] : 0.f;
-                float v = wb * (f - dot);
-                if (a.scoring == kRouterSigmoid) v *= slope[j];
-                d[j] = valid ? (p[j] * inv) * (v + gz) : 0.f;
+            for (int j = 0; j < 4 * NV; ++j) {
+                float2 v = __fadd2_rn(f[j], splat2(-dot));
+                if (a.scoring == kRouterSigmoid) v = __fmul2_rn(__fmul2_rn(v, slope[j]), splat2(pb));
+                else v = __ffma2_rn(v, splat2(pb), splat2(gz));
+                v = __fmul2_rn(v, p[j]);
+                d[2 * j] = v.x;
+                d[2 * j + 1] = v.y;
             }
-            router_store<kType, NV>((Ty*)a.dlogits + (long long)it.l * a.dl_stride_l + (long long)b * a.dl_stride_b + (long long)t * a.dl_stride_t,
-                                    e0, a.E, a.vec_out, d);
+            router_store<kType, NV>(dst, e0, a.E, a.vec_out, d);
         }
         if (valid && sub == 0) {
-            if (total != 0.f) sum_b += 1.0 + (double)dot;    // (0: a token that may choose no expert)
-            if (a.z_coef != 0.f) sum_z += (double)lse * (double)lse;
+            if (total != 0.f) {                          // (0: a token that may choose no expert)
+                sum_dot += dot;
+                ++tokens;
+            }
+            sum_lse = fmaf(lse, lse, sum_lse);
         }
     }
+    double sum_b = (double)tokens + (double)sum_dot, sum_z = (double)sum_lse;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         sum_b += __shfl_xor_sync(0xffffffffu, sum_b, o);

@@ -10,7 +10,7 @@ namespace {
 using namespace rlhf;
 
 struct RouterPlan {
-    long long groups = 0, n_chunks = 0, n_partials = 0, chunk_rows = 0;
+    long long groups = 0, n_chunks = 0, n_partials = 0;
     int cluster = 1;
 };
 
@@ -28,7 +28,6 @@ RouterPlan plan_router(int L, int B, int T, bool per_sequence)
         p.n_chunks = p.n_chunks / kRouterCluster * kRouterCluster;
     }
     p.n_partials = p.n_chunks / p.cluster;
-    p.chunk_rows = (rows + p.n_chunks - 1) / p.n_chunks;
     return p;
 }
 
@@ -44,26 +43,30 @@ bool router_shape_ok(int L, int B, int T, int E)
            (long long)L * ((long long)B * T) <= kMaxTokens;
 }
 
-template <int kType, int NV>
+template <int kType, int NV, int G>
 int launch_router_as(const RouterArgs& a, int grid, cudaStream_t s)
 {
-    if (int e = keep_max_carveout(router_count_kernel<kType, NV>)) return e;
-    RLHF_CUDA(launch_kernel_cluster(router_count_kernel<kType, NV>, grid, kRouterThreads, 0, a.cluster, s, a));
+    if (int e = keep_max_carveout(router_count_kernel<kType, NV, G>)) return e;
+    RLHF_CUDA(launch_kernel_cluster(router_count_kernel<kType, NV, G>, grid, kRouterThreads, 0, a.cluster, s, a));
     if (int e = launch_check("router_count_kernel")) return e;
-    if (int e = keep_max_carveout(router_loss_kernel<kType, NV>)) return e;
-    RLHF_CUDA(launch_kernel(router_loss_kernel<kType, NV>, grid, kRouterThreads, 0, s, a));
+    if (int e = keep_max_carveout(router_loss_kernel<kType, NV, G>)) return e;
+    RLHF_CUDA(launch_kernel(router_loss_kernel<kType, NV, G>, grid, kRouterThreads, 0, s, a));
     return launch_check("router_loss_kernel");
 }
 
 template <int kType>
 int launch_router(RouterArgs& a, int grid, cudaStream_t s)
 {
-    const int nv = a.E <= 256 ? 1 : (a.E <= 512 ? 2 : 4);
-    a.lanes = 1;
-    while (a.lanes * 8 * nv < a.E) a.lanes *= 2;
-    if (nv == 1) return launch_router_as<kType, 1>(a, grid, s);
-    if (nv == 2) return launch_router_as<kType, 2>(a, grid, s);
-    return launch_router_as<kType, 4>(a, grid, s);
+    if (a.E > 512) return launch_router_as<kType, 4, 32>(a, grid, s);
+    if (a.E > 256) return launch_router_as<kType, 2, 32>(a, grid, s);
+    switch (router_lanes(a.E, 1)) {
+        case 1: return launch_router_as<kType, 1, 1>(a, grid, s);
+        case 2: return launch_router_as<kType, 1, 2>(a, grid, s);
+        case 4: return launch_router_as<kType, 1, 4>(a, grid, s);
+        case 8: return launch_router_as<kType, 1, 8>(a, grid, s);
+        case 16: return launch_router_as<kType, 1, 16>(a, grid, s);
+        default: return launch_router_as<kType, 1, 32>(a, grid, s);
+    }
 }
 
 }  // namespace
@@ -144,7 +147,6 @@ int rlhf_router_loss_fwd_bwd(const void* logits, int logits_dtype, long long str
     a.groups = (int)p.groups;
     a.n_chunks = (int)p.n_chunks;
     a.n_partials = (int)p.n_partials;
-    a.chunk_rows = (int)p.chunk_rows;
     a.cluster = p.cluster;
     const long long per = (long long)(16 / size);
     auto vec = [&](const void* base, long long sl, long long sb, long long st) {
