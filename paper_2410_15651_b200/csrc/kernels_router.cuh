@@ -45,6 +45,9 @@ struct RouterArgs {
     int groups, n_chunks, n_partials;
     int cluster;                             // blocks of the counting kernel that share a partial count
     int vec_in, vec_out;                     // rows can be moved in 16-byte pieces
+    int flat_in, flat_out;                   // all rows of a layer follow each other at stride_t
+    unsigned t_magic;                        // for divisions by T
+    int t_shift;
 };
 
 // The element types: 16-bit as elsewhere, and fp32.
@@ -72,22 +75,25 @@ __device__ __forceinline__ RouterItem router_item(const RouterArgs& a, int block
 
 // Row r of an item, its sequence and token, and whether it is a token of the sequence.
 struct RouterRow {
-    int b, t;
+    int r, b, t;
     bool row, valid;
 };
-__device__ __forceinline__ RouterRow router_row(const RouterArgs& a, const RouterItem& it, long long r)
+__device__ __forceinline__ RouterRow router_row(const RouterArgs& a, const RouterItem& it, int r)
 {
-    RouterRow w{0, 0, r < it.rows, false};
+    RouterRow w{r, it.b0, r, r < it.rows, false};
     if (!w.row) return w;
-    if (a.per_sequence) {
-        w.b = it.b0;
-        w.t = (int)r;
-    } else {
-        w.b = (int)((unsigned)r / (unsigned)a.T);
-        w.t = (int)r - w.b * a.T;
+    if (!a.per_sequence) {
+        // r / T by a product with 2^(32 + shift) / T, rounded up: T <= 2^(shift + 1), so that it is exact for r < 2^31
+        w.b = a.T == 1 ? r : (int)(__umulhi((unsigned)r, a.t_magic) >> a.t_shift);
+        w.t = r - w.b * a.T;
     }
     w.valid = w.t < __ldg(a.lengths + w.b);
     return w;
+}
+// Its offset in a tensor; `flat`: its rows follow each other at stride_t.
+__device__ __forceinline__ long long router_at(const RouterRow& w, bool flat, long long stride_b, long long stride_t)
+{
+    return flat ? (long long)w.r * stride_t : (long long)w.b * stride_b + (long long)w.t * stride_t;
 }
 
 // Entries e0 .. e0 + 8 NV - 1 of a row; `missing` past E.
@@ -164,6 +170,16 @@ __host__ __device__ constexpr int router_lanes(int E, int nv)
     return g;
 }
 
+// Two 16-bit logits in the order of unsigned numbers, -0 as 0.
+template <bool kF16>
+__device__ __forceinline__ uint32_t router_order2(uint32_t w)
+{
+    if (kF16) asm("add.rn.f16x2 %0, %0, %1;" : "+r"(w) : "r"(0u));
+    else asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(w) : "r"(0u));
+    const uint32_t negative = ((w >> 15) & 0x00010001u) * 0xffffu;
+    return w ^ (negative | 0x80008000u);
+}
+
 // ---------------------------------------------------------------- counts
 template <int kType, int NV, int G>
 __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __grid_constant__ RouterArgs a)
@@ -186,10 +202,10 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
     if (a.ids_in) {
         bool bad = false;
         const int* base = a.ids_in + (long long)it.l * a.ids_stride_l;
-        const long long choices = (long long)kRouterThreads * a.K;     // of a turn, a choice per thread
-        for (long long r0 = (long long)it.chunk * kRouterThreads; r0 < it.rows; r0 += (long long)a.n_chunks * kRouterThreads)
-            for (long long i = tid; i < choices; i += kRouterThreads) {
-                const int row = (int)i / a.K, k = (int)i - row * a.K;
+        const int choices = kRouterThreads * a.K;        // of a turn, a choice per thread
+        for (int r0 = it.chunk * kRouterThreads; r0 < it.rows; r0 += a.n_chunks * kRouterThreads)
+            for (int i = tid; i < choices; i += kRouterThreads) {
+                const int row = i / a.K, k = i - row * a.K;
                 const RouterRow w = router_row(a, it, r0 + row);
                 if (!w.valid) continue;
                 const int e = __ldg(base + (long long)w.b * a.ids_stride_b + (long long)w.t * a.ids_stride_t + k);
@@ -204,26 +220,50 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
         constexpr int kPerWarp = 32 / G, kTurn = kRouterThreads / 32 * kPerWarp;
         const int sub = lane & (G - 1), e0 = sub * 8 * NV;
         const uint32_t group = (G == 32 ? 0xffffffffu : ((1u << (G & 31)) - 1u)) << (lane & ~(G - 1));
-        const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l;
+        const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l + (a.per_sequence && a.flat_in ? it.b0 * a.stride_b : 0);
+        int* const ids_base = a.out_ids + ((long long)it.l * a.B + it.b0) * a.T * a.K;
         const int mine = warp * kPerWarp + lane / G;
-        const long long step = (long long)a.n_chunks * kTurn;
-        long long r = (long long)it.chunk * kTurn;
+        const int step = a.n_chunks * kTurn;
+        int r = it.chunk * kTurn;
         RouterRow w = router_row(a, it, r + mine);
         float z[8 * NV];
+        uint4 q = make_uint4(0, 0, 0, 0);                // kSorted and vec_in: the lane's logits as they are
         auto load = [&]() {
-            if (w.valid) router_load<kType, NV>(base + (long long)w.b * a.stride_b + (long long)w.t * a.stride_t, e0, a.E, a.vec_in, 0.f, z);
+            if (!w.valid) return;
+            const Ty* row = base + router_at(w, a.flat_in, a.stride_b, a.stride_t);
+            if (kSorted && a.vec_in) {
+                if (e0 < a.E) q = __ldg((const uint4*)(row + e0));
+            } else {
+                router_load<kType, NV>(row, e0, a.E, a.vec_in, 0.f, z);
+            }
         };
         load();
         // (every lane of a warp makes every turn: the shuffles want them all)
         for (; r < it.rows; r += step) {
             const bool row = w.row, valid = w.valid;
-            int* const out = a.out_ids && row ? a.out_ids + (((long long)it.l * a.B + w.b) * a.T + w.t) * a.K : nullptr;
+            int* const out = a.out_ids && row ? ids_base + (long long)w.r * a.K : nullptr;
             uint32_t key[8 * NV];
+            if (kSorted && a.vec_in) {
+                if (valid && e0 < a.E) {
+                    const uint32_t x[4] = {router_order2<kType == 1>(q.x), router_order2<kType == 1>(q.y), router_order2<kType == 1>(q.z),
+                                           router_order2<kType == 1>(q.w)};
 #pragma unroll
-            for (int j = 0; j < 8 * NV; ++j) {
-                key[j] = valid && e0 + j < a.E ? router_key(z[j]) : 0u;
-                // (the low 13 bits of a 16-bit logit's key say nothing, and there are at most 256 experts)
-                if (kSorted && key[j]) key[j] = (max(key[j], 0x100u) & 0xffffff00u) | (0xffu - (uint32_t)(e0 + j));
+                    for (int j = 0; j < 4; ++j) {
+                        key[2 * j] = (x[j] << 16) + (0xffffu - (uint32_t)(e0 + 2 * j));
+                        key[2 * j + 1] = (x[j] & 0xffff0000u) | (0xffffu - (uint32_t)(e0 + 2 * j + 1));
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) key[j] = 0u;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8 * NV; ++j) {
+                    key[j] = valid && e0 + j < a.E ? router_key(z[j]) : 0u;
+                    // (the low 13 bits of a 16-bit logit's key say nothing, and there are at most 256 experts; the top bits of the low
+                    // half are the logit's in this form and 1 in the other)
+                    if (kSorted && key[j]) key[j] = (max(key[j], 0x100u) & 0xffffff00u) | (0xffu - (uint32_t)(e0 + j));
+                }
             }
             w = router_row(a, it, r + step + mine);
             load();                                      // in flight meanwhile
@@ -365,8 +405,8 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
     const float wb = (float)((double)a.grad_scale * a.balance_coef * wd), wz = (float)((double)a.grad_scale * a.z_coef * 2.0 * zd);
     constexpr int kPerWarp = 32 / G, kTurn = kRouterThreads / 32 * kPerWarp;
     const int sub = lane & (G - 1), e0 = sub * 8 * NV;
-    const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l;
-    Ty* const dbase = (Ty*)a.dlogits + (long long)it.l * a.dl_stride_l;
+    const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l + (a.per_sequence && a.flat_in ? it.b0 * a.stride_b : 0);
+    Ty* const dbase = (Ty*)a.dlogits + (long long)it.l * a.dl_stride_l + (a.per_sequence && a.flat_out ? it.b0 * a.dl_stride_b : 0);
     const bool with_z = a.z_coef != 0.f;
     float2 f[4 * NV];                                    // the lane's experts are the same of every token
 #pragma unroll
@@ -376,13 +416,13 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
     float sum_dot = 0.f, sum_lse = 0.f;
     int tokens = 0;
     const int mine = warp * kPerWarp + lane / G;
-    const long long step = (long long)a.n_chunks * kTurn;
-    long long r = (long long)it.chunk * kTurn;
+    const int step = a.n_chunks * kTurn;
+    int r = it.chunk * kTurn;
     RouterRow w = router_row(a, it, r + mine);
     float z[8 * NV];
     auto load = [&]() {                                  // (a row that is no token has p = 0)
         if (w.valid) {
-            router_load<kType, NV>(base + (long long)w.b * a.stride_b + (long long)w.t * a.stride_t, e0, a.E, a.vec_in, -INFINITY, z);
+            router_load<kType, NV>(base + router_at(w, a.flat_in, a.stride_b, a.stride_t), e0, a.E, a.vec_in, -INFINITY, z);
         } else {
 #pragma unroll
             for (int j = 0; j < 8 * NV; ++j) z[j] = -INFINITY;
@@ -391,7 +431,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
     load();
     for (; r < it.rows; r += step) {
         const bool row = w.row, valid = w.valid;
-        Ty* const dst = dbase + (long long)w.b * a.dl_stride_b + (long long)w.t * a.dl_stride_t;
+        Ty* const dst = dbase + router_at(w, a.flat_out, a.dl_stride_b, a.dl_stride_t);
         float2 p[4 * NV], slope[4 * NV];
 #pragma unroll
         for (int j = 0; j < 4 * NV; ++j) p[j] = make_float2(z[2 * j], z[2 * j + 1]);
@@ -437,7 +477,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
         const float inv = total > 0.f ? __fdividef(1.f, total) : total;            // (0 stays 0, NaN NaN)
         dot *= inv;
         float lse = 0.f;
-        if (with_z && total > 0.f) lse = m + logf(total);
+        if (with_z && total > 0.f) lse = fmaf(lg2(total), kLn2, m);
         if (row) {
             const float pb = inv * wb, gz = with_z ? inv * wz * lse : 0.f;
             float d[8 * NV];

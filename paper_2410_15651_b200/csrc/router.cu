@@ -154,6 +154,17 @@ int rlhf_router_loss_fwd_bwd(const void* logits, int logits_dtype, long long str
     };
     a.vec_in = vec(logits, stride_l, stride_b, stride_t);
     a.vec_out = vec(out_dlogits, dl_stride_l, dl_stride_b, dl_stride_t);
+    a.flat_in = a.per_sequence || B == 1 || T == 1 || stride_b == (long long)T * stride_t;
+    a.flat_out = a.per_sequence || B == 1 || T == 1 || dl_stride_b == (long long)T * dl_stride_t;
+    // (rows of single tokens follow each other at the sequences' stride)
+    if (T == 1 && !a.per_sequence) {
+        a.stride_t = stride_b;
+        a.dl_stride_t = dl_stride_b;
+    }
+    // division by T: ceil(2^(32 + shift) / T), shift the bits of T - 1
+    while ((1ll << a.t_shift) < T) ++a.t_shift;
+    a.t_shift = a.t_shift > 0 ? a.t_shift - 1 : 0;
+    a.t_magic = (unsigned)(((1ull << (32 + a.t_shift)) + (unsigned)T - 1) / (unsigned)T);
     const int grid = (int)(p.groups * p.n_chunks);
     cudaStream_t s = (cudaStream_t)stream;
     if (logits_dtype == RLHF_BF16) return launch_router<0>(a, grid, s);
