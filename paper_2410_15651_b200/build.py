@@ -17,7 +17,7 @@ LIB = os.path.join(PKG, "librlhf_ppo.so")
 NVCC_FLAGS = [
     "-std=c++17", "-O3", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-Xcompiler", "-fPIC", "-cudart", "static",
+    "-Xcompiler", "-fPIC", "-cudart", "static", "--split-compile=0",
 ]
 
 

@@ -8,9 +8,14 @@
 // and the loss is the sum of the same dot products.  With f_e - 1 in place of f_e (both dots have sum p = 1) nothing is lost
 // where the experts are nearly balanced.
 //
-// Two launches: counts, then losses and gradient.  A token is held by G = 1 .. 32 lanes with 8 (16, 32 above 256, 512
-// experts) consecutive entries each.  Both are bound by HBM in the large and by their two launches in the small; the second
-// walks the tokens backwards, so that what the first read last comes from L2.
+// Two launches: counts, then losses and gradient.  A token is held by G = 1 .. 32 lanes with one vector of eight entries each, or
+// two (16-bit logits of more than 8 experts) or four (above 512 experts); the rows are dealt to the blocks in turns, so that the
+// padding of short sequences is shared out.  Large calls read the logits twice and write the gradient once; what bounds them is
+// the selection and the softmax themselves (24 layers x 16 x 1024 tokens x 128 experts, K = 8, bf16, half of them padding: 119 us
+// for 189 MB, 1.6 TB/s; both kernels issue in about 45 % of the cycles, three blocks a multiprocessor).  Small calls are bound by
+// their two launches (23 us with the host's share at 2 x 16 tokens of 8 experts, 22 us at 16 x 1024 of 256 in fp32).
+// Two vectors per lane halve the shuffles of a token (176 -> 148 us), and as many blocks as are resident at once spare the
+// later ones' start and the last ones' wait (1184 blocks 143 us, 888 123 us, 592 147 us, 444 119 us).
 #pragma once
 #include "common.cuh"
 
@@ -20,7 +25,7 @@ constexpr int kRouterThreads = 256;
 constexpr int kRouterMaxExperts = 1024;
 constexpr int kRouterMaxChunks = 256;        // chunks of a group (partial counts: one per kRouterCluster of them)
 constexpr int kRouterCluster = 8;
-constexpr int kRouterTargetBlocks = 1184;
+constexpr int kRouterTargetBlocks = 444;     // three a multiprocessor, all of them at once
 
 enum : int { kRouterSoftmax = 0, kRouterSigmoid = 1 };
 
@@ -52,9 +57,9 @@ struct RouterArgs {
 
 // The element types: 16-bit as elsewhere, and fp32.
 template <int kType> struct RouterEl;        // rlhf_dtype_t
-template <> struct RouterEl<0> { using T = uint16_t; static __device__ __forceinline__ float get(uint16_t v) { return El<false>::widen(v); } };
-template <> struct RouterEl<1> { using T = uint16_t; static __device__ __forceinline__ float get(uint16_t v) { return El<true>::widen(v); } };
-template <> struct RouterEl<2> { using T = float; static __device__ __forceinline__ float get(float v) { return v; } };
+template <> struct RouterEl<0> { using T = uint16_t; };
+template <> struct RouterEl<1> { using T = uint16_t; };
+template <> struct RouterEl<2> { using T = float; };
 
 // Which tokens a block has: of group g the rows (a row is (b, t)) in turns of `turn` rows, every n_chunks-th of them, so that
 // padding is shared out.
@@ -96,60 +101,85 @@ __device__ __forceinline__ long long router_at(const RouterRow& w, bool flat, lo
     return flat ? (long long)w.r * stride_t : (long long)w.b * stride_b + (long long)w.t * stride_t;
 }
 
-// Entries e0 .. e0 + 8 NV - 1 of a row; `missing` past E.
-template <int kType, int NV>
-__device__ __forceinline__ void router_load(const typename RouterEl<kType>::T* row, int e0, int E, bool vec, float missing,
-                                            float (&z)[8 * NV])
-{
+// A lane has NV vectors of eight entries, sub, sub + G and so on of its token's (neighbours in one access).  Its entries come in
+// pairs; the first expert of pair j:
+template <int G>
+__device__ __forceinline__ int router_expert(int sub, int j) { return 8 * (sub + G * (j >> 2)) + 2 * (j & 3); }
+
+// A lane's entries as they lie; `missing` past E.
+template <int kType, int NV, int G>
+struct RouterRaw {
     using Ty = typename RouterEl<kType>::T;
+    static constexpr bool kHalf = sizeof(Ty) == 2;
+    uint32_t w[(kHalf ? 4 : 8) * NV];
+
+    __device__ __forceinline__ void fill(uint32_t missing)
+    {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int e = e0 + 8 * v;
-        float* o = z + 8 * v;
-        if (vec && e < E) {                  // E is a multiple of 8 then
-            if constexpr (sizeof(Ty) == 2) {
-                const uint4 q = __ldg((const uint4*)(row + e));
-                const float2 p0 = El<kType == 1>::unpack2(q.x), p1 = El<kType == 1>::unpack2(q.y), p2 = El<kType == 1>::unpack2(q.z),
-                             p3 = El<kType == 1>::unpack2(q.w);
-                o[0] = p0.x; o[1] = p0.y; o[2] = p1.x; o[3] = p1.y; o[4] = p2.x; o[5] = p2.y; o[6] = p3.x; o[7] = p3.y;
+        for (int j = 0; j < (kHalf ? 4 : 8) * NV; ++j) w[j] = missing;
+    }
+    __device__ __forceinline__ void load(const Ty* row, int sub, int E, bool vec, uint32_t missing)
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int e = router_expert<G>(sub, 4 * v);
+            uint32_t* o = w + (kHalf ? 4 : 8) * v;
+            if (vec) {                       // E is a multiple of 8 then
+                uint4 q = make_uint4(missing, missing, missing, missing), x = q;
+                if (e < E) {
+                    q = __ldg((const uint4*)(row + e));
+                    if (!kHalf) x = __ldg((const uint4*)(row + e) + 1);
+                }
+                o[0] = q.x; o[1] = q.y; o[2] = q.z; o[3] = q.w;
+                if (!kHalf) { o[4] = x.x; o[5] = x.y; o[6] = x.z; o[7] = x.w; }
+            } else if constexpr (kHalf) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j] = (e + 2 * j < E ? (uint32_t)row[e + 2 * j] : missing & 0xffffu) |
+                           (e + 2 * j + 1 < E ? (uint32_t)row[e + 2 * j + 1] << 16 : missing & 0xffff0000u);
             } else {
-                const float4 q = __ldg((const float4*)(row + e)), w = __ldg((const float4*)(row + e) + 1);
-                o[0] = q.x; o[1] = q.y; o[2] = q.z; o[3] = q.w; o[4] = w.x; o[5] = w.y; o[6] = w.z; o[7] = w.w;
-            }
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = e + j < E ? RouterEl<kType>::get(row[e + j]) : missing;
+                for (int j = 0; j < 8; ++j) o[j] = e + j < E ? __float_as_uint(row[e + j]) : missing;
+            }
         }
     }
-}
+    __device__ __forceinline__ float2 pair(int j) const
+    {
+        if constexpr (kHalf) return El<kType == 1>::unpack2(w[j]);
+        else return make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+    }
+    static __device__ __forceinline__ uint32_t minus_inf() { return kType == 0 ? 0xff80ff80u : kType == 1 ? 0xfc00fc00u : 0xff800000u; }
+};
 
-template <int kType, int NV>
-__device__ __forceinline__ void router_store(typename RouterEl<kType>::T* row, int e0, int E, bool vec, const float (&d)[8 * NV])
+template <int kType, int NV, int G>
+__device__ __forceinline__ void router_store(typename RouterEl<kType>::T* row, int sub, int E, bool vec, const float2 (&d)[4 * NV])
 {
     using Ty = typename RouterEl<kType>::T;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int e = e0 + 8 * v;
-        const float* x = d + 8 * v;
+        const int e = router_expert<G>(sub, 4 * v);
+        const float2* x = d + 4 * v;
         if constexpr (sizeof(Ty) == 2) {
-            const uint4 w = make_uint4(El<kType == 1>::pack2(x[0], x[1]), El<kType == 1>::pack2(x[2], x[3]),
-                                       El<kType == 1>::pack2(x[4], x[5]), El<kType == 1>::pack2(x[6], x[7]));
-            if (vec && e < E) {
-                __stcs((uint4*)(row + e), w);
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = El<kType == 1>::pack2(x[j].x, x[j].y);
+            if (vec) {
+                if (e < E) __stcs((uint4*)(row + e), make_uint4(w[0], w[1], w[2], w[3]));
             } else {
-                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (e + j < E) row[e + j] = (uint16_t)(ww[j >> 1] >> (16 * (j & 1)));
+                    if (e + j < E) row[e + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
             }
         } else {
-            if (vec && e < E) {
-                __stcs((float4*)(row + e), make_float4(x[0], x[1], x[2], x[3]));
-                __stcs((float4*)(row + e) + 1, make_float4(x[4], x[5], x[6], x[7]));
+            if (vec) {
+                if (e < E) {
+                    __stcs((float4*)(row + e), make_float4(x[0].x, x[0].y, x[1].x, x[1].y));
+                    __stcs((float4*)(row + e) + 1, make_float4(x[2].x, x[2].y, x[3].x, x[3].y));
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (e + j < E) row[e + j] = x[j];
+                    if (e + j < E) row[e + j] = j & 1 ? x[j >> 1].y : x[j >> 1].x;
             }
         }
     }
@@ -162,7 +192,7 @@ __device__ __forceinline__ uint32_t router_key(float z)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Lanes of a token.
+// Lanes of a token with nv vectors each.
 __host__ __device__ constexpr int router_lanes(int E, int nv)
 {
     int g = 1;
@@ -214,56 +244,43 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
             }
         if (bad) atomicOr(a.status, kErrIdRange);
     } else {
-        // 16-bit logits of one vector per lane: a key orders logit and expert at once (the higher logit, then the lower expert).  A
-        // lane sorts its eight, and every turn takes the largest head.  Else a turn looks for the largest of all.
-        constexpr bool kSorted = sizeof(Ty) == 2 && NV == 1;
+        // 16-bit logits of up to 256 experts: a key orders logit and expert at once (the higher logit, then the lower expert).  A lane
+        // sorts its own, and each choice is the largest head of the token's lanes.  Else a choice looks through all.
+        constexpr int N = 8 * NV;
+        constexpr bool kSorted = sizeof(Ty) == 2 && N * G <= 256;
         constexpr int kPerWarp = 32 / G, kTurn = kRouterThreads / 32 * kPerWarp;
-        const int sub = lane & (G - 1), e0 = sub * 8 * NV;
-        const uint32_t group = (G == 32 ? 0xffffffffu : ((1u << (G & 31)) - 1u)) << (lane & ~(G - 1));
+        const int sub = lane & (G - 1);
         const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l + (a.per_sequence && a.flat_in ? it.b0 * a.stride_b : 0);
         int* const ids_base = a.out_ids + ((long long)it.l * a.B + it.b0) * a.T * a.K;
         const int mine = warp * kPerWarp + lane / G;
         const int step = a.n_chunks * kTurn;
         int r = it.chunk * kTurn;
         RouterRow w = router_row(a, it, r + mine);
-        float z[8 * NV];
-        uint4 q = make_uint4(0, 0, 0, 0);                // kSorted and vec_in: the lane's logits as they are
+        RouterRaw<kType, NV, G> z;
+        z.fill(0u);
         auto load = [&]() {
-            if (!w.valid) return;
-            const Ty* row = base + router_at(w, a.flat_in, a.stride_b, a.stride_t);
-            if (kSorted && a.vec_in) {
-                if (e0 < a.E) q = __ldg((const uint4*)(row + e0));
-            } else {
-                router_load<kType, NV>(row, e0, a.E, a.vec_in, 0.f, z);
-            }
+            if (w.valid) z.load(base + router_at(w, a.flat_in, a.stride_b, a.stride_t), sub, a.E, a.vec_in, 0u);
         };
         load();
         // (every lane of a warp makes every turn: the shuffles want them all)
         for (; r < it.rows; r += step) {
-            const bool row = w.row, valid = w.valid;
-            int* const out = a.out_ids && row ? ids_base + (long long)w.r * a.K : nullptr;
-            uint32_t key[8 * NV];
-            if (kSorted && a.vec_in) {
-                if (valid && e0 < a.E) {
-                    const uint32_t x[4] = {router_order2<kType == 1>(q.x), router_order2<kType == 1>(q.y), router_order2<kType == 1>(q.z),
-                                           router_order2<kType == 1>(q.w)};
+            const bool valid = w.valid;
+            int* const out = a.out_ids && w.row ? ids_base + (long long)w.r * a.K : nullptr;
+            uint32_t key[N];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        key[2 * j] = (x[j] << 16) + (0xffffu - (uint32_t)(e0 + 2 * j));
-                        key[2 * j + 1] = (x[j] & 0xffff0000u) | (0xffffu - (uint32_t)(e0 + 2 * j + 1));
-                    }
+            for (int j = 0; j < N / 2; ++j) {
+                const int e = router_expert<G>(sub, j);
+                if constexpr (kSorted) {
+                    const uint32_t x = router_order2<kType == 1>(z.w[j]);
+                    key[2 * j] = (x << 16) + (0xffffu - (uint32_t)e);
+                    key[2 * j + 1] = (x & 0xffff0000u) | (0xfffeu - (uint32_t)e);
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) key[j] = 0u;
+                    const float2 x = z.pair(j);
+                    key[2 * j] = router_key(x.x);
+                    key[2 * j + 1] = router_key(x.y);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8 * NV; ++j) {
-                    key[j] = valid && e0 + j < a.E ? router_key(z[j]) : 0u;
-                    // (the low 13 bits of a 16-bit logit's key say nothing, and there are at most 256 experts; the top bits of the low
-                    // half are the logit's in this form and 1 in the other)
-                    if (kSorted && key[j]) key[j] = (max(key[j], 0x100u) & 0xffffff00u) | (0xffu - (uint32_t)(e0 + j));
-                }
+                if (!valid || e >= a.E) key[2 * j] = 0u;
+                if (!valid || e + 1 >= a.E) key[2 * j + 1] = 0u;
             }
             w = router_row(a, it, r + step + mine);
             load();                                      // in flight meanwhile
@@ -278,42 +295,70 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
                     key[x] = hi;
                     key[y] = lo;
                 };
-                // Batcher's odd-even merge of eight
-                order(0, 1); order(2, 3); order(4, 5); order(6, 7);
-                order(0, 2); order(1, 3); order(4, 6); order(5, 7);
-                order(1, 2); order(5, 6);
-                order(0, 4); order(1, 5); order(2, 6); order(3, 7);
-                order(2, 4); order(3, 5);
-                order(1, 2); order(3, 4); order(5, 6);
+#pragma unroll
+                for (int i = 0; i < N; i += 8) {         // Batcher's odd-even merge of eight
+                    order(i, i + 1); order(i + 2, i + 3); order(i + 4, i + 5); order(i + 6, i + 7);
+                    order(i, i + 2); order(i + 1, i + 3); order(i + 4, i + 6); order(i + 5, i + 7);
+                    order(i + 1, i + 2); order(i + 5, i + 6);
+                    order(i, i + 4); order(i + 1, i + 5); order(i + 2, i + 6); order(i + 3, i + 7);
+                    order(i + 2, i + 4); order(i + 3, i + 5);
+                    order(i + 1, i + 2); order(i + 3, i + 4); order(i + 5, i + 6);
+                }
+                auto bitonic = [&](int i) {              // sorts eight that rise and fall
+                    order(i, i + 4); order(i + 1, i + 5); order(i + 2, i + 6); order(i + 3, i + 7);
+                    order(i, i + 2); order(i + 1, i + 3); order(i + 4, i + 6); order(i + 5, i + 7);
+                    order(i, i + 1); order(i + 2, i + 3); order(i + 4, i + 5); order(i + 6, i + 7);
+                };
                 auto top = [&]() {
                     uint32_t best = key[0];
 #pragma unroll
                     for (int o = G / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
                     return best;
                 };
-                if (G >= 8 && a.K <= 8) {                // lane k of a token keeps its k-th choice
-                    uint32_t got = 0u;
+                if (a.K <= 8) {                          // lane k % G of a token keeps its k-th choice
+                    if constexpr (NV == 2) {             // (eight of sixteen will do)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) key[i] = max(key[i], key[15 - i]);
+                        bitonic(0);
+                    }
+                    uint32_t got[8 / (G < 8 ? G : 8)];
+#pragma unroll
+                    for (int i = 0; i < 8 / (G < 8 ? G : 8); ++i) got[i] = 0u;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         if (k >= a.K) break;
                         const uint32_t best = top();
                         const bool won = key[0] == best;
-                        if (sub == k) got = best;
+                        if (sub == (k & (G - 1))) got[k / G] = best;
 #pragma unroll
                         for (int j = 0; j < 7 - k; ++j) key[j] = won ? key[j + 1] : key[j];
                     }
-                    if (sub < a.K) {
-                        const int e = got ? 0xff - (int)(got & 0xffu) : 0;
-                        if (got) atomicAdd(s_count + e, 1);
-                        if (out) out[sub] = e;
+#pragma unroll
+                    for (int i = 0; i < 8 / (G < 8 ? G : 8); ++i) {
+                        const int k = i * G + sub;
+                        if (k < a.K) {
+                            const int e = got[i] ? 0xff - (int)(got[i] & 0xffu) : 0;
+                            if (got[i]) atomicAdd(s_count + e, 1);
+                            if (out) out[k] = e;
+                        }
                     }
                 } else {
+                    if constexpr (NV == 2) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {    // the upper eight, the lower eight
+                            const uint32_t x = key[i], y = key[15 - i];
+                            key[i] = max(x, y);
+                            key[15 - i] = min(x, y);
+                        }
+                        bitonic(0);
+                        bitonic(8);
+                    }
                     for (int k = 0; k < a.K; ++k) {
                         const uint32_t best = top();
                         if (key[0] == best && best != 0u) {
 #pragma unroll
-                            for (int j = 0; j < 7; ++j) key[j] = key[j + 1];
-                            key[7] = 0u;
+                            for (int j = 0; j < N - 1; ++j) key[j] = key[j + 1];
+                            key[N - 1] = 0u;
                             const int e = 0xff - (int)(best & 0xffu);
                             atomicAdd(s_count + e, 1);
                             if (out) out[k] = e;
@@ -323,22 +368,21 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
                 }
             } else {
                 for (int k = 0; k < a.K; ++k) {
-                    uint32_t top = key[0];
+                    uint32_t best = key[0];
 #pragma unroll
-                    for (int j = 1; j < 8 * NV; ++j) top = max(top, key[j]);
-                    uint32_t best = top;
+                    for (int j = 1; j < N; ++j) best = max(best, key[j]);
 #pragma unroll
                     for (int o = G / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-                    const uint32_t who = __ballot_sync(0xffffffffu, top == best) & group;
-                    if (lane == __ffs(who) - 1) {        // the lowest expert of those that are equal
-                        int at = 0;
+                    int e = kRouterMaxExperts;           // the lowest expert of those that are equal
 #pragma unroll
-                        for (int j = 8 * NV - 1; j >= 0; --j)
-                            if (key[j] == best) at = j;
+                    for (int j = N - 1; j >= 0; --j)
+                        if (key[j] == best) e = router_expert<G>(sub, j >> 1) + (j & 1);
 #pragma unroll
-                        for (int j = 0; j < 8 * NV; ++j)
-                            if (j == at) key[j] = 0u;
-                        const int e = min(e0 + at, a.E - 1);
+                    for (int o = G / 2; o > 0; o >>= 1) e = min(e, __shfl_xor_sync(0xffffffffu, e, o));
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (e == router_expert<G>(sub, j >> 1) + (j & 1)) key[j] = 0u;
+                    if (sub == 0) {
                         if (valid) atomicAdd(s_count + e, 1);
                         if (out) out[k] = valid ? e : 0;
                     }
@@ -375,7 +419,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_count_kernel(const __gr
 
 // ---------------------------------------------------------------- losses and gradient
 template <int kType, int NV, int G>
-__global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __grid_constant__ RouterArgs a)
+__global__ void __launch_bounds__(kRouterThreads, NV == 1 ? 4 : NV == 2 ? 3 : 1) router_loss_kernel(const __grid_constant__ RouterArgs a)
 {
     using Ty = typename RouterEl<kType>::T;
     __shared__ float s_f[kRouterMaxExperts];             // f_e - 1
@@ -404,14 +448,16 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
     const double wd = n > 0 ? 1.0 / ((double)n * (double)filled) : 0.0, zd = N > 0 ? 1.0 / (double)N : 0.0;
     const float wb = (float)((double)a.grad_scale * a.balance_coef * wd), wz = (float)((double)a.grad_scale * a.z_coef * 2.0 * zd);
     constexpr int kPerWarp = 32 / G, kTurn = kRouterThreads / 32 * kPerWarp;
-    const int sub = lane & (G - 1), e0 = sub * 8 * NV;
+    const int sub = lane & (G - 1);
     const Ty* const base = (const Ty*)a.logits + (long long)it.l * a.stride_l + (a.per_sequence && a.flat_in ? it.b0 * a.stride_b : 0);
     Ty* const dbase = (Ty*)a.dlogits + (long long)it.l * a.dl_stride_l + (a.per_sequence && a.flat_out ? it.b0 * a.dl_stride_b : 0);
     const bool with_z = a.z_coef != 0.f;
     float2 f[4 * NV];                                    // the lane's experts are the same of every token
 #pragma unroll
-    for (int j = 0; j < 4 * NV; ++j)
-        f[j] = make_float2(e0 + 2 * j < a.E ? s_f[e0 + 2 * j] : 0.f, e0 + 2 * j + 1 < a.E ? s_f[e0 + 2 * j + 1] : 0.f);
+    for (int j = 0; j < 4 * NV; ++j) {
+        const int e = router_expert<G>(sub, j);
+        f[j] = make_float2(e < a.E ? s_f[e] : 0.f, e + 1 < a.E ? s_f[e + 1] : 0.f);
+    }
     // sums of a block's tokens: a lane has some tens of them, added in fp32, then in double
     float sum_dot = 0.f, sum_lse = 0.f;
     int tokens = 0;
@@ -419,14 +465,10 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
     const int step = a.n_chunks * kTurn;
     int r = it.chunk * kTurn;
     RouterRow w = router_row(a, it, r + mine);
-    float z[8 * NV];
+    RouterRaw<kType, NV, G> z;
     auto load = [&]() {                                  // (a row that is no token has p = 0)
-        if (w.valid) {
-            router_load<kType, NV>(base + router_at(w, a.flat_in, a.stride_b, a.stride_t), e0, a.E, a.vec_in, -INFINITY, z);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8 * NV; ++j) z[j] = -INFINITY;
-        }
+        if (w.valid) z.load(base + router_at(w, a.flat_in, a.stride_b, a.stride_t), sub, a.E, a.vec_in, z.minus_inf());
+        else z.fill(z.minus_inf());
     };
     load();
     for (; r < it.rows; r += step) {
@@ -434,7 +476,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
         Ty* const dst = dbase + router_at(w, a.flat_out, a.dl_stride_b, a.dl_stride_t);
         float2 p[4 * NV], slope[4 * NV];
 #pragma unroll
-        for (int j = 0; j < 4 * NV; ++j) p[j] = make_float2(z[2 * j], z[2 * j + 1]);
+        for (int j = 0; j < 4 * NV; ++j) p[j] = z.pair(j);
         w = router_row(a, it, r + step + mine);
         load();                                          // in flight meanwhile
         float m = 0.f;
@@ -480,17 +522,14 @@ __global__ void __launch_bounds__(kRouterThreads) router_loss_kernel(const __gri
         if (with_z && total > 0.f) lse = fmaf(lg2(total), kLn2, m);
         if (row) {
             const float pb = inv * wb, gz = with_z ? inv * wz * lse : 0.f;
-            float d[8 * NV];
 #pragma unroll
             for (int j = 0; j < 4 * NV; ++j) {
                 float2 v = __fadd2_rn(f[j], splat2(-dot));
                 if (a.scoring == kRouterSigmoid) v = __fmul2_rn(__fmul2_rn(v, slope[j]), splat2(pb));
                 else v = __ffma2_rn(v, splat2(pb), splat2(gz));
-                v = __fmul2_rn(v, p[j]);
-                d[2 * j] = v.x;
-                d[2 * j + 1] = v.y;
+                p[j] = __fmul2_rn(v, p[j]);
             }
-            router_store<kType, NV>(dst, e0, a.E, a.vec_out, d);
+            router_store<kType, NV, G>(dst, sub, a.E, a.vec_out, p);
         }
         if (valid && sub == 0) {
             if (total != 0.f) {                          // (0: a token that may choose no expert)
