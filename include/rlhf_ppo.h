@@ -439,7 +439,8 @@ int rlhf_preference_loss_fwd_bwd(const void* logits, int logits_dtype, long long
  *     x_v = (z2 + bias_v) / temperature[b]                where the mask allows v; else -inf, whatever z_v and bias_v are.
  * A decoding step has T = 1 and start[b] tokens so far; the rows of whole answers have start = NULL and tokens = ids.
  *   prompt, tokens   int64, [b*stride_b + i], i < prompt_len / tokens_len.  An id of -1 is no token (padding); another one outside
- *                    [0,V) sets RLHF_ERR_ID_RANGE and is none.  Tokens from start[b] + lengths[b] - 1 on are not read.
+ *                    [0,V) sets RLHF_ERR_ID_RANGE and is none.  Tokens from start[b] + lengths[b] - 1 on are not read. prompt_len,
+ *                    tokens_len and V are at most 2^30 (RLHF_ERR_SHAPE).
  *   prompt_lengths   int32 [B]; NULL: prompt_len.   start   int32 [B]; NULL: 0.  A prompt length outside [0, prompt_len], a
  *                    negative start, or tokens that end before a row's history (start[b] + lengths[b] - 1 > tokens_len) set
  *                    RLHF_ERR_LENGTH_RANGE; what there is counts.

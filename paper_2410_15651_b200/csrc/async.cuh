@@ -56,6 +56,19 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, unsigne
     if (mbar_try_wait(bar, parity)) return;
     if (!mbar_wait_slow(bar, parity, status, limit_ns)) aborted = true;
 }
+// The same without a call, whose saved registers cost a kernel that often waits more than the few instructions.
+__device__ __forceinline__ void mbar_wait_here(uint32_t bar, uint32_t parity, unsigned* status, bool& aborted,
+                                               unsigned long long limit_ns)
+{
+    if (aborted || mbar_try_wait(bar, parity)) return;
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(bar, parity))
+        if (global_timer_ns() - t0 > limit_ns) {
+            atomicOr(status, kErrTimeout);
+            aborted = true;
+            return;
+        }
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
 {
     asm volatile(

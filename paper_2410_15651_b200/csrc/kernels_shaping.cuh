@@ -30,6 +30,8 @@ namespace rlhf {
 constexpr unsigned kErrValueRange = 128u;
 
 constexpr int kShapeWarps = 24;             // warps of a block of shaping_kernel, at most
+constexpr int kShapeLpWarps = 20;           // the same of log-probs, which want 96 registers (16 x 512 of 128256 with masks and
+                                            // entropy: 24 warps of 80 registers 696 us, 20 565 us, 16 675 us)
 constexpr int kShapeSegment = 512;          // vectors of eight entries of a warp, at most
 constexpr int kShapeRows = 32;              // rows between two updates of the table
 constexpr int kShapeMaxCluster = 8;
@@ -104,7 +106,7 @@ __host__ __device__ inline ShapeSmem shape_smem(const ShapeKernelArgs& a, int wa
     ShapeSmem s;
     s.bufs = 0;
     s.words = s.bufs + (a.sparse ? 0 : buf * warps * a.n_bufs);
-    s.bars = s.words + (a.sh.mask ? 2 * 4 * ((size_t)a.segment / 4 + 2) * warps : 0);
+    s.bars = s.words + (a.sh.mask ? 2 * 4 * ((size_t)a.segment / 4 + 4) * warps : 0);
     s.bars = (s.bars + 15) / 16 * 16;
     s.bits = s.bars + ((size_t)warps * a.n_bufs * 8 + 15) / 16 * 16;
     s.list = s.bits + 4 * (size_t)a.bits_words;
@@ -231,29 +233,31 @@ __device__ __forceinline__ void lane_add16(LaneSums& a, const float2 (&z)[2][4],
         if (m == kNoRef) return;
         lane_rebase(a, m, k);
     }
-    const float2 nc = splat2(-a.c), kk = splat2(k);
-    float2 sum[2] = {splat2(0.f), splat2(0.f)}, ez[2] = {splat2(0.f), splat2(0.f)};
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 y = __ffma2_rn(z[u][j], kk, nc);
-            const float2 e = make_float2(ex2(y.x), ex2(y.y));
-            sum[u] = __fadd2_rn(sum[u], e);
-            if (want_ent) ez[u] = __ffma2_rn(e, make_float2(fmaxf(y.x, kLpClamp), fmaxf(y.y, kLpClamp)), ez[u]);
-        }
-    const float2 vs = __fadd2_rn(sum[0], sum[1]);
-    if (vs.x + vs.y <= 1.8446744e19f) {
-        a.s += vs.x + vs.y;
-        if (want_ent) a.ez += (ez[0].x + ez[0].y) + (ez[1].x + ez[1].y);
-    } else {                                               // a term more than 64 binades above the reference
+    for (bool again = false;; again = true) {              // (a loop: the registers of two copies would not fit)
+        const float2 nc = splat2(-a.c), kk = splat2(k);
+        float2 sum[2] = {splat2(0.f), splat2(0.f)}, ez[2] = {splat2(0.f), splat2(0.f)};
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                lane_add1(a, z[u][j].x, k, want_ent);
-                lane_add1(a, z[u][j].y, k, want_ent);
+                const float2 y = __ffma2_rn(z[u][j], kk, nc);
+                const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                sum[u] = __fadd2_rn(sum[u], e);
+                if (want_ent) ez[u] = __ffma2_rn(e, make_float2(fmaxf(y.x, kLpClamp), fmaxf(y.y, kLpClamp)), ez[u]);
             }
+        const float2 vs = __fadd2_rn(sum[0], sum[1]);
+        if (again || vs.x + vs.y <= 1.8446744e19f) {
+            a.s += vs.x + vs.y;
+            if (want_ent) a.ez += (ez[0].x + ez[0].y) + (ez[1].x + ez[1].y);
+            return;
+        }
+        // a term more than 64 binades above the reference: their maximum is the next one
+        float m = kNoRef;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(z[u][j].x, z[u][j].y));
+        if (m > a.ref) lane_rebase(a, m, k);               // (not for NaN)
     }
 }
 
@@ -620,7 +624,8 @@ __global__ void __launch_bounds__(kRowThreads, 4) shaping_row_kernel(const __gri
         }
     }
     if (tid == 0) load_settings(sh, b, s_w);
-    auto in_table = [&](long long v) { return v >= max(tb, 0) && v < (long long)tb + n_ent && v < V; };
+    const long long lo = max(tb, 0), span = max(min((long long)tb + n_ent, (long long)V) - lo, 0ll);
+    auto in_table = [&](long long v) { return (unsigned long long)v - (unsigned long long)lo < (unsigned long long)span; };
     // an entry next to the slice's border is in two tables: the block that has its vector forms it
     auto has = [&](int v) {
         const int i = (v + oo) >> 3;
@@ -631,7 +636,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) shaping_row_kernel(const __gri
         bool bad_id = false;
         auto mark = [&](long long v, bool of_answer) {
             if (!in_table(v)) {
-                if (v < -1 || v >= V) bad_id = true;
+                if ((unsigned long long)v + 1 > (unsigned long long)V) bad_id = true;
                 return;
             }
             const int el = (int)v - tb;
@@ -646,8 +651,17 @@ __global__ void __launch_bounds__(kRowThreads, 4) shaping_row_kernel(const __gri
         const long long* p = sh.prompt + (long long)b * sh.prompt_stride_b;
         const long long* k = sh.tokens + (long long)b * sh.tokens_stride_b;
         const int n = sh.tokens ? (int)min((long long)s_w.first + t, (long long)sh.S) : 0;
-        for (int i = tid; i < plen; i += kRowThreads) mark(__ldg(p + i), false);
-        for (int i = tid; i < n; i += kRowThreads) mark(__ldg(k + i), true);
+        auto scan = [&](const long long* from, int n, bool of_answer) {         // (four loads at a time: the block waits for them)
+            for (int i = tid; i < n; i += 4 * kRowThreads) {
+                long long v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = u * kRowThreads < n - i ? __ldg(from + i + u * kRowThreads) : -1;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) mark(v[u], of_answer);
+            }
+        };
+        scan(p, plen, false);
+        scan(k, n, true);
         if (bad_id) atomicOr(a.status, kErrIdRange);
         __syncthreads();
     }
@@ -710,11 +724,12 @@ struct ShapeRow {
 // kAny: rows of any alignment.  The vectors then follow the rows that are written (the source's where none are), and a source
 // that is off them by `delta` entries is shifted into place from two aligned vectors.
 template <int kMode, bool kF16, bool kAny>
-__global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __grid_constant__ ShapeKernelArgs a)
+__global__ void __launch_bounds__((kMode == kShapeLp ? kShapeLpWarps : kShapeWarps) * 32, 1) shaping_kernel(const __grid_constant__ ShapeKernelArgs a)
 {
     constexpr bool kLp = kMode == kShapeLp, kLpBwd = kMode == kShapeLpBwd, kBwd = kMode == kShapeBwd, k32 = kMode == kShape32;
     constexpr bool kTokens = kLp || kLpBwd;                // a row has a generated token
     extern __shared__ __align__(16) unsigned char smem[];
+    const bool sparse = !kLp && a.sparse;
     __shared__ ShapeWalk s_w;
     __shared__ int s_scan[kShapeWarps];
     // the tokens before the coming rows: each one (less tb), the rows (bits) that it stands before, and whether H has it already
@@ -745,7 +760,7 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
     uint16_t* const s_list = (uint16_t*)(smem + at.list);        // those entries, less tb
     uint8_t* const s_mark = smem + at.marks;                     // 1 + place among s_token of a listed entry that is there, or 0
     uint32_t* const s_cnt = (uint32_t*)(smem + at.counts);       // how often the answer has an entry (16 or 32 bits)
-    const int buf_bytes = 16 * a.segment + (kAny ? 32 : 0), n_words = a.segment / 4 + 2;
+    const int buf_bytes = 16 * a.segment + (kAny ? 32 : 0), n_words = a.segment / 4 + 4;
     unsigned char* const bufs = smem + (size_t)warp * a.n_bufs * buf_bytes;
     uint32_t* const words = (uint32_t*)(smem + at.words) + warp * 2 * n_words;   // the warp's mask words of two rows
     const uint32_t bars = smem_u32(smem + at.bars) + 8u * (uint32_t)(warp * a.n_bufs);
@@ -824,7 +839,8 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
             const int tb = begin * 8 - (kAny ? 8 : 0);     // entry of the table's first bit
             const float inv_tau = s_w.inv_tau;
             const bool ragged = kAny || (V & 7);
-            auto in_table = [&](long long v) { return v >= max(tb, 0) && v < (long long)tb + n_ent && v < V; };
+            const long long lo = max(tb, 0), span = max(min((long long)tb + n_ent, (long long)V) - lo, 0ll);
+    auto in_table = [&](long long v) { return (unsigned long long)v - (unsigned long long)lo < (unsigned long long)span; };
             auto row_at = [&](int t) {
                 ShapeRow r;
                 r.src = s_w.src + (long long)t * a.src_stride_t;
@@ -857,13 +873,20 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
             // The row's mask words from that of the warp's first entry on, into the half of `words` that is not in use.
             auto issue_words = [&](int t) {
                 const int w0 = (8 * v0 - (kAny ? row_at(t).oo : 0)) >> 5;
-                const uint32_t* m = s_w.mask + (long long)t * sh.mask_stride_t;
-                for (int i = lane; i < n_words; i += 32)
-                    if (w0 + i >= 0 && w0 + i < (V + 31) >> 5)
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(words + (t & 1) * n_words + i)), "l"(m + w0 + i) : "memory");
+                const uint32_t* const m = s_w.mask + (long long)t * sh.mask_stride_t + w0;
+                const uint32_t to = smem_u32(words) + 4u * (uint32_t)((t & 1) * n_words);
+                const int left = ((V + 31) >> 5) - w0;     // (a row may leave the last warp nothing)
+                if (!kAny && left >= a.segment / 4 && ((uintptr_t)m & 15) == 0) {
+                    for (int i = lane; i < a.segment / 16; i += 32)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16u * i), "l"(m + 4 * i) : "memory");
+                } else {
+                    for (int i = lane; i < min(n_words, left); i += 32)
+                        if (w0 + i >= 0)
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4u * i), "l"(m + i) : "memory");
+                }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
-            if (lane == 0 && !a.sparse)
+            if (lane == 0 && !sparse)
                 for (int i = 0; i < a.n_bufs && t + i < te; ++i) issue(t + i, i);
             if (sh.mask) issue_words(t);
 
@@ -896,8 +919,17 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                 const int plen = sh.prompt_lengths ? clamp_len(__ldg(sh.prompt_lengths + b), sh.P) : sh.P;
                 const long long* p = sh.prompt + (long long)b * sh.prompt_stride_b;
                 const int n = sh.tokens ? (int)min((long long)s_w.first + t, (long long)sh.S) : 0;
-                for (int i = tid; i < plen; i += nt) mark(__ldg(p + i), false);
-                for (int i = tid; i < n; i += nt) mark(__ldg(s_w.answer + i), true);
+                auto scan = [&](const long long* from, int n, bool of_answer) {
+                    for (int i = tid; i < n; i += 4 * nt) {
+                        long long v[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) v[u] = u * nt < n - i ? __ldg(from + i + u * nt) : -1;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) mark(v[u], of_answer);
+                    }
+                };
+                scan(p, plen, false);
+                scan(s_w.answer, n, true);
                 if (bad_id) atomicOr(a.status, kErrIdRange);
             }
 
@@ -916,7 +948,7 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                 if (warp == 0 && a.uses_history) {
                     int el = -1;
                     if (sh.tokens && lane < n && t + lane > s_w.ta && (long long)s_w.first + t + lane - 1 < sh.S) {
-                        const long long v = __ldg(s_w.answer + s_w.first + t + lane - 1);
+                        const long long v = s_w.answer[s_w.first + t + lane - 1];
                         if (in_table(v)) el = (int)v - tb;
                         else if (v < -1 || v >= V) atomicOr(a.status, kErrIdRange);
                     }
@@ -1028,15 +1060,15 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                     const uint32_t j = k < l1 ? s_mark[k] : 0u;
                     const uint32_t so_far = j ? s_before[j - 1] & ((2u << r) - 1u) : 0u;
                     const bool listed = k < l1 && (so_far || !(j && (s_fresh >> (j - 1) & 1u)));
-                    const float raw = El<kF16>::widen(a.sparse ? row.src[v] : ((const uint16_t*)buf)[v - (first - row.delta)]);
+                    const float raw = El<kF16>::widen(sparse ? row.src[v] : ((const uint16_t*)buf)[v - (first - row.delta)]);
                     const bool ok = !sh.mask || (my_words[(v >> 5) - (first >> 5)] >> (v & 31) & 1u);
                     uint32_t c = 0;
                     if (a.uses_counts && listed) c = (a.wide_counts ? s_cnt[el] : ((const uint16_t*)s_cnt)[el]) + __popc(so_far);
                     return shape1<kMode>(raw, listed ? ((kBwd ? sign : raw) < 0.f ? s_w.rep : s_w.inv_rep) : 1.f, c, s_w.freq, s_w.pres,
-                                         sh.bias ? s_w.bias + v : nullptr, ok, inv_tau, norm, a.grad_entropy != nullptr,
+                                         sh.bias ? s_w.bias + v : nullptr, ok, kLp ? s_w.inv_tau : inv_tau, norm, a.grad_entropy != nullptr,
                                          kLpBwd && v == y, kLpBwd ? s_lp[r] : 0.f);
                 };
-                int el = mine ? entry_of(l0 + lane) : -1;
+                int el = mine && !kLp ? entry_of(l0 + lane) : -1;
                 float sign = sign_of(el);                  // (in flight during the row)
                 if (kLp && y_here) {                       // (left out of the sum as the listed are)
                     __syncwarp();
@@ -1046,8 +1078,8 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
 
                 LaneSums acc = lane_sums();
                 const float k2 = kLog2e * inv_tau;
-                if (mine && !a.sparse) {
-                    mbar_wait(bars + 8u * slot, (phases >> slot) & 1u, a.status, aborted, a.wait_limit_ns);
+                if (mine && !sparse) {
+                    mbar_wait_here(bars + 8u * slot, (phases >> slot) & 1u, a.status, aborted, a.wait_limit_ns);
                     phases ^= 1u << slot;
                     const uint4* const vecs = (const uint4*)buf;
                     const int n = row.end - v0;
@@ -1061,6 +1093,31 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                     };
                     if (kLp) {
                         // two vectors at a time, what is not summed at -inf
+                        if (!kAny && !sh.bias && n == a.segment && first + 8 * n <= V) {
+                            // (what aligned rows need and nothing else: the loop is bound by its instructions)
+                            uint32_t pv = smem_u32(buf) + 16u * lane, pb = smem_u32(s_bits) + (uint32_t)(v0 - begin + lane), pm = smem_u32(my_words) + lane;
+                            auto stream = [&](auto masked, auto entropy) {
+#pragma unroll 1
+                                for (const uint32_t pe = pv + 16u * (uint32_t)a.segment; pv < pe; pv += 1024u, pb += 64u, pm += 64u) {
+                                    float2 z[2][4];
+#pragma unroll
+                                    for (int u = 0; u < 2; ++u) {
+                                        uint4 w;
+                                        uint32_t drop, allow = ~0u;
+                                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(pv + 512u * u) : "memory");
+                                        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(drop) : "r"(pb + 32u * u) : "memory");
+                                        if (decltype(masked)::value) asm volatile("ld.shared.u8 %0, [%1];" : "=r"(allow) : "r"(pm + 32u * u) : "memory");
+                                        widen8<kF16>(keep_entries(w, allow & ~drop, El<kF16>::kNegInf2), z[u]);
+                                    }
+                                    lane_add16(acc, z, k2, decltype(entropy)::value);
+                                }
+                            };
+                            if (sh.mask) {
+                                if (want_ent) stream(std::true_type{}, std::true_type{}); else stream(std::true_type{}, std::false_type{});
+                            } else {
+                                if (want_ent) stream(std::false_type{}, std::true_type{}); else stream(std::false_type{}, std::false_type{});
+                            }
+                        } else {
                         auto turn = [&](int i, auto kind) {
                             constexpr bool whole = decltype(kind)::value;
                             float2 z[2][4];
@@ -1101,6 +1158,7 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                         } else {
                             for (int i = lane; i - lane < n; i += 64) turn(i, std::false_type{});
                         }
+                        }
                     } else {
 #pragma unroll 2
                         for (int i = lane; i < n; i += 32) {
@@ -1117,11 +1175,12 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                 if (mine) {
                     __syncwarp();                          // (what follows writes over what the stream of vectors wrote)
                     const int last = l1 + (y_here ? 1 : 0);
+                    if (kLp) el = entry_of(l0 + lane);
                     for (int k = l0 + lane; k - lane < last;) {
                         if (el >= 0) {
                             const float x = form(k, el, sign);
                             if (!kLp) store1<kMode, kF16>(dst, el + tb, x);
-                            else if (el + tb == y) s_zy[r] = x * inv_tau;
+                            else if (el + tb == y) s_zy[r] = x * s_w.inv_tau;
                             else lane_add1(acc, x, k2, want_ent);
                         }
                         k += 32;
@@ -1132,13 +1191,13 @@ __global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __gr
                     if (kLp && y_here && lane == 0) atomicAnd(s_bits + ((y - tb) >> 5), ~(1u << ((y - tb) & 31)));
                     __syncwarp();                          // every lane is done with the buffer
                 }
-                if (!a.sparse) {
+                if (!sparse) {
                     if (lane == 0 && t + a.n_bufs < te) issue(t + a.n_bufs, slot);
                     slot = slot + 1 == a.n_bufs ? 0 : slot + 1;
                 }
 
                 if (kLp) {
-                    const LpAcc mine = lane_done(acc, k2, inv_tau);
+                    const LpAcc mine = lane_done(acc, k2, s_w.inv_tau);
                     const float M = warp_max(mine.m);
                     const float up = M - mine.m, sc = ex2(-up * kLog2e);
                     float s = mine.s * sc, ez = sc * (mine.ez - up * mine.s);

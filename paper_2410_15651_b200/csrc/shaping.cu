@@ -10,11 +10,14 @@ namespace {
 
 using namespace rlhf;
 
+// Entries of a row and tokens of a history are counted with 32 bits, some turns past their end.
+constexpr int kMost = 1 << 30;
+
 // The shaping's arguments into the kernel's form.
 int check_shaping(const rlhf_shaping_t* sh, ShapingArgs& out)
 {
     if (!sh) return RLHF_ERR_NULL;
-    if (sh->prompt_len < 0 || sh->tokens_len < 0) return RLHF_ERR_SHAPE;
+    if (sh->prompt_len < 0 || sh->tokens_len < 0 || sh->prompt_len > kMost || sh->tokens_len > kMost) return RLHF_ERR_SHAPE;
     if ((sh->prompt_len > 0 && !sh->prompt) || (sh->tokens_len > 0 && !sh->tokens)) return RLHF_ERR_NULL;
     if (sh->prompt_stride_b < 0 || sh->tokens_stride_b < 0 || sh->bias_stride_b < 0 || sh->mask_stride_b < 0 ||
         sh->mask_stride_t < 0)
@@ -62,6 +65,7 @@ int check_common(int dtype, const int* lengths, int B, int T, int V, const void*
 {
     if (dtype != RLHF_BF16 && dtype != RLHF_F16) return RLHF_ERR_SCALAR;
     if (int e = check_shape(B, T, V)) return e;
+    if (V > kMost) return RLHF_ERR_SHAPE;
     if (!aligned(lengths, 4)) return RLHF_ERR_ALIGN;
     return check_workspace(ws, ws_bytes, objective_workspace_bytes(B, T));
 }
@@ -161,8 +165,8 @@ int launch_shaping(ShapeKernelArgs& a, bool f16, bool any, cudaStream_t s)
 
     if constexpr (!kLp) {
         // short sequences, and batches of at most four blocks per SM
-        constexpr int kMost = kRowThreads * kRowVecs;
-        const int slices = (vecs + kMost - 1) / kMost;
+        constexpr int kHeld = kRowThreads * kRowVecs;
+        const int slices = (vecs + kHeld - 1) / kHeld;
         if (a.T < kShapeShortRows || rows * slices <= 4ll * dev.sm_count) {
             a.n_slices = slices;
             while (rows * a.n_slices < 2ll * dev.sm_count && vecs / a.n_slices > kRowThreads) ++a.n_slices;
@@ -173,12 +177,12 @@ int launch_shaping(ShapeKernelArgs& a, bool f16, bool any, cudaStream_t s)
         }
     }
     // Segments of whole turns of a warp, with two buffers at least.  Log-probs of few rows are cut finer, so that they reach every SM.
-    constexpr int kTurn = kLp ? 64 : 32;
+    constexpr int kTurn = kLp ? 64 : 32, kWarps = kLp ? kShapeLpWarps : kShapeWarps;
     const size_t room = (size_t)dev.max_smem_optin - 12 * 1024;
     int warps = 0;
     for (a.n_slices = 1;; ++a.n_slices) {
         const int per = (vecs + a.n_slices - 1) / a.n_slices;
-        a.segment = ((per + kShapeWarps - 1) / kShapeWarps + kTurn - 1) / kTurn * kTurn;
+        a.segment = ((per + kWarps - 1) / kWarps + kTurn - 1) / kTurn * kTurn;
         warps = std::max(2, (per + a.segment - 1) / a.segment);
         if (a.segment > kShapeSegment) continue;
         if (kLp && a.segment > kTurn && rows * a.n_slices < dev.sm_count && a.n_slices < kShapeMaxCluster) continue;

@@ -88,6 +88,15 @@ def test_the_shaping(lib, p):
             assert call(sh=shaping(p, **{k: p + 2}), **ok) == ALIGN, (name, k)
 
 
+def test_sizes_beyond_what_is_counted(lib, p):
+    most = 1 << 30
+    for name, call in calls(lib, p):
+        assert call(V=most + 1) == SHAPE, name
+        for k in ("prompt_len", "tokens_len"):
+            assert call(sh=shaping(p, **{k: most}), wsn=100) == WORKSPACE, (name, k)
+            assert call(sh=shaping(p, **{k: most + 1}), wsn=100) == SHAPE, (name, k)
+
+
 def test_what_each_of_them_checks(lib, p):
     c = dict(calls(lib, p))
     for odt in (1, 3, -1):
