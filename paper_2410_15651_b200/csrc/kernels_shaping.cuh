@@ -724,7 +724,7 @@ struct ShapeRow {
 // kAny: rows of any alignment.  The vectors then follow the rows that are written (the source's where none are), and a source
 // that is off them by `delta` entries is shifted into place from two aligned vectors.
 template <int kMode, bool kF16, bool kAny>
-__global__ void __launch_bounds__((kMode == kShapeLp ? kShapeLpWarps : kShapeWarps) * 32, 1) shaping_kernel(const __grid_constant__ ShapeKernelArgs a)
+__device__ __forceinline__ void shaping_walk(const ShapeKernelArgs& a)
 {
     constexpr bool kLp = kMode == kShapeLp, kLpBwd = kMode == kShapeLpBwd, kBwd = kMode == kShapeBwd, k32 = kMode == kShape32;
     constexpr bool kTokens = kLp || kLpBwd;                // a row has a generated token
@@ -873,16 +873,16 @@ __global__ void __launch_bounds__((kMode == kShapeLp ? kShapeLpWarps : kShapeWar
             // The row's mask words from that of the warp's first entry on, into the half of `words` that is not in use.
             auto issue_words = [&](int t) {
                 const int w0 = (8 * v0 - (kAny ? row_at(t).oo : 0)) >> 5;
-                const uint32_t* const m = s_w.mask + (long long)t * sh.mask_stride_t + w0;
-                const uint32_t to = smem_u32(words) + 4u * (uint32_t)((t & 1) * n_words);
-                const int left = ((V + 31) >> 5) - w0;     // (a row may leave the last warp nothing)
-                if (!kAny && left >= a.segment / 4 && ((uintptr_t)m & 15) == 0) {
+                const uint32_t* const m = s_w.mask + (long long)t * sh.mask_stride_t;
+                // (16 bytes at a time for log-probs, which are bound by their instructions: 699 us where words take 785)
+                if (kLp && !kAny && ((V + 31) >> 5) - w0 >= a.segment / 4 && ((uintptr_t)(m + w0) & 15) == 0) {
                     for (int i = lane; i < a.segment / 16; i += 32)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16u * i), "l"(m + 4 * i) : "memory");
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                                     ::"r"(smem_u32(words + (t & 1) * n_words + 4 * i)), "l"(m + w0 + 4 * i) : "memory");
                 } else {
-                    for (int i = lane; i < min(n_words, left); i += 32)
-                        if (w0 + i >= 0)
-                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4u * i), "l"(m + i) : "memory");
+                    for (int i = lane; i < n_words; i += 32)
+                        if (w0 + i >= 0 && w0 + i < (V + 31) >> 5)
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(words + (t & 1) * n_words + i)), "l"(m + w0 + i) : "memory");
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
@@ -1273,6 +1273,17 @@ __global__ void __launch_bounds__((kMode == kShapeLp ? kShapeLpWarps : kShapeWar
             if (a.out_entropy) a.out_entropy[i] = 0.f;
         }
     }
+}
+
+template <int kMode, bool kF16, bool kAny>
+__global__ void __launch_bounds__(kShapeWarps * 32, 1) shaping_kernel(const __grid_constant__ ShapeKernelArgs a)
+{
+    shaping_walk<kMode, kF16, kAny>(a);
+}
+template <bool kF16, bool kAny>
+__global__ void __launch_bounds__(kShapeLpWarps * 32, 1) shaping_lp_kernel(const __grid_constant__ ShapeKernelArgs a)
+{
+    shaping_walk<kShapeLp, kF16, kAny>(a);
 }
 
 }  // namespace rlhf

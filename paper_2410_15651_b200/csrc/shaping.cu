@@ -112,7 +112,9 @@ int resident_units(K kernel, int cluster, int threads, size_t smem, const Device
 template <int kMode, bool kF16, bool kAny>
 int launch_shaping_as(ShapeKernelArgs& a, int warps, const DeviceInfo& dev, cudaStream_t s)
 {
-    auto kernel = shaping_kernel<kMode, kF16, kAny>;
+    void (*kernel)(const ShapeKernelArgs) = nullptr;
+    if constexpr (kMode == kShapeLp) kernel = shaping_lp_kernel<kF16, kAny>;
+    else kernel = shaping_kernel<kMode, kF16, kAny>;
     const size_t smem = shape_smem(a, warps, kAny).total;
     RLHF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (int e = keep_max_carveout(kernel)) return e;
